@@ -64,7 +64,9 @@ typedef enum {
   DA2_ERR_HIP = -4          /* the HIP runtime reported an error (launch or query)   */
 } da2_status;
 
-typedef enum { DA2_BF16 = 0, DA2_FP32 = 1 } da2_dtype;
+/* DA2_FP16 is taken by the token operators at the end of this file only; the
+ * four calls above return DA2_ERR_INVALID_ARG for it. */
+typedef enum { DA2_BF16 = 0, DA2_FP32 = 1, DA2_FP16 = 2 } da2_dtype;
 typedef enum { DA2_SCOPE_HEAD = 0, DA2_SCOPE_ROW = 1 } da2_scope;
 
 /* Encodings of the 4-bit path. NVFP4 is the paper's format (E2M1 with an
@@ -346,6 +348,69 @@ int32_t da2_ops_offsets(const da2_problem* p, int32_t fmt4, int32_t with16, int6
 int32_t da2_mixed_attn(const void* ops, int64_t ops_bytes, const void* lists, const int32_t* layout,
                        const da2_problem* p, int32_t fmt4, const da2_tensor* out, void* O,
                        void* stream);
+
+/* ---- Token operators: what a layer computes around the attention ------------
+ *
+ * These calls take no da2_problem: they work on [B, H, N, C] token rows in any
+ * memory order with C contiguous (da2_tensor; hidden rows are H = 1), of type
+ * bf16, fp16 or fp32 as each call says. Unlike the calls above they place no
+ * condition on alignment beyond the element's own. For every one of them:
+ *   - strides are >= 0 and at most 2^40 elements; the stride of an extent of 1
+ *     is not looked at. An output's rows must not overlap one another; an input
+ *     may repeat rows (stride 0).
+ *   - an output may be the same memory as an input only where a call says so,
+ *     and then with the input's strides.
+ *   - sums and statistics are held in fp32 or more; results are rounded once.
+ *   - results do not depend on the order in which workgroups run (no atomics).
+ *   - extents are >= 1, B <= 65535, and H*N <= 2^31 - 1; else INVALID_ARG. */
+
+/* Rows of a token tensor. */
+typedef struct {
+  int32_t B, H, N, C;
+} da2_rows;
+
+typedef enum { DA2_NORM_LAYER = 0, DA2_NORM_RMS = 1 } da2_norm_kind;
+
+/* Row norm and its weights. stride_b is 0 for a weight and bias [C] that all
+ * rows share, or the distance in elements between the samples' ones [B][C]
+ * (adaptive norms), at least C. plus_one: the factor is 1 + w (w a scale around zero). */
+typedef struct {
+  int32_t kind;     /* da2_norm_kind                      */
+  int32_t wdtype;   /* da2_dtype of w, b, dw and db       */
+  int32_t plus_one; /* 0: factor w, 1: factor 1 + w       */
+  int32_t reserved;
+  int64_t stride_b;
+  double eps;       /* >= 0, added to the variance (the mean square) */
+} da2_norm_desc;
+
+/* Row norm: y = (x - mean) rstd f + b over the C channels of each row, with
+ * rstd = 1 / sqrt(var + eps), var the mean of (x - mean)^2, and f = w or 1 + w;
+ * DA2_NORM_RMS takes mean = 0.
+ *   X      device, rows *r per *x; Y device out per *y, of X's dtype (may be X)
+ *   w, b   device, per *n, or NULL: factor 1, no bias
+ *   stats  device out, float32 [B*H*N][2]: mean and rstd of each row (row
+ *          (b*H + h)*N + n), or NULL. da2_norm_bwd reads them. */
+int32_t da2_norm(const void* X, const da2_tensor* x, const da2_rows* r, const da2_norm_desc* n,
+                 const void* w, const void* b, void* Y, const da2_tensor* y, float* stats,
+                 void* stream);
+
+/* Host only: workspace bytes that da2_norm_bwd needs for dw or db of these rows
+ * of X's dtype; adaptive (0 or 1): weights per sample (stride_b > 0). */
+int32_t da2_norm_ws_bytes(const da2_rows* r, int32_t dtype, int32_t adaptive, int64_t* bytes);
+
+/* Gradients of da2_norm. With g = dY f and xh = (x - mean) rstd:
+ *   dX = rstd (g - mean(g) - xh mean(g xh))   (RMS: without mean(g))
+ *   dw = sum over the rows of dY xh, db = sum of dY (per sample when stride_b > 0)
+ *   dY, X   device, of one dtype; stats as da2_norm wrote them for this X and *n
+ *   w       as in da2_norm (NULL: factor 1)
+ *   dX      device out per *dx, of X's dtype, or NULL (may be dY or X)
+ *   dw, db  device out of n->wdtype, laid out like w and b, or NULL
+ *   ws      device scratch of da2_norm_ws_bytes, needed when dw or db is given
+ * Errors: INVALID_ARG when all three outputs are NULL; WORKSPACE. */
+int32_t da2_norm_bwd(const void* dY, const da2_tensor* dy, const void* X, const da2_tensor* x,
+                     const da2_rows* r, const da2_norm_desc* n, const void* w, const float* stats,
+                     void* dX, const da2_tensor* dx, void* dw, void* db, void* ws, int64_t ws_bytes,
+                     void* stream);
 
 #ifdef __cplusplus
 }

@@ -10,18 +10,20 @@ HERE = os.path.dirname(os.path.abspath(__file__))
 LIB_PATH = os.path.join(HERE, "libda2.so")
 
 DA2_OK, DA2_ERR_INVALID_ARG, DA2_ERR_UNSUPPORTED, DA2_ERR_WORKSPACE, DA2_ERR_HIP = 0, -1, -2, -3, -4
-DA2_BF16, DA2_FP32 = 0, 1
+DA2_BF16, DA2_FP32, DA2_FP16 = 0, 1, 2
 DA2_SCOPE_HEAD, DA2_SCOPE_ROW = 0, 1
 DA2_PART_TILES8, DA2_PART_RAGGED = 0, 1
 DA2_FMT4_NVFP4, DA2_FMT4_MXFP4 = 0, 1
 DA2_RANK_NOALLOC_MAX_BYTES = 8 << 20   # include/da2.h
 DA2_OPS_LAYOUT_VERSION = 2
+DA2_NORM_LAYER, DA2_NORM_RMS = 0, 1
 DA2_ATTN_ERR_LAYOUT, DA2_ATTN_ERR_FMT4, DA2_ATTN_ERR_NO16 = 1, 2, 4
 TAG_MARKER = 0xDA200000   # encoding tag in word 3 of each head's g entry
 
 # Every symbol include/da2.h declares.
 EXPORTS = ("da2_status_string", "da2_sizes", "da2_ops_layout_version", "da2_layout_build", "da2_draft_map", "da2_ws_draft_offsets",
-           "da2_rank_assign", "da2_rank_assign_noalloc", "da2_lists_offsets", "da2_prep_operands", "da2_ops_offsets", "da2_mixed_attn")
+           "da2_rank_assign", "da2_rank_assign_noalloc", "da2_lists_offsets", "da2_prep_operands", "da2_ops_offsets", "da2_mixed_attn",
+           "da2_norm", "da2_norm_ws_bytes", "da2_norm_bwd")
 
 
 class Problem(ctypes.Structure):
@@ -43,6 +45,15 @@ class Sizes(ctypes.Structure):
                 ("ws_prep_bytes", ctypes.c_int64)]
 
 
+class Rows(ctypes.Structure):
+    _fields_ = [("B", ctypes.c_int32), ("H", ctypes.c_int32), ("N", ctypes.c_int32), ("C", ctypes.c_int32)]
+
+
+class NormDesc(ctypes.Structure):
+    _fields_ = [("kind", ctypes.c_int32), ("wdtype", ctypes.c_int32), ("plus_one", ctypes.c_int32),
+                ("reserved", ctypes.c_int32), ("stride_b", ctypes.c_int64), ("eps", ctypes.c_double)]
+
+
 class Da2Error(RuntimeError):
     def __init__(self, call, status, lib):
         msg = lib.da2_status_string(status).decode()
@@ -62,6 +73,7 @@ def lib():
         L = ctypes.CDLL(LIB_PATH)
         vp, i32, i64, dbl = ctypes.c_void_p, ctypes.c_int32, ctypes.c_int64, ctypes.c_double
         P, T, S = ctypes.POINTER(Problem), ctypes.POINTER(Tensor), ctypes.POINTER(Sizes)
+        R, ND = ctypes.POINTER(Rows), ctypes.POINTER(NormDesc)
         pi64, pi32 = ctypes.POINTER(ctypes.c_int64), ctypes.POINTER(ctypes.c_int32)
         sig = {
             "da2_status_string": (ctypes.c_char_p, [i32]),
@@ -76,6 +88,9 @@ def lib():
             "da2_prep_operands": (i32, [vp, vp, vp, T, vp, P, i32, i32, vp, vp, i64, vp, i64, vp]),
             "da2_ops_offsets": (i32, [P, i32, i32, pi64]),
             "da2_mixed_attn": (i32, [vp, i64, vp, vp, P, i32, T, vp, vp]),
+            "da2_norm": (i32, [vp, T, R, ND, vp, vp, vp, T, vp, vp]),
+            "da2_norm_ws_bytes": (i32, [R, i32, i32, pi64]),
+            "da2_norm_bwd": (i32, [vp, T, vp, T, R, ND, vp, vp, vp, T, vp, vp, vp, i64, vp]),
         }
         for name, (res, args) in sig.items():
             f = getattr(L, name)

@@ -4,7 +4,13 @@ Argument marshalling only: tensors are torch tensors on the GPU (device
 memory and streams come from PyTorch); every step of the path runs in the
 library's HIP kernels. Each call is enqueued on ``stream`` (default: torch's
 current stream) and returns without synchronizing.
+
+The token operators (norm, rotary positions, differential attention) check
+that their tensors' shapes and types belong together and that all of them are
+on one GPU, and raise ValueError before the call otherwise. They run on the
+tensors' GPU, whichever device is current.
 """
+import contextlib
 import ctypes
 from dataclasses import dataclass
 
@@ -12,8 +18,9 @@ import numpy as np
 import torch
 
 from . import _lib
-from ._lib import (DA2_BF16, DA2_FMT4_MXFP4, DA2_FMT4_NVFP4, DA2_FP32, DA2_PART_RAGGED, DA2_PART_TILES8,
-                   DA2_SCOPE_HEAD, DA2_SCOPE_ROW, Problem, Tensor, check, lib)
+from ._lib import (DA2_BF16, DA2_FMT4_MXFP4, DA2_FMT4_NVFP4, DA2_FP16, DA2_FP32, DA2_NORM_LAYER, DA2_NORM_RMS,
+                   DA2_PART_RAGGED, DA2_PART_TILES8, DA2_SCOPE_HEAD, DA2_SCOPE_ROW, NormDesc, Problem, Rows, Tensor,
+                   check, lib)
 
 SCOPES = {"head": DA2_SCOPE_HEAD, "row": DA2_SCOPE_ROW}
 PARTITIONS = {"tiles8": DA2_PART_TILES8, "ragged": DA2_PART_RAGGED}
@@ -165,3 +172,102 @@ def attention(Q, K, V, buf, lam, budgets, O, stream=None, num16=0, fmt4=None):
     da2_prep_operands(Q, K, V, buf.layout, p, int(num16 > 0), fmt4, buf.stats, buf.ops, None, stream)
     da2_mixed_attn(buf.ops, buf.lists, buf.layout, p, O, stream, fmt4)
     return O
+
+
+# ---- token operators ---------------------------------------------------------------
+DTYPES = {torch.bfloat16: DA2_BF16, torch.float32: DA2_FP32, torch.float16: DA2_FP16}
+NORM_KINDS = {"layer": DA2_NORM_LAYER, "rms": DA2_NORM_RMS}
+
+
+def _rows(name, x, shape=None, dtype=None):
+    """Descriptor of a [B, H, N, C] tensor, checked against the shape and type it must have."""
+    if x.dim() != 4 or (x.stride(3) != 1 and x.shape[3] > 1):
+        raise ValueError(f"{name}: expected a [B, H, N, C] tensor with its last dimension contiguous")
+    if x.dtype not in DTYPES or (dtype is not None and x.dtype != dtype):
+        raise ValueError(f"{name}: unsupported dtype {x.dtype}" + (f", expected {dtype}" if dtype else ""))
+    if shape is not None and tuple(x.shape) != tuple(shape):
+        raise ValueError(f"{name}: expected shape {tuple(shape)}, got {tuple(x.shape)}")
+    sb, sh, sn, _ = x.stride()
+    return Tensor(sb, sh, sn, DTYPES[x.dtype], 0)
+
+
+def _plain(name, x, shape, dtype):
+    """Address of a contiguous tensor of the given shape and type (None: a null pointer)."""
+    if x is None:
+        return None
+    if tuple(x.shape) != tuple(shape) or x.dtype != dtype or not x.is_contiguous():
+        raise ValueError(f"{name}: expected a contiguous {dtype} tensor of shape {tuple(shape)}")
+    return x.data_ptr()
+
+
+def _addr(x):
+    return None if x is None else x.data_ptr()
+
+
+def _on(stream, *tensors):
+    """The stream's handle, and a context in which the tensors' GPU is the current device."""
+    dev = tensors[0].device
+    if dev.type != "cuda" or any(t is not None and t.device != dev for t in tensors):
+        raise ValueError("expected all tensors on one GPU")
+    if stream is not None and stream.device != dev:
+        raise ValueError(f"the stream belongs to {stream.device}, the tensors to {dev}")
+    s = torch.cuda.current_stream(dev) if stream is None else stream
+    here = torch.cuda.current_device() == dev.index
+    return s.cuda_stream, contextlib.nullcontext() if here else torch.cuda.device(dev)
+
+
+def _norm_desc(X, w, b, kind, eps, plus_one):
+    """Rows and NormDesc of a norm over X's last dimension with weights [C] or [B, C]."""
+    B, H, N, C = X.shape
+    stride, wdtype = 0, X.dtype
+    given = [(n, t) for n, t in (("w", w), ("b", b)) if t is not None]
+    for name, t in given:
+        if t.dtype not in DTYPES or tuple(t.shape) not in ((C,), (B, C)) or (C > 1 and t.stride(-1) != 1):
+            raise ValueError(f"{name}: expected [C] or [B, C] weights with C contiguous")
+        if t.shape != given[0][1].shape or t.dtype != given[0][1].dtype or t.stride() != given[0][1].stride():
+            raise ValueError("weights and bias (and their gradients) must share shape, strides and dtype")
+        # one sample's weights serve all its rows whatever their stride
+        stride, wdtype = (t.stride(0) if t.dim() == 2 and B > 1 else 0), t.dtype
+        if t.dim() == 2 and B > 1 and stride < C:
+            raise ValueError(f"{name}: the samples' weights overlap")
+    return Rows(B, H, N, C), NormDesc(NORM_KINDS[kind], DTYPES[wdtype], int(plus_one), 0, stride, float(eps))
+
+
+def da2_norm(X, Y, w=None, b=None, kind="layer", eps=1e-6, plus_one=False, stats=None, stream=None):
+    """Y = norm of X's rows (the last dimension of [B, H, N, C]) times w (or 1 + w) plus b; w, b: [C], or [B, C] per
+    sample. ``stats``: float32 [B, H, N, 2] for da2_norm_bwd. Y may be X."""
+    x = _rows("X", X)
+    y = _rows("Y", Y, X.shape, X.dtype)
+    r, n = _norm_desc(X, w, b, kind, eps, plus_one)
+    st = _plain("stats", stats, X.shape[:3] + (2,), torch.float32)
+    s, dev = _on(stream, X, Y, w, b, stats)
+    with dev:
+        check("da2_norm", lib().da2_norm(X.data_ptr(), x, r, n, _addr(w), _addr(b), Y.data_ptr(), y, st, s))
+    return Y
+
+
+def da2_norm_ws_bytes(X, w=None):
+    """Workspace bytes of da2_norm_bwd for the gradients of weights like ``w`` ([C] or [B, C])."""
+    _rows("X", X)
+    B, H, N, C = X.shape
+    out = ctypes.c_int64()
+    check("da2_norm_ws_bytes", lib().da2_norm_ws_bytes(Rows(B, H, N, C), DTYPES[X.dtype],
+                                                       int(w is not None and w.dim() == 2 and B > 1), out))
+    return out.value
+
+
+def da2_norm_bwd(dY, X, stats, dX=None, w=None, dw=None, db=None, kind="layer", plus_one=False, ws=None, stream=None):
+    """Gradients of da2_norm; dX, dw and db are written where given. ``ws``: da2_norm_ws_bytes(X, w) bytes, for dw and db."""
+    x = _rows("X", X)
+    dy = _rows("dY", dY, X.shape, X.dtype)
+    dx = None if dX is None else _rows("dX", dX, X.shape, X.dtype)
+    given = [t for t in (w, dw, db) if t is not None]
+    r, n = _norm_desc(X, given[0] if given else None, given[-1] if given else None, kind, 0.0, plus_one)
+    if len(given) == 3:
+        _norm_desc(X, w, dw, kind, 0.0, plus_one)
+    st = _plain("stats", stats, X.shape[:3] + (2,), torch.float32)
+    s, dev = _on(stream, X, dY, stats, dX, w, dw, db, ws)
+    with dev:
+        check("da2_norm_bwd", lib().da2_norm_bwd(
+            dY.data_ptr(), dy, X.data_ptr(), x, r, n, _addr(w), st, _addr(dX), dx, _addr(dw), _addr(db), _addr(ws),
+            0 if ws is None else ws.numel() * ws.element_size(), s))

@@ -4,15 +4,18 @@
 #include <hip/hip_runtime.h>
 
 #include <algorithm>
-#include <atomic>
 #include <cmath>
 #include <cstring>
 #include <vector>
 
 #include "../../include/da2.h"
+#include "host_util.hpp"
 #include "launch.hpp"
 
 namespace {
+
+using da2::check_device;
+using da2::hip_status;
 
 constexpr int64_t kAlign = 256;
 inline int64_t align_up(int64_t x) { return (x + kAlign - 1) / kAlign * kAlign; }
@@ -135,26 +138,6 @@ int32_t check_tensor(const da2_tensor* t, const Dims& d, bool out) {
 }
 
 bool aligned16(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 15u) == 0; }
-
-// gfx950 check, cached per device ordinal (0 unknown, 1 ok, 2 unsupported).
-std::atomic<int8_t> g_arch_ok[64];
-
-int32_t check_device() {
-  int dev = -1;
-  if (hipGetDevice(&dev) != hipSuccess || dev < 0) return DA2_ERR_UNSUPPORTED;
-  if (dev < 64) {
-    int8_t c = g_arch_ok[dev].load(std::memory_order_relaxed);
-    if (c == 1) return DA2_OK;
-    if (c == 2) return DA2_ERR_UNSUPPORTED;
-  }
-  hipDeviceProp_t prop;
-  if (hipGetDeviceProperties(&prop, dev) != hipSuccess) return DA2_ERR_HIP;
-  const bool ok = std::strncmp(prop.gcnArchName, "gfx950", 6) == 0;
-  if (dev < 64) g_arch_ok[dev].store(ok ? 1 : 2, std::memory_order_relaxed);
-  return ok ? DA2_OK : DA2_ERR_UNSUPPORTED;
-}
-
-int32_t hip_status(hipError_t e) { return e == hipSuccess ? DA2_OK : DA2_ERR_HIP; }
 
 // Ragged partition of one H x W frame (the candidate family documented in
 // da2.h): the label of every cell, row-major.
