@@ -412,6 +412,69 @@ int32_t da2_norm_bwd(const void* dY, const da2_tensor* dy, const void* X, const 
                      void* dX, const da2_tensor* dx, void* dw, void* db, void* ws, int64_t ws_bytes,
                      void* stream);
 
+typedef enum { DA2_ROPE_INTERLEAVED = 0, DA2_ROPE_HALF = 1 } da2_rope_layout;
+typedef enum {
+  DA2_ROPE_PLAIN = 0,
+  DA2_ROPE_LINEAR = 1, /* every frequency divided by factor */
+  DA2_ROPE_NTK = 2,    /* base times factor^(D / (D - 2)): the slowest pair is stretched by factor */
+  DA2_ROPE_YARN = 3    /* by frequency: fast pairs keep theirs, slow ones are divided by factor, a ramp between */
+} da2_rope_scaling;
+
+/* Rotary positions. A row of d channels is d / block blocks that rotate alike
+ * (block = d, or d/2 for the halves of differential attention); the first
+ * rot = rot_axis[0] + .. + rot_axis[axes-1] channels of each block rotate, the
+ * rest stay. Pair p of rot/2 is channels (2p, 2p+1) of the block (INTERLEAVED)
+ * or (p, p + rot/2) (HALF); the first rot_axis[0]/2 pairs turn with the token's
+ * position on axis 0, the next rot_axis[1]/2 with axis 1, and so on. */
+typedef struct {
+  int32_t layout;      /* da2_rope_layout */
+  int32_t block;
+  int32_t axes;        /* 1, 2 or 3 */
+  int32_t rot_axis[3]; /* channels of each axis: even, >= 2; unused ones 0 */
+} da2_rope_desc;
+
+/* Frequencies of a plan: base > 1; factor >= 1 (> 1 only with a scaling);
+ * orig_len, beta_fast, beta_slow for YARN: over orig_len positions, pairs that
+ * turn beta_fast times or more keep their frequency, those that turn beta_slow
+ * times or fewer are stretched. */
+typedef struct {
+  int32_t scaling; /* da2_rope_scaling */
+  int32_t orig_len;
+  double base, factor, beta_fast, beta_slow;
+} da2_rope_freq;
+
+/* Host only: turns[rot/2], the turns (angle / 2 pi) per position of every pair:
+ * base^(-2i/D) / (2 pi) for pair i of an axis of D channels, scaled as *f says;
+ * and *scale, the factor of cosine and sine (1; 0.1 ln(factor) + 1 for YARN).
+ * Copy turns to a device buffer for da2_rope. */
+int32_t da2_rope_plan(const da2_rope_desc* r, const da2_rope_freq* f, double* turns, double* scale);
+
+/* Rows of Q and K: Hq heads of Q and Hk of K (0: Q alone), N tokens of d
+ * channels each. */
+typedef struct {
+  int32_t B, Hq, Hk, N, d;
+  int32_t grid_h, grid_w; /* the token grid, see pos; 0 when positions are given */
+  int32_t inverse;        /* 1: the transposed rotation, which is the gradient */
+} da2_rope_rows;
+
+/* Rotates every row of Q and of K: (a, b) -> scale (a cos - b sin, a sin + b cos)
+ * with the angle 2 pi turns[p] pos, computed in float64 and reduced by whole
+ * turns, so that far positions lose nothing; inverse = 1 turns back (same scale).
+ *   turns   device, float64 [rot/2]; scale finite
+ *   pos     device, int32 [B][N][axes] with pos_stride_b elements between the
+ *           samples (0: shared, else >= N*axes), any values; or NULL: the token
+ *           numbers of the grid, n on 1 axis, (n / grid_w, n % grid_w) on 2,
+ *           (n / (grid_h grid_w), n / grid_w % grid_h, n % grid_w) on 3
+ *   Q, K    device, [B, H, N, d] per *q and *k, of one dtype; Qo, Ko device out
+ *           per *qo and *ko, of that dtype (may be Q and K). K, Ko, k, ko are
+ *           not looked at when Hk = 0.
+ * Errors: INVALID_ARG for d not a multiple of block, rot > block, a d above
+ * 65,536, or a grid that does not fit the axes. */
+int32_t da2_rope(const da2_rope_desc* r, const double* turns, double scale, const int32_t* pos,
+                 int64_t pos_stride_b, const da2_rope_rows* s, const void* Q, const da2_tensor* q,
+                 void* Qo, const da2_tensor* qo, const void* K, const da2_tensor* k, void* Ko,
+                 const da2_tensor* ko, void* stream);
+
 #ifdef __cplusplus
 }
 #endif

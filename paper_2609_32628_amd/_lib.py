@@ -17,13 +17,15 @@ DA2_FMT4_NVFP4, DA2_FMT4_MXFP4 = 0, 1
 DA2_RANK_NOALLOC_MAX_BYTES = 8 << 20   # include/da2.h
 DA2_OPS_LAYOUT_VERSION = 2
 DA2_NORM_LAYER, DA2_NORM_RMS = 0, 1
+DA2_ROPE_INTERLEAVED, DA2_ROPE_HALF = 0, 1
+DA2_ROPE_PLAIN, DA2_ROPE_LINEAR, DA2_ROPE_NTK, DA2_ROPE_YARN = 0, 1, 2, 3
 DA2_ATTN_ERR_LAYOUT, DA2_ATTN_ERR_FMT4, DA2_ATTN_ERR_NO16 = 1, 2, 4
 TAG_MARKER = 0xDA200000   # encoding tag in word 3 of each head's g entry
 
 # Every symbol include/da2.h declares.
 EXPORTS = ("da2_status_string", "da2_sizes", "da2_ops_layout_version", "da2_layout_build", "da2_draft_map", "da2_ws_draft_offsets",
            "da2_rank_assign", "da2_rank_assign_noalloc", "da2_lists_offsets", "da2_prep_operands", "da2_ops_offsets", "da2_mixed_attn",
-           "da2_norm", "da2_norm_ws_bytes", "da2_norm_bwd")
+           "da2_norm", "da2_norm_ws_bytes", "da2_norm_bwd", "da2_rope_plan", "da2_rope")
 
 
 class Problem(ctypes.Structure):
@@ -54,6 +56,22 @@ class NormDesc(ctypes.Structure):
                 ("reserved", ctypes.c_int32), ("stride_b", ctypes.c_int64), ("eps", ctypes.c_double)]
 
 
+class RopeDesc(ctypes.Structure):
+    _fields_ = [("layout", ctypes.c_int32), ("block", ctypes.c_int32), ("axes", ctypes.c_int32),
+                ("rot_axis", ctypes.c_int32 * 3)]
+
+
+class RopeFreq(ctypes.Structure):
+    _fields_ = [("scaling", ctypes.c_int32), ("orig_len", ctypes.c_int32), ("base", ctypes.c_double),
+                ("factor", ctypes.c_double), ("beta_fast", ctypes.c_double), ("beta_slow", ctypes.c_double)]
+
+
+class RopeRows(ctypes.Structure):
+    _fields_ = [("B", ctypes.c_int32), ("Hq", ctypes.c_int32), ("Hk", ctypes.c_int32), ("N", ctypes.c_int32),
+                ("d", ctypes.c_int32), ("grid_h", ctypes.c_int32), ("grid_w", ctypes.c_int32),
+                ("inverse", ctypes.c_int32)]
+
+
 class Da2Error(RuntimeError):
     def __init__(self, call, status, lib):
         msg = lib.da2_status_string(status).decode()
@@ -74,6 +92,8 @@ def lib():
         vp, i32, i64, dbl = ctypes.c_void_p, ctypes.c_int32, ctypes.c_int64, ctypes.c_double
         P, T, S = ctypes.POINTER(Problem), ctypes.POINTER(Tensor), ctypes.POINTER(Sizes)
         R, ND = ctypes.POINTER(Rows), ctypes.POINTER(NormDesc)
+        RD, RF, RR = ctypes.POINTER(RopeDesc), ctypes.POINTER(RopeFreq), ctypes.POINTER(RopeRows)
+        pdbl = ctypes.POINTER(ctypes.c_double)
         pi64, pi32 = ctypes.POINTER(ctypes.c_int64), ctypes.POINTER(ctypes.c_int32)
         sig = {
             "da2_status_string": (ctypes.c_char_p, [i32]),
@@ -91,6 +111,8 @@ def lib():
             "da2_norm": (i32, [vp, T, R, ND, vp, vp, vp, T, vp, vp]),
             "da2_norm_ws_bytes": (i32, [R, i32, i32, pi64]),
             "da2_norm_bwd": (i32, [vp, T, vp, T, R, ND, vp, vp, vp, T, vp, vp, vp, i64, vp]),
+            "da2_rope_plan": (i32, [RD, RF, pdbl, pdbl]),
+            "da2_rope": (i32, [RD, vp, dbl, vp, i64, RR, vp, T, vp, T, vp, T, vp, T, vp]),
         }
         for name, (res, args) in sig.items():
             f = getattr(L, name)

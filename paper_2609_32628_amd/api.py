@@ -19,8 +19,9 @@ import torch
 
 from . import _lib
 from ._lib import (DA2_BF16, DA2_FMT4_MXFP4, DA2_FMT4_NVFP4, DA2_FP16, DA2_FP32, DA2_NORM_LAYER, DA2_NORM_RMS,
-                   DA2_PART_RAGGED, DA2_PART_TILES8, DA2_SCOPE_HEAD, DA2_SCOPE_ROW, NormDesc, Problem, Rows, Tensor,
-                   check, lib)
+                   DA2_PART_RAGGED, DA2_PART_TILES8, DA2_ROPE_HALF, DA2_ROPE_INTERLEAVED, DA2_ROPE_LINEAR,
+                   DA2_ROPE_NTK, DA2_ROPE_PLAIN, DA2_ROPE_YARN, DA2_SCOPE_HEAD, DA2_SCOPE_ROW, NormDesc, Problem,
+                   RopeDesc, RopeFreq, RopeRows, Rows, Tensor, check, lib)
 
 SCOPES = {"head": DA2_SCOPE_HEAD, "row": DA2_SCOPE_ROW}
 PARTITIONS = {"tiles8": DA2_PART_TILES8, "ragged": DA2_PART_RAGGED}
@@ -176,6 +177,8 @@ def attention(Q, K, V, buf, lam, budgets, O, stream=None, num16=0, fmt4=None):
 
 # ---- token operators ---------------------------------------------------------------
 DTYPES = {torch.bfloat16: DA2_BF16, torch.float32: DA2_FP32, torch.float16: DA2_FP16}
+ROPE_LAYOUTS = {"interleaved": DA2_ROPE_INTERLEAVED, "half": DA2_ROPE_HALF}
+ROPE_SCALINGS = {"none": DA2_ROPE_PLAIN, "linear": DA2_ROPE_LINEAR, "ntk": DA2_ROPE_NTK, "yarn": DA2_ROPE_YARN}
 NORM_KINDS = {"layer": DA2_NORM_LAYER, "rms": DA2_NORM_RMS}
 
 
@@ -271,3 +274,63 @@ def da2_norm_bwd(dY, X, stats, dX=None, w=None, dw=None, db=None, kind="layer", 
         check("da2_norm_bwd", lib().da2_norm_bwd(
             dY.data_ptr(), dy, X.data_ptr(), x, r, n, _addr(w), st, _addr(dX), dx, _addr(dw), _addr(db), _addr(ws),
             0 if ws is None else ws.numel() * ws.element_size(), s))
+
+
+@dataclass
+class Rope:
+    """Plan of the rotary positions: layout ("interleaved" or "half"), channels of a rotated block, rotated channels of
+    each position axis, and the turns per position of every pair (float64 [rot / 2] on the GPU) with the factor of
+    cosine and sine, from da2_rope_plan or the caller's own."""
+    layout: str
+    block: int
+    rot_axis: tuple
+    turns: torch.Tensor
+    scale: float = 1.0
+
+    def desc(self):
+        n = len(self.rot_axis)
+        if not 1 <= n <= 3:
+            raise ValueError("rot_axis: expected 1 to 3 axes")
+        return RopeDesc(ROPE_LAYOUTS[self.layout], self.block, n, (ctypes.c_int32 * 3)(*self.rot_axis))
+
+
+def da2_rope_plan(block, rot_axis, layout="interleaved", base=10000.0, scaling="none", factor=1.0, orig_len=4096,
+                  beta_fast=32.0, beta_slow=1.0, device="cuda"):
+    """Rope of blocks of ``block`` channels with rot_axis[i] of them turning with position axis i. scaling: "none",
+    "linear", "ntk" or "yarn", for contexts ``factor`` times longer than trained on (orig_len: for yarn)."""
+    rope = Rope(layout, block, tuple(rot_axis), torch.empty(max(sum(rot_axis) // 2, 1), dtype=torch.float64))
+    scale = ctypes.c_double()
+    check("da2_rope_plan", lib().da2_rope_plan(
+        rope.desc(), RopeFreq(ROPE_SCALINGS[scaling], orig_len, base, factor, beta_fast, beta_slow),
+        ctypes.cast(rope.turns.data_ptr(), ctypes.POINTER(ctypes.c_double)), scale))
+    rope.turns, rope.scale = rope.turns.to(device), scale.value
+    return rope
+
+
+def da2_rope(rope, Q, Qo, K=None, Ko=None, pos=None, grid=None, inverse=False, stream=None):
+    """Rotates Q (and K) into Qo (and Ko), which may be the inputs. pos: int32 [B or 1, N, axes] positions; without it
+    the tokens are numbered, on 2 and 3 axes over a ``grid`` of (height, width) per frame. inverse: the gradient."""
+    q = _rows("Q", Q)
+    qo = _rows("Qo", Qo, Q.shape, Q.dtype)
+    B, Hq, N, d = Q.shape
+    Hk, k, ko = 0, None, None
+    if (K is None) != (Ko is None):
+        raise ValueError("K and Ko are given together")
+    if K is not None:
+        Hk = K.shape[1] if K.dim() == 4 else 0
+        k = _rows("K", K, (B, Hk, N, d), Q.dtype)
+        ko = _rows("Ko", Ko, K.shape, Q.dtype)
+    axes, stride = len(rope.rot_axis), 0
+    if pos is not None:
+        if tuple(pos.shape) not in ((B, N, axes), (1, N, axes)) or pos.dtype != torch.int32:
+            raise ValueError(f"pos: expected int32 [{B} or 1, {N}, {axes}]")
+        if not pos[0].is_contiguous():
+            raise ValueError("pos: expected each sample's positions contiguous")
+        stride = pos.stride(0) if pos.shape[0] > 1 else 0
+    t = _plain("turns", rope.turns, (sum(rope.rot_axis) // 2,), torch.float64)
+    gh, gw = grid if grid is not None else (0, 0)
+    s, dev = _on(stream, Q, Qo, K, Ko, pos, rope.turns)
+    with dev:
+        check("da2_rope", lib().da2_rope(
+            rope.desc(), t, rope.scale, _addr(pos), stride, RopeRows(B, Hq, Hk, N, d, gh, gw, int(inverse)),
+            Q.data_ptr(), q, Qo.data_ptr(), qo, _addr(K), k, _addr(Ko), ko, s))

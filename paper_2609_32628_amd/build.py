@@ -12,7 +12,7 @@ HERE = os.path.dirname(os.path.abspath(__file__))
 CSRC = os.path.join(HERE, "csrc")
 OUT = os.path.join(HERE, "libda2.so")
 BUILD = os.path.join(HERE, "_build")
-SOURCES = ["host.cpp", "draft.hip", "rank.hip", "prep.hip", "attn.hip", "host_token.cpp", "norm.hip"]
+SOURCES = ["host.cpp", "draft.hip", "rank.hip", "prep.hip", "attn.hip", "host_token.cpp", "norm.hip", "rope.hip"]
 HIPCC = os.environ.get("HIPCC", "/opt/rocm/bin/hipcc")
 FLAGS = [
     "--offload-arch=gfx950", "-O3", "-fPIC", "-std=c++20",

@@ -92,6 +92,20 @@ da2::NormArgs norm_args(const Ext& e, const da2_norm_desc* n, int32_t dtype) {
   return a;
 }
 
+// ---- rotary positions ----------------------------------------------------------------
+// Rotated channels of a block, or -1 for a descriptor that is not one.
+int64_t rope_rot(const da2_rope_desc* r) {
+  if (!r || (r->layout != DA2_ROPE_INTERLEAVED && r->layout != DA2_ROPE_HALF)) return -1;
+  if (r->axes < 1 || r->axes > 3 || r->block < 2) return -1;
+  int64_t rot = 0;
+  for (int i = 0; i < 3; ++i) {
+    const int32_t D = r->rot_axis[i];
+    if (i < r->axes ? (D < 2 || D % 2) : D != 0) return -1;
+    rot += D;
+  }
+  return rot <= r->block && r->block <= 65536 ? rot : -1;
+}
+
 }  // namespace
 
 extern "C" {
@@ -151,6 +165,101 @@ int32_t da2_norm_bwd(const void* dY, const da2_tensor* dy, const void* X, const 
   a.db = db;
   a.ws = static_cast<float*>(ws);
   return hip_status(da2::launch_norm_bwd(a, static_cast<hipStream_t>(stream)));
+}
+
+int32_t da2_rope_plan(const da2_rope_desc* r, const da2_rope_freq* f, double* turns, double* scale) {
+  if (rope_rot(r) < 0 || !f || !turns || !scale) return DA2_ERR_INVALID_ARG;
+  if (f->scaling < DA2_ROPE_PLAIN || f->scaling > DA2_ROPE_YARN) return DA2_ERR_INVALID_ARG;
+  if (!(f->base > 1.0) || !(f->factor >= 1.0) || !std::isfinite(f->base) || !std::isfinite(f->factor))
+    return DA2_ERR_INVALID_ARG;
+  if (f->scaling == DA2_ROPE_PLAIN && f->factor != 1.0) return DA2_ERR_INVALID_ARG;
+  const bool yarn = f->scaling == DA2_ROPE_YARN;
+  if (yarn && (f->orig_len < 1 || !(f->beta_slow > 0.0) || !(f->beta_fast >= f->beta_slow) ||
+               !std::isfinite(f->beta_fast)))
+    return DA2_ERR_INVALID_ARG;
+  constexpr double kTwoPi = 6.283185307179586476925286766559;
+  int64_t p = 0;
+  for (int ax = 0; ax < r->axes; ++ax) {
+    const double D = r->rot_axis[ax];
+    const double base =
+        f->scaling == DA2_ROPE_NTK && D > 2 ? f->base * std::pow(f->factor, D / (D - 2)) : f->base;
+    // the pair that turns n times over orig_len positions: base^(-2i/D) orig_len / (2 pi) = n
+    const auto pair_of = [&](double n) { return D * std::log(f->orig_len / (n * kTwoPi)) / (2 * std::log(f->base)); };
+    double lo = 0, hi = 0;
+    if (yarn) {
+      lo = std::max(std::floor(pair_of(f->beta_fast)), 0.0);
+      hi = std::min(std::ceil(pair_of(f->beta_slow)), D - 1);
+    }
+    for (int i = 0; i < r->rot_axis[ax] / 2; ++i) {
+      double w = std::pow(base, -2.0 * i / D);
+      if (f->scaling == DA2_ROPE_LINEAR) w /= f->factor;
+      if (yarn) {
+        const double ramp = std::min(std::max((i - lo) / std::max(hi - lo, 0.001), 0.0), 1.0);
+        w = w / f->factor * ramp + w * (1.0 - ramp);
+      }
+      turns[p++] = w / kTwoPi;
+    }
+  }
+  *scale = yarn ? 0.1 * std::log(f->factor) + 1.0 : 1.0;
+  return DA2_OK;
+}
+
+int32_t da2_rope(const da2_rope_desc* r, const double* turns, double scale, const int32_t* pos, int64_t pos_stride_b,
+                 const da2_rope_rows* s, const void* Q, const da2_tensor* q, void* Qo, const da2_tensor* qo,
+                 const void* K, const da2_tensor* k, void* Ko, const da2_tensor* ko, void* stream) {
+  const int64_t rot = rope_rot(r);
+  if (rot < 0 || !s || !turns || !std::isfinite(scale)) return DA2_ERR_INVALID_ARG;
+  if (s->d < 1 || s->d > 65536 || s->d % r->block || s->Hk < 0 || (s->inverse != 0 && s->inverse != 1))
+    return DA2_ERR_INVALID_ARG;
+  const Ext eq{s->B, s->Hq, s->N, s->d}, ek{s->B, s->Hk, s->N, s->d};
+  int32_t st = check_ext(eq);
+  if (st || (s->Hk && (st = check_ext(ek)))) return st;
+  if ((int64_t)s->Hq + s->Hk > 65535) return DA2_ERR_INVALID_ARG;
+  // one thread per unit of a token: the grid ends at 2^32 threads
+  if ((int64_t)s->B * s->N * r->block > (1ll << 32) - 256) return DA2_ERR_INVALID_ARG;
+  if (pos) {
+    if (s->grid_h || s->grid_w || (pos_stride_b != 0 && pos_stride_b < (int64_t)s->N * r->axes))
+      return DA2_ERR_INVALID_ARG;
+    if (pos_stride_b > (1ll << 40)) return DA2_ERR_INVALID_ARG;
+  } else if (r->axes > 1 && (s->grid_w < 1 || (r->axes > 2 && s->grid_h < 1))) {
+    return DA2_ERR_INVALID_ARG;
+  }
+  if (!q || check_view(q, eq, q->dtype, false) || check_view(qo, eq, q->dtype, true)) return DA2_ERR_INVALID_ARG;
+  if (!Q || !Qo || (Q == Qo && !same_strides(q, qo, eq))) return DA2_ERR_INVALID_ARG;
+  if (s->Hk) {
+    if (check_view(k, ek, q->dtype, false) || check_view(ko, ek, q->dtype, true)) return DA2_ERR_INVALID_ARG;
+    if (!K || !Ko || (K == Ko && !same_strides(k, ko, ek))) return DA2_ERR_INVALID_ARG;
+  }
+  if ((st = check_device())) return st;
+  da2::RopeArgs a{};
+  a.q = view(Q, q);
+  a.qo = out_view(Qo, qo);
+  a.q_in_place = Q == Qo;
+  if (s->Hk) {
+    a.k = view(K, k);
+    a.ko = out_view(Ko, ko);
+    a.k_in_place = K == Ko;
+  }
+  a.turns = turns;
+  a.pos = pos;
+  a.pos_sb = pos_stride_b;
+  a.B = s->B;
+  a.Hq = s->Hq;
+  a.Hk = s->Hk;
+  a.N = s->N;
+  a.d = s->d;
+  a.block = r->block;
+  a.rot = (int)rot;
+  a.axes = r->axes;
+  a.pair0 = r->rot_axis[0] / 2;
+  a.pair1 = a.pair0 + r->rot_axis[1] / 2;
+  a.grid_h = s->grid_h;
+  a.grid_w = s->grid_w;
+  a.layout = r->layout;
+  a.dtype = q->dtype;
+  a.scale = (float)scale;
+  a.sign = s->inverse ? -1.0f : 1.0f;
+  return hip_status(da2::launch_rope(a, static_cast<hipStream_t>(stream)));
 }
 
 }  // extern "C"

@@ -100,4 +100,20 @@ int64_t norm_parts(int64_t rows, int64_t groups, int C, int dtype);
 hipError_t launch_norm(const NormArgs& a, hipStream_t stream);
 hipError_t launch_norm_bwd(const NormArgs& a, hipStream_t stream);
 
+// ---- rotary positions (rope.hip) ---------------------------------------------------
+struct RopeArgs {
+  View q, k;
+  OutView qo, ko;
+  const double* turns;
+  const int32_t* pos;
+  int64_t pos_sb;
+  int B, Hq, Hk, N, d, block, rot;
+  int axes, pair0, pair1;  // pairs of axis 0, and of axes 0 and 1 together
+  int grid_h, grid_w;
+  int layout, dtype;
+  float scale, sign;       // sign of the sine: -1 turns back
+  bool q_in_place, k_in_place;
+};
+hipError_t launch_rope(const RopeArgs& a, hipStream_t stream);
+
 }  // namespace da2
