@@ -353,8 +353,8 @@ int32_t da2_mixed_attn(const void* ops, int64_t ops_bytes, const void* lists, co
  *
  * These calls take no da2_problem: they work on [B, H, N, C] token rows in any
  * memory order with C contiguous (da2_tensor; hidden rows are H = 1), of type
- * bf16, fp16 or fp32 as each call says. Unlike the calls above they place no
- * condition on alignment beyond the element's own. For every one of them:
+ * bf16, fp16 or fp32 as each call says. The norms and rotary positions place
+ * no condition on alignment beyond the element's own. For every one of them:
  *   - strides are >= 0 and at most 2^40 elements; the stride of an extent of 1
  *     is not looked at. An output's rows must not overlap one another; an input
  *     may repeat rows (stride 0).
@@ -474,6 +474,61 @@ int32_t da2_rope(const da2_rope_desc* r, const double* turns, double scale, cons
                  int64_t pos_stride_b, const da2_rope_rows* s, const void* Q, const da2_tensor* q,
                  void* Qo, const da2_tensor* qo, const void* K, const da2_tensor* k, void* Ko,
                  const da2_tensor* ko, void* stream);
+
+/* Differential attention. A head of d channels holds two query and key vectors
+ * of d/2 (its halves) that share the head's values:
+ *   O = (softmax(scale Q1 K1^T) - lambda_h softmax(scale Q2 K2^T)) V.
+ * Hq query heads share Hk key and value heads (Hq a multiple of Hk: query head h
+ * reads key head h / (Hq/Hk)), N queries see M keys. */
+typedef struct {
+  int32_t B, Hq, Hk, N, M, d; /* d = 64 or 128, else DA2_ERR_UNSUPPORTED */
+  int32_t causal;             /* 0 or 1, see q_start */
+  int32_t reserved;
+  double scale;               /* 2^-64 .. 2^64; 1 / sqrt(d/2) is usual */
+} da2_diff_problem;
+
+/* Host only: workspace bytes of da2_diff_attn (and with train = 1 of
+ * da2_diff_attn_bwd too). */
+int32_t da2_diff_ws_bytes(const da2_diff_problem* p, int32_t train, int64_t* bytes);
+
+/* Forward pass. Tensors are bf16 or fp16, all of one dtype, with 16-byte
+ * aligned bases and every stride a multiple of 8 elements; the stride_n of K
+ * and V (and of Q, dO) is at most 2^24.
+ *   Q       device [B,Hq,N,d]; K, V device [B,Hk,M,d]
+ *   lambda  device float32 [Hq]
+ *   kv_lens device int32 [B] or NULL: sample b has its first kv_lens[b] keys
+ *           (values outside [0, M] are clamped); what K and V hold beyond them
+ *           is not used. NULL: M.
+ *   q_start device int32 [B] or NULL: with causal = 1, query n of sample b sees
+ *           key j when j <= q_start[b] + n (any value: a query may see no key).
+ *           NULL: the queries are the last ones, q_start = kv_lens[b] - N.
+ *   O       device out [B,Hq,N,d]; rows that see no key are zero
+ *   lse     device out float32 [B,Hq,2,N] or NULL: log of each map's sum of
+ *           exponentials (-inf for a row that sees no key), which the backward
+ *           pass reads
+ *   ws      device scratch of da2_diff_ws_bytes(p, 0); may be NULL when that is 0
+ * Scores, softmax statistics and sums are float32; the weights are rounded to
+ * the tensors' type for the product with V. Keys that a query's mask hides must
+ * be finite where another query of the call sees them.
+ * Errors: INVALID_ARG, UNSUPPORTED (d, float32), WORKSPACE. */
+int32_t da2_diff_attn(const da2_diff_problem* p, const void* Q, const da2_tensor* q, const void* K,
+                      const da2_tensor* k, const void* V, const da2_tensor* v, const float* lambda,
+                      const int32_t* kv_lens, const int32_t* q_start, void* O, const da2_tensor* o,
+                      float* lse, void* ws, int64_t ws_bytes, void* stream);
+
+/* Gradients of da2_diff_attn, from its inputs and what it wrote to lse. Rows
+ * that see no key give nothing; keys beyond kv_lens get zeros.
+ *   dO      device [B,Hq,N,d]; dQ device out like Q; dK, dV device out like K
+ *           and V (summed over the query heads that share them)
+ *   dlambda device out float32 [Hq]
+ *   ws      device scratch of da2_diff_ws_bytes(p, 1) */
+int32_t da2_diff_attn_bwd(const da2_diff_problem* p, const void* Q, const da2_tensor* q,
+                          const void* K, const da2_tensor* k, const void* V, const da2_tensor* v,
+                          const float* lambda, const int32_t* kv_lens, const int32_t* q_start,
+                          const float* lse, const void* dO, const da2_tensor* d_o, void* dQ,
+                          const da2_tensor* dq, void* dK, const da2_tensor* dk, void* dV,
+                          const da2_tensor* dv, float* dlambda, void* ws, int64_t ws_bytes,
+                          void* stream);
 
 #ifdef __cplusplus
 }

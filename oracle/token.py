@@ -112,12 +112,12 @@ def _clean(x, see_any):
 
 
 def diff_attn(Q, K, V, lam, n_keys, start, causal, scale=None, dO=None):
-    """Dict of O, O2, lse and, with dO, of dQ, dK, dV and dlam. n_keys and start: one per sample."""
+    """Dict of O, lse and, with dO, of dQ, dK, dV and dlam. n_keys and start: one per sample."""
     B, H, N, d = Q.shape
     Hk, M = K.shape[1], K.shape[2]
     scale = 1.0 / math.sqrt(d // 2) if scale is None else scale
     h = d // 2
-    out = {"O": np.zeros((B, H, N, d)), "O2": np.zeros((B, H, N, d)), "lse": np.zeros((B, H, 2, N))}
+    out = {"O": np.zeros((B, H, N, d)), "lse": np.zeros((B, H, 2, N))}
     if dO is not None:
         out.update(dQ=np.zeros((B, H, N, d)), dK=np.zeros((B, Hk, M, d)), dV=np.zeros((B, Hk, M, d)), dlam=np.zeros(H))
     for b in range(B):
@@ -127,8 +127,7 @@ def diff_attn(Q, K, V, lam, n_keys, start, causal, scale=None, dO=None):
             q = Q[b, hq].astype(np.float64)
             k, v = (_clean(x[b, kh], np.arange(M) < n_keys[b]) for x in (K, V))
             P, out["lse"][b, hq] = _maps(q, k, see, scale)
-            out["O2"][b, hq] = P[1] @ v
-            out["O"][b, hq] = P[0] @ v - lam[hq] * out["O2"][b, hq]
+            out["O"][b, hq] = (P[0] - lam[hq] * P[1]) @ v
             if dO is None:
                 continue
             g = dO[b, hq].astype(np.float64)

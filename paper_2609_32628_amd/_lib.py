@@ -25,7 +25,8 @@ TAG_MARKER = 0xDA200000   # encoding tag in word 3 of each head's g entry
 # Every symbol include/da2.h declares.
 EXPORTS = ("da2_status_string", "da2_sizes", "da2_ops_layout_version", "da2_layout_build", "da2_draft_map", "da2_ws_draft_offsets",
            "da2_rank_assign", "da2_rank_assign_noalloc", "da2_lists_offsets", "da2_prep_operands", "da2_ops_offsets", "da2_mixed_attn",
-           "da2_norm", "da2_norm_ws_bytes", "da2_norm_bwd", "da2_rope_plan", "da2_rope")
+           "da2_norm", "da2_norm_ws_bytes", "da2_norm_bwd", "da2_rope_plan", "da2_rope",
+           "da2_diff_ws_bytes", "da2_diff_attn", "da2_diff_attn_bwd")
 
 
 class Problem(ctypes.Structure):
@@ -72,6 +73,12 @@ class RopeRows(ctypes.Structure):
                 ("inverse", ctypes.c_int32)]
 
 
+class DiffProblem(ctypes.Structure):
+    _fields_ = [("B", ctypes.c_int32), ("Hq", ctypes.c_int32), ("Hk", ctypes.c_int32), ("N", ctypes.c_int32),
+                ("M", ctypes.c_int32), ("d", ctypes.c_int32), ("causal", ctypes.c_int32), ("reserved", ctypes.c_int32),
+                ("scale", ctypes.c_double)]
+
+
 class Da2Error(RuntimeError):
     def __init__(self, call, status, lib):
         msg = lib.da2_status_string(status).decode()
@@ -93,6 +100,7 @@ def lib():
         P, T, S = ctypes.POINTER(Problem), ctypes.POINTER(Tensor), ctypes.POINTER(Sizes)
         R, ND = ctypes.POINTER(Rows), ctypes.POINTER(NormDesc)
         RD, RF, RR = ctypes.POINTER(RopeDesc), ctypes.POINTER(RopeFreq), ctypes.POINTER(RopeRows)
+        DP = ctypes.POINTER(DiffProblem)
         pdbl = ctypes.POINTER(ctypes.c_double)
         pi64, pi32 = ctypes.POINTER(ctypes.c_int64), ctypes.POINTER(ctypes.c_int32)
         sig = {
@@ -113,6 +121,10 @@ def lib():
             "da2_norm_bwd": (i32, [vp, T, vp, T, R, ND, vp, vp, vp, T, vp, vp, vp, i64, vp]),
             "da2_rope_plan": (i32, [RD, RF, pdbl, pdbl]),
             "da2_rope": (i32, [RD, vp, dbl, vp, i64, RR, vp, T, vp, T, vp, T, vp, T, vp]),
+            "da2_diff_ws_bytes": (i32, [DP, i32, pi64]),
+            "da2_diff_attn": (i32, [DP, vp, T, vp, T, vp, T, vp, vp, vp, vp, T, vp, vp, i64, vp]),
+            "da2_diff_attn_bwd": (i32, [DP, vp, T, vp, T, vp, T, vp, vp, vp, vp, vp, T, vp, T, vp, T, vp, T, vp, vp,
+                                        i64, vp]),
         }
         for name, (res, args) in sig.items():
             f = getattr(L, name)

@@ -20,7 +20,7 @@ import torch
 from . import _lib
 from ._lib import (DA2_BF16, DA2_FMT4_MXFP4, DA2_FMT4_NVFP4, DA2_FP16, DA2_FP32, DA2_NORM_LAYER, DA2_NORM_RMS,
                    DA2_PART_RAGGED, DA2_PART_TILES8, DA2_ROPE_HALF, DA2_ROPE_INTERLEAVED, DA2_ROPE_LINEAR,
-                   DA2_ROPE_NTK, DA2_ROPE_PLAIN, DA2_ROPE_YARN, DA2_SCOPE_HEAD, DA2_SCOPE_ROW, NormDesc, Problem,
+                   DA2_ROPE_NTK, DA2_ROPE_PLAIN, DA2_ROPE_YARN, DA2_SCOPE_HEAD, DA2_SCOPE_ROW, DiffProblem, NormDesc, Problem,
                    RopeDesc, RopeFreq, RopeRows, Rows, Tensor, check, lib)
 
 SCOPES = {"head": DA2_SCOPE_HEAD, "row": DA2_SCOPE_ROW}
@@ -334,3 +334,66 @@ def da2_rope(rope, Q, Qo, K=None, Ko=None, pos=None, grid=None, inverse=False, s
         check("da2_rope", lib().da2_rope(
             rope.desc(), t, rope.scale, _addr(pos), stride, RopeRows(B, Hq, Hk, N, d, gh, gw, int(inverse)),
             Q.data_ptr(), q, Qo.data_ptr(), qo, _addr(K), k, _addr(Ko), ko, s))
+
+
+def _diff_problem(Q, K, causal=False, scale=None):
+    if Q.dim() != 4 or K.dim() != 4:
+        raise ValueError("expected [B, H, N, d] tensors")
+    B, Hq, N, d = Q.shape
+    Hk, M = K.shape[1:3]
+    if K.shape[0] != B or K.shape[3] != d or Hk == 0 or Hq % Hk:
+        raise ValueError(f"Q {tuple(Q.shape)} and K {tuple(K.shape)} do not belong together")
+    return DiffProblem(B, Hq, Hk, N, M, d, int(causal), 0, (d / 2) ** -0.5 if scale is None else float(scale))
+
+
+def _bytes(ws):
+    return 0 if ws is None else ws.numel() * ws.element_size()
+
+
+def da2_diff_ws_bytes(Q, K, train=False):
+    """Workspace bytes of da2_diff_attn (train: and of da2_diff_attn_bwd) for tensors of these shapes."""
+    out = ctypes.c_int64()
+    check("da2_diff_ws_bytes", lib().da2_diff_ws_bytes(_diff_problem(Q, K), int(train), out))
+    return out.value
+
+
+def _diff_inputs(Q, K, V, lam, kv_lens, q_start, causal, scale):
+    """Problem, descriptors of Q, K, V and addresses of lam, kv_lens, q_start."""
+    q, k = _rows("Q", Q), _rows("K", K, dtype=Q.dtype)
+    p = _diff_problem(Q, K, causal, scale)
+    v = _rows("V", V, K.shape, Q.dtype)
+    if lam is None:
+        raise ValueError("lam: expected float32 weights of the query heads")
+    return p, q, k, v, (_plain("lam", lam, (p.Hq,), torch.float32), _plain("kv_lens", kv_lens, (p.B,), torch.int32),
+                        _plain("q_start", q_start, (p.B,), torch.int32))
+
+
+def da2_diff_attn(Q, K, V, lam, O, ws=None, lse=None, kv_lens=None, q_start=None, causal=False, scale=None, stream=None):
+    """O = (softmax(scale Q1 K1') - lam softmax(scale Q2 K2')) V, with Q1 and Q2 (K1, K2) the halves of a head's channels
+    and the heads of K and V shared by Hq / Hk heads of Q. lam: float32 [Hq]. kv_lens, q_start: int32 [B], the valid keys
+    of each sample and the position of its first query (default: all keys, and the queries are the last of them). lse
+    (float32 [B, Hq, 2, N]) is for da2_diff_attn_bwd. ws: da2_diff_ws_bytes(Q, K)."""
+    p, q, k, v, (l, kl, qs) = _diff_inputs(Q, K, V, lam, kv_lens, q_start, causal, scale)
+    o = _rows("O", O, Q.shape, Q.dtype)
+    ls = _plain("lse", lse, (p.B, p.Hq, 2, p.N), torch.float32)
+    s, dev = _on(stream, Q, K, V, lam, O, ws, lse, kv_lens, q_start)
+    with dev:
+        check("da2_diff_attn", lib().da2_diff_attn(
+            p, Q.data_ptr(), q, K.data_ptr(), k, V.data_ptr(), v, l, kl, qs, O.data_ptr(), o, ls, _addr(ws),
+            _bytes(ws), s))
+    return O
+
+
+def da2_diff_attn_bwd(Q, K, V, lam, lse, dO, dQ, dK, dV, dlam, ws, kv_lens=None, q_start=None, causal=False, scale=None,
+                      stream=None):
+    """Gradients of da2_diff_attn from its inputs and what it wrote to lse. ws: da2_diff_ws_bytes(Q, K, True)."""
+    p, q, k, v, (l, kl, qs) = _diff_inputs(Q, K, V, lam, kv_lens, q_start, causal, scale)
+    do, dq = (_rows(n, t, Q.shape, Q.dtype) for n, t in (("dO", dO), ("dQ", dQ)))
+    dk, dv = (_rows(n, t, K.shape, Q.dtype) for n, t in (("dK", dK), ("dV", dV)))
+    ls = _plain("lse", lse, (p.B, p.Hq, 2, p.N), torch.float32)
+    dl = _plain("dlam", dlam, (p.Hq,), torch.float32)
+    s, dev = _on(stream, Q, K, V, lam, lse, dO, dQ, dK, dV, dlam, ws, kv_lens, q_start)
+    with dev:
+        check("da2_diff_attn_bwd", lib().da2_diff_attn_bwd(
+            p, Q.data_ptr(), q, K.data_ptr(), k, V.data_ptr(), v, l, kl, qs, ls, dO.data_ptr(), do, dQ.data_ptr(), dq,
+            dK.data_ptr(), dk, dV.data_ptr(), dv, dl, _addr(ws), _bytes(ws), s))

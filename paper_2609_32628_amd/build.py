@@ -12,7 +12,8 @@ HERE = os.path.dirname(os.path.abspath(__file__))
 CSRC = os.path.join(HERE, "csrc")
 OUT = os.path.join(HERE, "libda2.so")
 BUILD = os.path.join(HERE, "_build")
-SOURCES = ["host.cpp", "draft.hip", "rank.hip", "prep.hip", "attn.hip", "host_token.cpp", "norm.hip", "rope.hip"]
+SOURCES = ["host.cpp", "draft.hip", "rank.hip", "prep.hip", "attn.hip", "host_token.cpp", "norm.hip", "rope.hip",
+           "diff_fwd.hip", "diff_bwd.hip"]
 HIPCC = os.environ.get("HIPCC", "/opt/rocm/bin/hipcc")
 FLAGS = [
     "--offload-arch=gfx950", "-O3", "-fPIC", "-std=c++20",
@@ -24,11 +25,12 @@ FLAGS = [
 ]
 
 
-# No maximum or minimum of the attention and draft kernels sees a NaN: operands
-# are finite and -inf marks masked logits and padding (16-bit padding logits of
+# No maximum or minimum of the attention and draft kernels sees a NaN of valid
+# operands: they are finite and -inf marks masked logits and padding (16-bit padding logits of
 # an infinite query, which are NaN, are replaced on their bits before the first
-# maximum), so none needs NaN canonicalization.
-EXTRA = {"attn.hip": ["-fno-honor-nans"], "draft.hip": ["-fno-honor-nans"]}
+# maximum), so none needs NaN canonicalization. In differential attention a NaN of
+# the caller's reaches its rows through the exponentials, whatever the maximum.
+EXTRA = {f: ["-fno-honor-nans"] for f in ("attn.hip", "draft.hip", "diff_fwd.hip", "diff_bwd.hip")}
 
 
 def _compile(src):

@@ -1,0 +1,357 @@
+// Differential attention, backward.
+//
+// With P1, P2 the softmax maps, dP = dO V^T and del_i the row sums of P_i dP:
+//   dS1 = P1 (dP - del1),  dS2 = -lambda P2 (dP - del2),
+//   dQ_i = c dS_i K_i,  dK_i = c dS_i^T Q_i,  dV = (P1 - lambda P2)^T dO,
+//   dlambda = -sum of del2.
+// The maps are computed again from the scores and the forward pass's log sums.
+//
+// del_i equals dO . (output of map i), but outputs stored in 16 bits are too
+// coarse for it: their rounding moves every dS_i of a row the same way, which
+// the mean of K does not cancel (2.5 times the error of the gradients' own
+// rounding, measured), and dlambda is a sum in which most of del2 cancels. So
+// the rows are walked twice: once for del_i, in float32 from unrounded weights,
+// then for dQ.
+//
+// Two kernels: dQ, where a wave keeps 32 queries and walks over the keys; dK and
+// dV, where a wave keeps 32 keys and walks over the queries. Each recomputes the
+// scores and dP, and neither adds into memory, so the results do not depend on
+// the order of workgroups and nothing has to be cleared. In multiply-adds of d
+// per pair: 2 for del, 3 for dQ, 4 for dK and dV, where one pass over both sides
+// (which would need sums in memory) takes 5 beside del.
+#include <type_traits>
+
+#include "diff.hpp"
+
+namespace da2 {
+
+namespace {
+
+using namespace diff;
+
+constexpr int kThreads = 256;
+
+// Statistics of the rows of a head, 64 at a time: minus the log sums of both maps in units of the raw scores (where the
+// sums of the scores start, so that their exponentials are the weights), minus del1 (where dP's sums start), and
+// del1 - del2. Rows from N on hold values that make every weight zero.
+constexpr int kStat = 4 * 64;  // floats of 64 rows: [4][64]
+constexpr int64_t padded(int64_t n) { return (n + 63) / 64 * 64; }
+__device__ inline float* stat_at(float* stat, int64_t bh, int64_t n, int N) {
+  return stat + (bh * (padded(N) / 64) + n / 64) * kStat + n % 64;
+}
+__device__ inline void put_stat(float* s, float l1, float l2, float d1, float d2) {
+  s[0] = -l1;
+  s[64] = -l2;
+  s[128] = -d1;
+  s[192] = d1 - d2;
+}
+constexpr float kNever = __builtin_inff();
+
+// 16 floats of LDS, the same for all lanes of a half.
+__device__ inline f32x16 read16(const float* p) {
+  f32x16 x;
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    const f32x4 v = *reinterpret_cast<const f32x4*>(p + 4 * i);
+#pragma unroll
+    for (int e = 0; e < 4; ++e) x[4 * i + e] = v[e];
+  }
+  return x;
+}
+
+// dK and dV of 128 keys: 4 waves with 32 keys each; 32 queries of one head at a time in LDS. A wave's keys are in
+// registers, its values in LDS: both in registers would leave one wave a SIMD at d = 128.
+template <typename T, int D>
+__global__ __launch_bounds__(kThreads, 2) void diff_dkv_kernel(DiffArgs a, float* stat, int tiles, int64_t units) {
+  constexpr int S = D / 32, Q = 32, BYTES = Q * Tile<D>::kRow, R = Tile<D>::kRowsPerCopy;
+  __shared__ __align__(256) char lds[2][2][BYTES];  // [buffer][Q, dO]
+  __shared__ __align__(256) char val[4 * BYTES];    // the workgroup's rows of V
+  __shared__ __align__(16) float st[2][4][Q];
+  const int64_t unit = unit_of(blockIdx.x, units);
+  if (unit < 0) return;
+  // the first keys are seen by most queries under a causal mask: they go first
+  const int tile = static_cast<int>(unit % tiles);
+  const int64_t bh = unit / tiles;
+  const int b = static_cast<int>(bh / a.Hk), hk = static_cast<int>(bh % a.Hk), G = a.Hq / a.Hk;
+  const int lane = threadIdx.x % 64, g = lane / 32, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64);
+  const Visible vis = visible(a, b);
+  const int key0 = tile * 128 + 32 * wave, key = key0 + lane % 32;
+
+  f32x16 dv[S], dk[2][S / 2];
+#pragma unroll
+  for (int t = 0; t < S; ++t) dv[t] = dk[t / (S / 2)][t % (S / 2)] = f32x16{};
+
+  // queries that see the tile's first key
+  const int64_t first = a.causal ? tile * 128 - vis.start : 0;
+  const int n_first = static_cast<int>(first < 0 ? 0 : first < a.N ? first : a.N) / Q * Q;
+  const int n_tiles = tile * 128 < vis.len && first < a.N ? (a.N - n_first + Q - 1) / Q : 0;
+
+  if (n_tiles > 0) {
+    s16x8 kf[2][S];
+    {
+      const int64_t row = min(key, vis.len - 1);
+      const T* kp = static_cast<const T*>(a.k.p) + b * a.k.sb + hk * a.k.sh + row * a.k.sn + 8 * g;
+#pragma unroll
+      for (int c = 0; c < 2 * S; ++c) kf[c / S][c % S] = *reinterpret_cast<const s16x8*>(kp + 16 * c);
+    }
+    const T* vp = static_cast<const T*>(a.v.p) + b * a.v.sb + hk * a.v.sh + static_cast<int64_t>(tile) * 128 * a.v.sn;
+#pragma unroll
+    for (int i = 0; i < Q / R; ++i)  // each wave its own rows
+      copy_rows<D>(vp, 2 * a.v.sn, Q * wave + i * R, vis.len - 1 - tile * 128, lane, lds_offset(val) + wave * BYTES + i * 1024);
+    const uint32_t vt = lds_offset(val) + wave * BYTES;
+    const RowReader<D> rows(lane, true), keys(lane, false);
+    const ColReader<D> cols(lane);
+    const float c = a.scale * kLog2e;
+    const int total = G * n_tiles;
+    const auto copy = [&](int at, int buf) {
+      const int h = hk * G + at / n_tiles, n0 = n_first + at % n_tiles * Q;
+      const T* qp = static_cast<const T*>(a.q.p) + b * a.q.sb + h * a.q.sh + n0 * a.q.sn;
+      const T* op = static_cast<const T*>(a.dout.p) + b * a.dout.sb + h * a.dout.sh + n0 * a.dout.sn;
+      // 2 Q / R copies of 1 KB: each wave takes its share of Q's and of dO's rows
+#pragma unroll
+      for (int i = wave; i < Q / R; i += 4) {
+        copy_rows<D>(qp, 2 * a.q.sn, i * R, a.N - 1 - n0, lane, lds_offset(lds[buf][0]) + i * 1024);
+        copy_rows<D>(op, 2 * a.dout.sn, i * R, a.N - 1 - n0, lane, lds_offset(lds[buf][1]) + i * 1024);
+      }
+      if (wave == 0 && lane < Q)  // four times 32 floats
+        copy_1k(stat_at(stat, static_cast<int64_t>(b) * a.Hq + h, n0, a.N), (lane / 8) * 256 + (lane % 8) * 16,
+                __builtin_amdgcn_readfirstlane(lds_offset(st[buf])));
+    };
+    copy(0, 0);
+    for (int at = 0; at < total; ++at) {
+      const int buf = at % 2;
+      wait_copies();
+      barrier();  // every wave's copies have arrived, and the other buffer has been read
+      if (at + 1 < total) copy(at + 1, buf ^ 1);
+      const int n = n_first + at % n_tiles * Q;
+      // the wave's first key is seen by none of the 32 queries
+      if (a.causal && key0 > vis.start + n + 31) continue;
+      const float minus = -a.lam[hk * G + at / n_tiles];
+      const uint32_t qt = lds_offset(lds[buf][0]), ot = lds_offset(lds[buf][1]);
+      int hidden = 0;  // queries from here on see the key
+      if (a.causal && key0 + 31 > vis.start + n) {
+        const int64_t w = key - vis.start - n - 16 * g;
+        hidden = static_cast<int>(w < 0 ? 0 : w < 16 ? w : 16);
+      }
+      f32x16 dp = read16(&st[buf][2][16 * g]);  // dP - del1
+#pragma unroll
+      for (int s = 0; s < 2 * S; ++s) dp = mma<T>(rows.read(ot, 0, s), keys.read(vt, 0, s), dp);
+      s16x8 df[2][2];
+      float w[16];
+#pragma unroll
+      for (int i = 0; i < 2; ++i) {
+        f32x16 x = read16(&st[buf][i][16 * g]);
+#pragma unroll
+        for (int s = 0; s < S; ++s) x = mma<T>(rows.read(qt, 0, i * S + s), kf[i][s], x);
+        float d[16];
+        if (i) dp += read16(&st[buf][3][16 * g]);  // dP - del2
+#pragma unroll
+        for (int e = 0; e < 16; ++e) {
+          float p = exp2_fast(x[e] * c);
+          if (i) p *= minus;
+          p = e < hidden ? 0.0f : p;
+          w[e] = i ? w[e] + p : p;
+          d[e] = p * dp[e];
+        }
+        df[i][0] = pack8<T>(d);
+        df[i][1] = pack8<T>(d + 8);
+      }
+#pragma unroll
+      for (int s = 0; s < 2; ++s) {
+        const s16x8 wf = pack8<T>(w + 8 * s);
+#pragma unroll
+        for (int t = 0; t < S; ++t) {
+          dv[t] = mma<T>(wf, cols.read(ot, 0, t, s), dv[t]);
+          f32x16& k = dk[t / (S / 2)][t % (S / 2)];
+          k = mma<T>(df[t / (S / 2)][s], cols.read(qt, 0, t, s), k);
+        }
+      }
+    }
+  }
+  // accumulator register e: key 8 (e/4) + 4 g + e%4, lane%32: channel
+#pragma unroll
+  for (int e = 0; e < 16; ++e) {
+    const int kk = key0 + 8 * (e / 4) + 4 * g + e % 4;
+    if (kk >= a.M) continue;
+    const bool valid = kk < vis.len;
+    T* kp = static_cast<T*>(a.dk.p) + b * a.dk.sb + hk * a.dk.sh + kk * a.dk.sn + lane % 32;
+    T* vp = static_cast<T*>(a.dv.p) + b * a.dv.sb + hk * a.dv.sh + kk * a.dv.sn + lane % 32;
+#pragma unroll
+    for (int t = 0; t < S; ++t) {
+      kp[32 * t] = static_cast<T>(valid ? dk[t / (S / 2)][t % (S / 2)][e] * a.scale : 0.0f);
+      vp[32 * t] = static_cast<T>(valid ? dv[t][e] : 0.0f);
+    }
+  }
+}
+
+// del and dQ of 128 rows (a key head's query heads together, as in the forward pass): 4 waves with 32 rows each; 64 keys
+// at a time in LDS, twice over. The rows' statistics go to `stat`.
+template <typename T, int D>
+__global__ __launch_bounds__(kThreads, 2) void diff_dq_kernel(DiffArgs a, float* stat, int tiles, int64_t units) {
+  constexpr int S = D / 32, K = 64, BYTES = K * Tile<D>::kRow, R = Tile<D>::kRowsPerCopy;
+  __shared__ __align__(256) char lds[2][2][BYTES];  // [buffer][K, V]
+  const int64_t unit = unit_of(blockIdx.x, units);
+  if (unit < 0) return;
+  const int tile = tiles - 1 - static_cast<int>(unit % tiles);
+  const int64_t bh = unit / tiles;
+  const int b = static_cast<int>(bh / a.Hk), hk = static_cast<int>(bh % a.Hk), G = a.Hq / a.Hk;
+  const int lane = threadIdx.x % 64, g = lane / 32, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64);
+  const int64_t rows_all = static_cast<int64_t>(a.N) * G, row0 = static_cast<int64_t>(tile) * 128 + 32 * wave;
+  const auto token = [&](int64_t r) { return static_cast<int>((r < rows_all ? r : rows_all - 1) / G); };
+  const int64_t row = row0 + lane % 32;
+  const bool live = row < rows_all;
+  const int n = token(row), h = hk * G + static_cast<int>((live ? row : rows_all - 1) % G);
+  const Visible vis = visible(a, b);
+  const int limit = key_limit(a, vis, n);
+  const int low = key_limit(a, vis, token(row0)), high = key_limit(a, vis, token(row0 + 31));
+  const int end = key_limit(a, vis, token(static_cast<int64_t>(tile) * 128 + 127));
+
+  s16x8 qf[2][S], of[2 * S];
+  {
+    const T* qp = static_cast<const T*>(a.q.p) + b * a.q.sb + h * a.q.sh + n * a.q.sn + 8 * g;
+    const T* op = static_cast<const T*>(a.dout.p) + b * a.dout.sb + h * a.dout.sh + n * a.dout.sn + 8 * g;
+#pragma unroll
+    for (int s = 0; s < 2 * S; ++s) {
+      qf[s / S][s % S] = *reinterpret_cast<const s16x8*>(qp + 16 * s);
+      of[s] = *reinterpret_cast<const s16x8*>(op + 16 * s);
+    }
+  }
+  const int64_t bhn = static_cast<int64_t>(b) * a.Hq + h;
+  float lse[2], d[2] = {0.0f, 0.0f};
+#pragma unroll
+  for (int i = 0; i < 2; ++i) {
+    const float l = a.rlse[(bhn * 2 + i) * a.N + n];
+    lse[i] = l == -__builtin_inff() ? kNever : l / a.scale;
+  }
+  f32x16 dq[2][S / 2];
+#pragma unroll
+  for (int t = 0; t < S; ++t) dq[t / (S / 2)][t % (S / 2)] = f32x16{};
+  const RowReader<D> rows(lane, true);
+  const ColReader<D> cols(lane);
+  const T* kp = static_cast<const T*>(a.k.p) + b * a.k.sb + hk * a.k.sh;
+  const T* vp = static_cast<const T*>(a.v.p) + b * a.v.sb + hk * a.v.sh;
+  const float c = a.scale * kLog2e;
+  const auto copy = [&](int at, int buf) {
+#pragma unroll
+    for (int i = 0; i < K / R / 4; ++i) {
+      const int r0 = (wave * (K / R / 4) + i) * R;
+      copy_rows<D>(kp + at * a.k.sn, 2 * a.k.sn, r0, vis.len - 1 - at, lane, lds_offset(lds[buf][0]) + r0 * Tile<D>::kRow);
+      copy_rows<D>(vp + at * a.v.sn, 2 * a.v.sn, r0, vis.len - 1 - at, lane, lds_offset(lds[buf][1]) + r0 * Tile<D>::kRow);
+    }
+  };
+  // P_i dP (pass 0, summed) or dS_i (pass 1) of 32 keys at rows 32 j of the tiles
+  const auto walk = [&](auto pass) {
+    constexpr bool kSums = decltype(pass)::value == 0;
+    if (end > 0) copy(0, 0);
+    for (int key = 0, buf = 0; key < end; key += K, buf ^= 1) {
+      wait_copies();
+      barrier();
+      if (key + K < end) copy(key + K, buf ^ 1);
+      const uint32_t kt = lds_offset(lds[buf][0]), vt = lds_offset(lds[buf][1]);
+#pragma unroll 1
+      for (int j = 0; j < 2; ++j) {
+        const int at = key + 32 * j;
+        if (at >= high) continue;
+        f32x16 dp{};
+#pragma unroll
+        for (int s = 0; s < 2 * S; ++s) dp = mma<T>(rows.read(vt, j, s), of[s], dp);
+        s16x8 df[2][2];
+        const int left = at + 32 > low ? limit - at - 16 * g : 16;
+#pragma unroll
+        for (int i = 0; i < 2; ++i) {
+          f32x16 x{};
+#pragma unroll
+          for (int s = 0; s < S; ++s) x = mma<T>(rows.read(kt, j, i * S + s), qf[i][s], x);
+          const float l = lse[i] * c;
+          float ds[16];
+#pragma unroll
+          for (int e = 0; e < 16; ++e) {
+            float p = exp2_fast(__builtin_fmaf(x[e], c, -l));
+            p = e < left ? p : 0.0f;
+            if constexpr (kSums) {
+              d[i] = __builtin_fmaf(p, dp[e], d[i]);
+            } else {
+              ds[e] = p * (dp[e] - d[i]);
+            }
+          }
+          if constexpr (!kSums) {
+            df[i][0] = pack8<T>(ds);
+            df[i][1] = pack8<T>(ds + 8);
+          }
+        }
+        if constexpr (!kSums) {
+#pragma unroll
+          for (int t = 0; t < S; ++t)
+#pragma unroll
+            for (int s = 0; s < 2; ++s) {
+              f32x16& q = dq[t / (S / 2)][t % (S / 2)];
+              q = mma<T>(cols.read(kt, j, t, s), df[t / (S / 2)][s], q);
+            }
+        }
+      }
+    }
+  };
+  walk(std::integral_constant<int, 0>{});
+#pragma unroll
+  for (int i = 0; i < 2; ++i) d[i] = sum_halves(d[i]);
+  if (live && lane < 32) put_stat(stat_at(stat, bhn, n, a.N), lse[0], lse[1], d[0], d[1]);
+  if (tile == tiles - 1)  // rows behind the last token
+    for (int x = threadIdx.x; x < G * static_cast<int>(padded(a.N) - a.N); x += kThreads)
+      put_stat(stat_at(stat, static_cast<int64_t>(b) * a.Hq + hk * G + x % G, a.N + x / G, a.N), kNever, kNever, 0.0f, 0.0f);
+  wait_copies();
+  barrier();  // the tiles have been read
+  walk(std::integral_constant<int, 1>{});
+  const float f[2] = {a.scale, -a.lam[h] * a.scale};
+  T* out = static_cast<T*>(a.dq.p) + b * a.dq.sb + h * a.dq.sh + n * a.dq.sn;
+#pragma unroll
+  for (int t = 0; t < S; ++t) {
+    float x[16];
+#pragma unroll
+    for (int e = 0; e < 16; ++e) x[e] = dq[t / (S / 2)][t % (S / 2)][e] * f[t / (S / 2)];
+    store_columns(out + 32 * t, x, live);
+  }
+}
+
+// dlambda of a head: minus the sum of its rows' del2, in float64 and in a fixed order.
+__global__ __launch_bounds__(kThreads) void diff_dlam_kernel(DiffArgs a, float* stat) {
+  __shared__ double sums[kThreads];
+  const int h = blockIdx.x;
+  double t = 0.0;
+  for (int b = 0; b < a.B; ++b) {
+    for (int n = threadIdx.x; n < a.N; n += kThreads) {
+      const float* s = stat_at(stat, static_cast<int64_t>(b) * a.Hq + h, n, a.N);
+      t += -static_cast<double>(s[128]) - s[192];
+    }
+  }
+  sums[threadIdx.x] = t;
+  __syncthreads();
+  for (int o = kThreads / 2; o > 0; o >>= 1) {
+    if (threadIdx.x < o) sums[threadIdx.x] += sums[threadIdx.x + o];
+    __syncthreads();
+  }
+  if (threadIdx.x == 0) a.dlam[h] = static_cast<float>(-sums[0]);
+}
+
+template <typename T, int D>
+hipError_t launch(const DiffArgs& a, hipStream_t stream) {
+  float* stat = a.ws;
+  const int row_tiles = static_cast<int>((static_cast<int64_t>(a.N) * (a.Hq / a.Hk) + 127) / 128);
+  const int64_t row_units = static_cast<int64_t>(a.B) * a.Hk * row_tiles;
+  diff_dq_kernel<T, D><<<grid_of(row_units), kThreads, 0, stream>>>(a, stat, row_tiles, row_units);
+  const int key_tiles = static_cast<int>((a.M + 127ll) / 128);
+  const int64_t key_units = static_cast<int64_t>(a.B) * a.Hk * key_tiles;
+  diff_dkv_kernel<T, D><<<grid_of(key_units), kThreads, 0, stream>>>(a, stat, key_tiles, key_units);
+  diff_dlam_kernel<<<a.Hq, kThreads, 0, stream>>>(a, stat);
+  return hipGetLastError();
+}
+
+}  // namespace
+
+int64_t diff_bwd_ws_bytes(int B, int Hq, int N) { return static_cast<int64_t>(B) * Hq * padded(N) * 16; }
+
+hipError_t launch_diff_bwd(const DiffArgs& a, hipStream_t stream) {
+  if (a.dtype == DA2_BF16) return a.d == 128 ? launch<bf16_t, 128>(a, stream) : launch<bf16_t, 64>(a, stream);
+  return a.d == 128 ? launch<fp16_t, 128>(a, stream) : launch<fp16_t, 64>(a, stream);
+}
+
+}  // namespace da2

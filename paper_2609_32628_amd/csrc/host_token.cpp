@@ -106,6 +106,66 @@ int64_t rope_rot(const da2_rope_desc* r) {
   return rot <= r->block && r->block <= 65536 ? rot : -1;
 }
 
+// ---- differential attention --------------------------------------------------------------
+struct DiffExt {
+  Ext q, k;
+};
+
+int32_t check_diff(const da2_diff_problem* p, DiffExt* e) {
+  if (!p) return DA2_ERR_INVALID_ARG;
+  *e = DiffExt{Ext{p->B, p->Hq, p->N, p->d}, Ext{p->B, p->Hk, p->M, p->d}};
+  int32_t st = check_ext(e->q);
+  if (st || (st = check_ext(e->k))) return st;
+  if (p->Hq % p->Hk || (p->causal != 0 && p->causal != 1)) return DA2_ERR_INVALID_ARG;
+  if (!(p->scale >= 0x1p-64 && p->scale <= 0x1p64)) return DA2_ERR_INVALID_ARG;
+  if (p->d != 64 && p->d != 128) return DA2_ERR_UNSUPPORTED;
+  // positions in 32 bits; the launch grids end at 2^32 threads
+  const int64_t rows = (int64_t)p->N * (p->Hq / p->Hk);
+  if (p->N > (1 << 30) || p->M > (1 << 30) || rows > (1ll << 31) - 1) return DA2_ERR_INVALID_ARG;
+  const int64_t heads = (int64_t)p->B * p->Hk, most = (1 << 24) - 8;
+  if (heads * ((rows + 31) / 32) > most || heads * (((int64_t)p->M + 127) / 128) > most) return DA2_ERR_INVALID_ARG;
+  if ((int64_t)p->B * p->Hq * (((int64_t)p->N + 63) / 64 * 64) * (p->d / 8) > (1ll << 32) - 256)
+    return DA2_ERR_INVALID_ARG;
+  return DA2_OK;
+}
+
+bool aligned16(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 15u) == 0; }
+
+// A tensor of the attention: 16-byte vectors, 64 rows within 32 bits of byte offset.
+int32_t check_attn(const void* p, const da2_tensor* t, const Ext& e, int32_t dtype, bool out) {
+  if (!p || !aligned16(p)) return DA2_ERR_INVALID_ARG;
+  const int32_t st = check_view(t, e, dtype, out);
+  if (st) return st;
+  if (dtype == DA2_FP32) return DA2_ERR_UNSUPPORTED;
+  if ((e.B > 1 && t->stride_b % 8) || (e.H > 1 && t->stride_h % 8) || (e.N > 1 && t->stride_n % 8))
+    return DA2_ERR_INVALID_ARG;
+  return e.N > 1 && t->stride_n > (1 << 24) ? DA2_ERR_INVALID_ARG : DA2_OK;
+}
+
+da2::DiffArgs diff_args(const da2_diff_problem* p, int32_t dtype) {
+  da2::DiffArgs a{};
+  a.B = p->B;
+  a.Hq = p->Hq;
+  a.Hk = p->Hk;
+  a.N = p->N;
+  a.M = p->M;
+  a.d = p->d;
+  a.causal = p->causal;
+  a.dtype = dtype;
+  a.scale = (float)p->scale;
+  return a;
+}
+
+int64_t diff_ws(const da2_diff_problem* p, bool train) {
+  const int64_t f = da2::diff_fwd_ws_bytes(p->B, p->Hq, p->Hk, p->N, p->M, p->d);
+  return train ? std::max(f, da2::diff_bwd_ws_bytes(p->B, p->Hq, p->N)) : f;
+}
+
+// A stride of an extent of 1 is never multiplied by more than zero, but 64-row copies form row * stride in 32 bits.
+View attn_view(const void* p, const da2_tensor* t, const Ext& e) {
+  return View{p, t->stride_b, t->stride_h, e.N > 1 ? t->stride_n : 0};
+}
+
 }  // namespace
 
 extern "C" {
@@ -260,6 +320,84 @@ int32_t da2_rope(const da2_rope_desc* r, const double* turns, double scale, cons
   a.scale = (float)scale;
   a.sign = s->inverse ? -1.0f : 1.0f;
   return hip_status(da2::launch_rope(a, static_cast<hipStream_t>(stream)));
+}
+
+int32_t da2_diff_ws_bytes(const da2_diff_problem* p, int32_t train, int64_t* bytes) {
+  DiffExt e;
+  const int32_t st = check_diff(p, &e);
+  if (st) return st;
+  if (!bytes || (train != 0 && train != 1)) return DA2_ERR_INVALID_ARG;
+  *bytes = diff_ws(p, train != 0);
+  return DA2_OK;
+}
+
+int32_t da2_diff_attn(const da2_diff_problem* p, const void* Q, const da2_tensor* q, const void* K,
+                      const da2_tensor* k, const void* V, const da2_tensor* v, const float* lambda,
+                      const int32_t* kv_lens, const int32_t* q_start, void* O, const da2_tensor* o, float* lse,
+                      void* ws, int64_t ws_bytes, void* stream) {
+  DiffExt e;
+  int32_t st = check_diff(p, &e);
+  if (st) return st;
+  if (!q) return DA2_ERR_INVALID_ARG;
+  const int32_t t = q->dtype;
+  if ((st = check_attn(Q, q, e.q, t, false)) || (st = check_attn(K, k, e.k, t, false)) ||
+      (st = check_attn(V, v, e.k, t, false)) || (st = check_attn(O, o, e.q, t, true)))
+    return st;
+  if (!lambda || O == Q || O == K || O == V) return DA2_ERR_INVALID_ARG;
+  const int64_t need = diff_ws(p, false);
+  if (need && (!ws || !aligned16(ws))) return DA2_ERR_INVALID_ARG;
+  if (ws_bytes < need) return DA2_ERR_WORKSPACE;
+  if ((st = check_device())) return st;
+  da2::DiffArgs a = diff_args(p, t);
+  a.q = attn_view(Q, q, e.q);
+  a.k = attn_view(K, k, e.k);
+  a.v = attn_view(V, v, e.k);
+  a.o = out_view(O, o);
+  a.lam = lambda;
+  a.kv_lens = kv_lens;
+  a.q_start = q_start;
+  a.lse = lse;
+  a.ws = static_cast<float*>(ws);
+  return hip_status(da2::launch_diff_fwd(a, static_cast<hipStream_t>(stream)));
+}
+
+int32_t da2_diff_attn_bwd(const da2_diff_problem* p, const void* Q, const da2_tensor* q, const void* K,
+                          const da2_tensor* k, const void* V, const da2_tensor* v, const float* lambda,
+                          const int32_t* kv_lens, const int32_t* q_start, const float* lse, const void* dO,
+                          const da2_tensor* d_o, void* dQ, const da2_tensor* dq, void* dK, const da2_tensor* dk,
+                          void* dV, const da2_tensor* dv, float* dlambda, void* ws, int64_t ws_bytes, void* stream) {
+  DiffExt e;
+  int32_t st = check_diff(p, &e);
+  if (st) return st;
+  if (!q) return DA2_ERR_INVALID_ARG;
+  const int32_t t = q->dtype;
+  if ((st = check_attn(Q, q, e.q, t, false)) || (st = check_attn(K, k, e.k, t, false)) ||
+      (st = check_attn(V, v, e.k, t, false)) || (st = check_attn(dO, d_o, e.q, t, false)) ||
+      (st = check_attn(dQ, dq, e.q, t, true)) || (st = check_attn(dK, dk, e.k, t, true)) ||
+      (st = check_attn(dV, dv, e.k, t, true)))
+    return st;
+  if (!lambda || !lse || !dlambda || !ws || !aligned16(ws)) return DA2_ERR_INVALID_ARG;
+  const void* in[] = {Q, K, V, dO, dQ, dK, dV};
+  for (int i = 4; i < 7; ++i)
+    for (int j = 0; j < i; ++j)
+      if (in[i] == in[j]) return DA2_ERR_INVALID_ARG;
+  if (ws_bytes < diff_ws(p, true)) return DA2_ERR_WORKSPACE;
+  if ((st = check_device())) return st;
+  da2::DiffArgs a = diff_args(p, t);
+  a.q = attn_view(Q, q, e.q);
+  a.k = attn_view(K, k, e.k);
+  a.v = attn_view(V, v, e.k);
+  a.dout = attn_view(dO, d_o, e.q);
+  a.dq = out_view(dQ, dq);
+  a.dk = out_view(dK, dk);
+  a.dv = out_view(dV, dv);
+  a.lam = lambda;
+  a.kv_lens = kv_lens;
+  a.q_start = q_start;
+  a.rlse = lse;
+  a.dlam = dlambda;
+  a.ws = static_cast<float*>(ws);
+  return hip_status(da2::launch_diff_bwd(a, static_cast<hipStream_t>(stream)));
 }
 
 }  // extern "C"

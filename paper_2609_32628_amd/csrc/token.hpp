@@ -116,4 +116,26 @@ struct RopeArgs {
 };
 hipError_t launch_rope(const RopeArgs& a, hipStream_t stream);
 
+// ---- differential attention (diff_fwd.hip, diff_bwd.hip) ------------------------------
+struct DiffArgs {
+  View q, k, v;
+  OutView o;
+  const float* lam;
+  const int32_t *kv_lens, *q_start;  // null: M keys; the queries are the last ones
+  float* lse;           // written by the forward pass, or null
+  float* ws;
+  int B, Hq, Hk, N, M, d;
+  int causal, dtype;
+  float scale;
+  // backward pass
+  View dout;
+  const float* rlse;
+  OutView dq, dk, dv;
+  float* dlam;
+};
+int64_t diff_fwd_ws_bytes(int B, int Hq, int Hk, int N, int M, int d);
+int64_t diff_bwd_ws_bytes(int B, int Hq, int N);
+hipError_t launch_diff_fwd(const DiffArgs& a, hipStream_t stream);
+hipError_t launch_diff_bwd(const DiffArgs& a, hipStream_t stream);
+
 }  // namespace da2

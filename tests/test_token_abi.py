@@ -176,3 +176,102 @@ def test_rope_binding_refusals():
                  lambda: api.da2_rope_plan(64, (), device="cpu")):
         with pytest.raises((ValueError, _lib.Da2Error)):
             call()
+
+
+DIFF = dict(B=2, Hq=4, Hk=2, N=5, M=7, d=64, causal=0, reserved=0, scale=0.1)
+
+
+def _diff_problem(**kw):
+    return _lib.DiffProblem(*dict(DIFF, **kw).values())
+
+
+BAD_DIFFS = [dict(B=0), dict(Hq=0), dict(Hk=0), dict(N=0), dict(M=-1), dict(d=0), dict(Hq=5), dict(Hk=3), dict(causal=2),
+             dict(scale=0.0), dict(scale=-1.0), dict(scale=float("nan")), dict(scale=float("inf")), dict(scale=2.0 ** 65),
+             dict(scale=2.0 ** -65), dict(B=65536), dict(N=(1 << 30) + 1), dict(M=(1 << 30) + 1), dict(B=60000, Hq=600, Hk=600)]
+
+
+def test_diff_problem_refusals():
+    L = _lib.lib()
+    b = ctypes.c_int64()
+    assert L.da2_diff_ws_bytes(_diff_problem(), 0, b) == 0 and b.value >= 0
+    assert L.da2_diff_ws_bytes(_diff_problem(), 1, b) == 0 and b.value >= 2 * 4 * 5 * 20
+    for bad in BAD_DIFFS:
+        assert L.da2_diff_ws_bytes(_diff_problem(**bad), 1, b) == E, bad
+    assert L.da2_diff_ws_bytes(_diff_problem(d=96), 0, b) == U
+    assert L.da2_diff_ws_bytes(_diff_problem(), 2, b) == E
+    assert L.da2_diff_ws_bytes(None, 0, b) == E and L.da2_diff_ws_bytes(_diff_problem(), 0, None) == E
+
+
+def _refusals(call, base, cases):
+    for status, change in cases:
+        a = list(base)
+        for i, v in change.items():
+            a[i] = v
+        assert call(*a) == status, change
+
+
+def test_diff_refusals():
+    L = _lib.lib()
+    q, k = _desc(2, 4, 5, 64), _desc(2, 2, 7, 64)
+    A = [FAKE * (i + 1) for i in range(8)]
+    #       0                1     2  3     4  5     6  7     8     9     10    11 12    13    14       15
+    base = [_diff_problem(), A[0], q, A[1], k, A[2], k, FAKE, None, None, A[3], q, None, FAKE, 1 << 30, None]
+    odd = _lib.Tensor(4 * 5 * 64, 5 * 64, 68, 0, 0)
+    wide = _lib.Tensor(4 * 5 << 25, 5 << 25, (1 << 24) + 8, 0, 0)
+    over = _lib.Tensor(4 * 5 * 64, 5 * 64, 56, 0, 0)
+    f32, f16 = _desc(2, 4, 5, 64, _lib.DA2_FP32), _desc(2, 4, 5, 64, _lib.DA2_FP16)
+    need = [(E, {i: None}) for i in (0, 1, 2, 3, 4, 5, 6, 7, 10, 11)]
+    _refusals(L.da2_diff_attn, base, need + [
+        (E, {1: FAKE + 2}), (E, {3: FAKE + 8}), (E, {10: 3 * FAKE + 2}), (E, {2: odd}), (E, {2: wide}), (E, {11: over}),
+        (U, {2: f32, 4: _desc(2, 2, 7, 64, 1), 6: _desc(2, 2, 7, 64, 1), 11: f32}), (E, {2: f16}), (E, {2: _desc(2, 4, 5, 64, 3)}),
+        (E, {10: A[0]}), (E, {10: A[1]}), (E, {10: A[2]}),
+        (U, {0: _diff_problem(d=32)})] + [(E, {0: _diff_problem(**bad)}) for bad in BAD_DIFFS])
+    # a problem whose keys are split: a workspace that is missing, too small or not aligned
+    p = _diff_problem(N=1, M=4000)
+    b = ctypes.c_int64()
+    assert L.da2_diff_ws_bytes(p, 0, b) == 0 and b.value > 0
+    split = dict(zip((0, 2, 4, 6, 11), (p, _desc(2, 4, 1, 64), _desc(2, 2, 4000, 64), _desc(2, 2, 4000, 64), _desc(2, 4, 1, 64))))
+    _refusals(L.da2_diff_attn, base, [(E, {**split, 13: None}), (E, {**split, 13: FAKE + 4}), (W, {**split, 14: b.value - 1})])
+
+
+def test_diff_bwd_refusals():
+    L = _lib.lib()
+    q, k = _desc(2, 4, 5, 64), _desc(2, 2, 7, 64)
+    A = [FAKE * (i + 1) for i in range(12)]
+    b = ctypes.c_int64()
+    assert L.da2_diff_ws_bytes(_diff_problem(), 1, b) == 0
+    #       0                1     2  3     4  5     6  7     8     9     10    11    12 13   14 15   16 17   18 19    20    21       22
+    base = [_diff_problem(), A[0], q, A[1], k, A[2], k, FAKE, None, None, FAKE, A[5], q, A[6], q, A[7], k, A[8], k, FAKE, FAKE, b.value, None]
+    over = _lib.Tensor(4 * 5 * 64, 5 * 64, 56, 0, 0)
+    cases = [(E, {i: None}) for i in (0, 1, 2, 3, 4, 5, 6, 7, 10, 11, 12, 13, 14, 15, 16, 17, 18, 19, 20)]
+    cases += [(W, {21: b.value - 1}), (E, {20: FAKE + 4}), (E, {13: A[0]}), (E, {15: A[2]}), (E, {17: A[7]}), (E, {13: A[5]}),
+              (E, {14: over}), (E, {11: A[5] + 2}), (E, {12: _desc(2, 4, 5, 64, 2)})]
+    cases += [(E, {0: _diff_problem(**bad)}) for bad in BAD_DIFFS]
+    _refusals(L.da2_diff_attn_bwd, base, cases)
+
+
+def test_diff_binding_refusals():
+    Q, K = torch.zeros(2, 4, 5, 64, dtype=torch.bfloat16), torch.zeros(2, 2, 7, 64, dtype=torch.bfloat16)
+    lam, O = torch.zeros(4), torch.zeros_like(Q)
+    ok = dict(kv_lens=torch.zeros(2, dtype=torch.int32), q_start=torch.zeros(2, dtype=torch.int32))
+    call = api.da2_diff_attn
+    for f in (lambda: call(Q, K, K, lam, O, **ok),                                         # not on a GPU
+              lambda: call(Q, K[:, :, :, :32], K, lam, O),
+              lambda: call(Q, K[:1], K, lam, O),
+              lambda: call(Q[:, :3], K, K, lam[:3], O[:, :3]),
+              lambda: call(Q, K, K[:, :1], lam, O),
+              lambda: call(Q, K.half(), K, lam, O),
+              lambda: call(Q, K, K, None, O),
+              lambda: call(Q, K, K, lam[:3], O),
+              lambda: call(Q, K, K, lam.double(), O),
+              lambda: call(Q, K, K, lam, O[:1]),
+              lambda: call(Q, K, K, lam, O.float()),
+              lambda: call(Q, K, K, lam, O, lse=torch.zeros(2, 4, 5, 2)),
+              lambda: call(Q, K, K, lam, O, kv_lens=torch.zeros(2)),
+              lambda: call(Q, K, K, lam, O, q_start=torch.zeros(3, dtype=torch.int32)),
+              lambda: call(Q[0], K, K, lam, O),
+              lambda: api.da2_diff_ws_bytes(Q[:, :, :, :32], K[:, :, :, :32]),
+              lambda: api.da2_diff_attn_bwd(Q, K, K, lam, torch.zeros(2, 4, 2, 5), O, O, K, K, lam, None),
+              lambda: api.da2_diff_attn_bwd(Q, K, K, lam, None, O, O, K, K[:, :1], lam, O)):
+        with pytest.raises((ValueError, _lib.Da2Error)):
+            f()
