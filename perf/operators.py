@@ -373,9 +373,9 @@ def _own_diff(s):
     if not train:
         api.da2_diff_attn(s["Q"], s["K"], s["V"], s["lam"], s["O"], s["ws"], **how)
         return {"O": s["O"]}
-    api.da2_diff_attn(s["Q"], s["K"], s["V"], s["lam"], s["O"], s["ws"], O2=s["O2"], lse=s["lse"], **how)
-    api.da2_diff_attn_bwd(s["Q"], s["K"], s["V"], s["lam"], s["O"], s["O2"], s["lse"], s["dO"], s["dQ"], s["dK"], s["dV"],
-                          s["dlam"], s["ws"], **how)
+    api.da2_diff_attn(s["Q"], s["K"], s["V"], s["lam"], s["O"], s["ws"], lse=s["lse"], **how)
+    api.da2_diff_attn_bwd(s["Q"], s["K"], s["V"], s["lam"], s["lse"], s["dO"], s["dQ"], s["dK"], s["dV"], s["dlam"],
+                          s["ws"], **how)
     return {n: s[n] for n in ("O", "lse", "dV", "dQ", "dK", "dlam")}
 
 
