@@ -31,21 +31,29 @@ using namespace diff;
 
 constexpr int kThreads = 256;
 
-// Statistics of the rows of a head, 64 at a time: minus the log sums of both maps in units of the raw scores (where the
-// sums of the scores start, so that their exponentials are the weights), minus del1 (where dP's sums start), and
-// del1 - del2. Rows from N on hold values that make every weight zero.
+// Statistics of the rows of a head, 64 at a time, as dK and dV take them:
+//   - minus the log sums of both maps in units of the raw scores, where the sums of the scores start, so that their
+//     exponentials are the weights (the second map's with |lambda| in its log sum);
+//   - minus del1, where dP's sums start; and del1 - del2 with lambda's sign turned, so that
+//     sgn dP' = (-sgn lambda) (dP - del1) + this is the second map's factor.
+// Rows from N on hold values that make every weight zero.
 constexpr int kStat = 4 * 64;  // floats of 64 rows: [4][64]
 constexpr int64_t padded(int64_t n) { return (n + 63) / 64 * 64; }
 __device__ inline float* stat_at(float* stat, int64_t bh, int64_t n, int N) {
   return stat + (bh * (padded(N) / 64) + n / 64) * kStat + n % 64;
 }
-__device__ inline void put_stat(float* s, float l1, float l2, float d1, float d2) {
+__device__ inline float minus_sign(float lambda) { return lambda < 0.0f ? 1.0f : -1.0f; }
+__device__ inline void put_stat(float* s, float l1, float l2, float d1, float d2, float lambda, float c) {
   s[0] = -l1;
-  s[64] = -l2;
+  s[64] = __builtin_amdgcn_logf(fabsf(lambda)) / c - l2;
   s[128] = -d1;
-  s[192] = d1 - d2;
+  s[192] = (d1 - d2) * minus_sign(lambda);
 }
 constexpr float kNever = __builtin_inff();
+
+// A value at a wave-uniform address that the kernel does not write, through the scalar cache: a vector load would wait
+// for the copies issued before it.
+__device__ inline float load_uniform(const float* p) { return *(const __attribute__((address_space(4))) float*)p; }
 
 // 16 floats of LDS, the same for all lanes of a half.
 __device__ inline f32x16 read16(const float* p) {
@@ -62,7 +70,7 @@ __device__ inline f32x16 read16(const float* p) {
 // dK and dV of 128 keys: 4 waves with 32 keys each; 32 queries of one head at a time in LDS. A wave's keys are in
 // registers, its values in LDS: both in registers would leave one wave a SIMD at d = 128.
 template <typename T, int D>
-__global__ __launch_bounds__(kThreads, 2) void diff_dkv_kernel(DiffArgs a, float* stat, int tiles, int64_t units) {
+__global__ __launch_bounds__(kThreads, 2) void diff_dkv_kernel(DiffArgs a, float* stat, float* sums, int tiles, int parts, int64_t units) {
   constexpr int S = D / 32, Q = 32, BYTES = Q * Tile<D>::kRow, R = Tile<D>::kRowsPerCopy;
   __shared__ __align__(256) char lds[2][2][BYTES];  // [buffer][Q, dO]
   __shared__ __align__(256) char val[4 * BYTES];    // the workgroup's rows of V
@@ -70,8 +78,8 @@ __global__ __launch_bounds__(kThreads, 2) void diff_dkv_kernel(DiffArgs a, float
   const int64_t unit = unit_of(blockIdx.x, units);
   if (unit < 0) return;
   // the first keys are seen by most queries under a causal mask: they go first
-  const int tile = static_cast<int>(unit % tiles);
-  const int64_t bh = unit / tiles;
+  const int part = static_cast<int>(unit % parts), tile = static_cast<int>(unit / parts % tiles);
+  const int64_t bh = unit / parts / tiles;
   const int b = static_cast<int>(bh / a.Hk), hk = static_cast<int>(bh % a.Hk), G = a.Hq / a.Hk;
   const int lane = threadIdx.x % 64, g = lane / 32, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64);
   const Visible vis = visible(a, b);
@@ -82,11 +90,14 @@ __global__ __launch_bounds__(kThreads, 2) void diff_dkv_kernel(DiffArgs a, float
   for (int t = 0; t < S; ++t) dv[t] = dk[t / (S / 2)][t % (S / 2)] = f32x16{};
 
   // queries that see the tile's first key
-  const int64_t first = a.causal ? tile * 128 - vis.start : 0;
-  const int n_first = static_cast<int>(first < 0 ? 0 : first < a.N ? first : a.N) / Q * Q;
-  const int n_tiles = tile * 128 < vis.len && first < a.N ? (a.N - n_first + Q - 1) / Q : 0;
+  const int64_t seen = a.causal ? tile * 128 - vis.start : 0;
+  const int n_first = static_cast<int>(seen < 0 ? 0 : seen < a.N ? seen : a.N) / Q * Q;
+  const int n_tiles = tile * 128 < vis.len && seen < a.N ? (a.N - n_first + Q - 1) / Q : 0;
+  // this part of them, over all heads
+  const int64_t all = static_cast<int64_t>(G) * n_tiles;
+  const int begin = static_cast<int>(all * part / parts), total = static_cast<int>(all * (part + 1) / parts);
 
-  if (n_tiles > 0) {
+  if (begin < total) {
     s16x8 kf[2][S];
     {
       const int64_t row = min(key, vis.len - 1);
@@ -102,7 +113,6 @@ __global__ __launch_bounds__(kThreads, 2) void diff_dkv_kernel(DiffArgs a, float
     const RowReader<D> rows(lane, true), keys(lane, false);
     const ColReader<D> cols(lane);
     const float c = a.scale * kLog2e;
-    const int total = G * n_tiles;
     const auto copy = [&](int at, int buf) {
       const int h = hk * G + at / n_tiles, n0 = n_first + at % n_tiles * Q;
       const T* qp = static_cast<const T*>(a.q.p) + b * a.q.sb + h * a.q.sh + n0 * a.q.sn;
@@ -117,22 +127,20 @@ __global__ __launch_bounds__(kThreads, 2) void diff_dkv_kernel(DiffArgs a, float
         copy_1k(stat_at(stat, static_cast<int64_t>(b) * a.Hq + h, n0, a.N), (lane / 8) * 256 + (lane % 8) * 16,
                 __builtin_amdgcn_readfirstlane(lds_offset(st[buf])));
     };
-    copy(0, 0);
-    for (int at = 0; at < total; ++at) {
-      const int buf = at % 2;
+    copy(begin, 0);
+    for (int at = begin, buf = 0; at < total; ++at, buf ^= 1) {
       wait_copies();
       barrier();  // every wave's copies have arrived, and the other buffer has been read
       if (at + 1 < total) copy(at + 1, buf ^ 1);
       const int n = n_first + at % n_tiles * Q;
       // the wave's first key is seen by none of the 32 queries
       if (a.causal && key0 > vis.start + n + 31) continue;
-      const float minus = -a.lam[hk * G + at / n_tiles];
+      const float minus = minus_sign(load_uniform(a.lam + hk * G + at / n_tiles));
       const uint32_t qt = lds_offset(lds[buf][0]), ot = lds_offset(lds[buf][1]);
-      int hidden = 0;  // queries from here on see the key
-      if (a.causal && key0 + 31 > vis.start + n) {
-        const int64_t w = key - vis.start - n - 16 * g;
-        hidden = static_cast<int>(w < 0 ? 0 : w < 16 ? w : 16);
-      }
+      // query n + 16 g + e sees the key from e = first on
+      const int64_t behind = key - vis.start - n - 16 * g;
+      const int first = static_cast<int>(behind < 0 ? 0 : behind < 16 ? behind : 16);
+      const bool hidden = a.causal && key0 + 31 > vis.start + n;  // the wave's last key from some of the queries
       f32x16 dp = read16(&st[buf][2][16 * g]);  // dP - del1
 #pragma unroll
       for (int s = 0; s < 2 * S; ++s) dp = mma<T>(rows.read(ot, 0, s), keys.read(vt, 0, s), dp);
@@ -143,14 +151,19 @@ __global__ __launch_bounds__(kThreads, 2) void diff_dkv_kernel(DiffArgs a, float
         f32x16 x = read16(&st[buf][i][16 * g]);
 #pragma unroll
         for (int s = 0; s < S; ++s) x = mma<T>(rows.read(qt, 0, i * S + s), kf[i][s], x);
+        if (hidden)
+#pragma unroll
+          for (int e = 0; e < 16; ++e) x[e] = e < first ? -__builtin_inff() : x[e];
         float d[16];
-        if (i) dp += read16(&st[buf][3][16 * g]);  // dP - del2
+        if (i) {  // (-sgn lambda) (dP - del2)
+          const f32x16 y = read16(&st[buf][3][16 * g]);
+#pragma unroll
+          for (int e = 0; e < 16; ++e) dp[e] = __builtin_fmaf(dp[e], minus, y[e]);
+        }
 #pragma unroll
         for (int e = 0; e < 16; ++e) {
-          float p = exp2_fast(x[e] * c);
-          if (i) p *= minus;
-          p = e < hidden ? 0.0f : p;
-          w[e] = i ? w[e] + p : p;
+          const float p = exp2_fast(x[e] * c);
+          w[e] = i ? __builtin_fmaf(p, minus, w[e]) : p;
           d[e] = p * dp[e];
         }
         df[i][0] = pack8<T>(d);
@@ -173,6 +186,15 @@ __global__ __launch_bounds__(kThreads, 2) void diff_dkv_kernel(DiffArgs a, float
   for (int e = 0; e < 16; ++e) {
     const int kk = key0 + 8 * (e / 4) + 4 * g + e % 4;
     if (kk >= a.M) continue;
+    if (parts > 1) {
+      float* s = sums + ((static_cast<int64_t>(part) * a.B * a.Hk + bh) * a.M + kk) * 2 * D + lane % 32;
+#pragma unroll
+      for (int t = 0; t < S; ++t) {
+        s[32 * t] = dk[t / (S / 2)][t % (S / 2)][e];
+        s[D + 32 * t] = dv[t][e];
+      }
+      continue;
+    }
     const bool valid = kk < vis.len;
     T* kp = static_cast<T*>(a.dk.p) + b * a.dk.sb + hk * a.dk.sh + kk * a.dk.sn + lane % 32;
     T* vp = static_cast<T*>(a.dv.p) + b * a.dv.sb + hk * a.dv.sh + kk * a.dv.sn + lane % 32;
@@ -182,6 +204,33 @@ __global__ __launch_bounds__(kThreads, 2) void diff_dkv_kernel(DiffArgs a, float
       vp[32 * t] = static_cast<T>(valid ? dv[t][e] : 0.0f);
     }
   }
+}
+
+// The parts of dK and dV added up in order: D/4 threads a key, with 4 channels of each.
+template <typename T, int D>
+__global__ __launch_bounds__(kThreads) void diff_dkv_join_kernel(DiffArgs a, const float* sums, int parts, int64_t keys) {
+  constexpr int TPK = D / 4;
+  const int64_t r = static_cast<int64_t>(blockIdx.x) * (kThreads / TPK) + threadIdx.x / TPK;
+  if (r >= keys) return;
+  const int64_t bh = r / a.M;
+  const int kk = static_cast<int>(r - bh * a.M), b = static_cast<int>(bh / a.Hk), hk = static_cast<int>(bh % a.Hk);
+  const int ch = threadIdx.x % TPK * 4;
+  f32x4 k{}, v{};
+  if (kk < visible(a, b).len)
+    for (int p = 0; p < parts; ++p) {
+      const float* s = sums + (p * keys + r) * 2 * D + ch;
+      k += *reinterpret_cast<const f32x4*>(s);
+      v += *reinterpret_cast<const f32x4*>(s + D);
+    }
+  typedef T Tx4 __attribute__((ext_vector_type(4)));
+  Tx4 ko, vo;
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    ko[i] = static_cast<T>(k[i] * a.scale);
+    vo[i] = static_cast<T>(v[i]);
+  }
+  *reinterpret_cast<Tx4*>(static_cast<T*>(a.dk.p) + b * a.dk.sb + hk * a.dk.sh + kk * a.dk.sn + ch) = ko;
+  *reinterpret_cast<Tx4*>(static_cast<T*>(a.dv.p) + b * a.dv.sb + hk * a.dv.sh + kk * a.dv.sn + ch) = vo;
 }
 
 // del and dQ of 128 rows (a key head's query heads together, as in the forward pass): 4 waves with 32 rows each; 64 keys
@@ -256,7 +305,8 @@ __global__ __launch_bounds__(kThreads, 2) void diff_dq_kernel(DiffArgs a, float*
 #pragma unroll
         for (int s = 0; s < 2 * S; ++s) dp = mma<T>(rows.read(vt, j, s), of[s], dp);
         s16x8 df[2][2];
-        const int left = at + 32 > low ? limit - at - 16 * g : 16;
+        const bool mask = at + 32 > low;
+        const int left = limit - at - 16 * g;
 #pragma unroll
         for (int i = 0; i < 2; ++i) {
           f32x16 x{};
@@ -264,10 +314,12 @@ __global__ __launch_bounds__(kThreads, 2) void diff_dq_kernel(DiffArgs a, float*
           for (int s = 0; s < S; ++s) x = mma<T>(rows.read(kt, j, i * S + s), qf[i][s], x);
           const float l = lse[i] * c;
           float ds[16];
+          if (mask)
+#pragma unroll
+            for (int e = 0; e < 16; ++e) x[e] = e < left ? x[e] : -__builtin_inff();
 #pragma unroll
           for (int e = 0; e < 16; ++e) {
-            float p = exp2_fast(__builtin_fmaf(x[e], c, -l));
-            p = e < left ? p : 0.0f;
+            const float p = exp2_fast(__builtin_fmaf(x[e], c, -l));
             if constexpr (kSums) {
               d[i] = __builtin_fmaf(p, dp[e], d[i]);
             } else {
@@ -294,10 +346,10 @@ __global__ __launch_bounds__(kThreads, 2) void diff_dq_kernel(DiffArgs a, float*
   walk(std::integral_constant<int, 0>{});
 #pragma unroll
   for (int i = 0; i < 2; ++i) d[i] = sum_halves(d[i]);
-  if (live && lane < 32) put_stat(stat_at(stat, bhn, n, a.N), lse[0], lse[1], d[0], d[1]);
+  if (live && lane < 32) put_stat(stat_at(stat, bhn, n, a.N), lse[0], lse[1], d[0], d[1], a.lam[h], c);
   if (tile == tiles - 1)  // rows behind the last token
     for (int x = threadIdx.x; x < G * static_cast<int>(padded(a.N) - a.N); x += kThreads)
-      put_stat(stat_at(stat, static_cast<int64_t>(b) * a.Hq + hk * G + x % G, a.N + x / G, a.N), kNever, kNever, 0.0f, 0.0f);
+      put_stat(stat_at(stat, static_cast<int64_t>(b) * a.Hq + hk * G + x % G, a.N + x / G, a.N), kNever, kNever, 0.0f, 0.0f, 1.0f, 1.0f);
   wait_copies();
   barrier();  // the tiles have been read
   walk(std::integral_constant<int, 1>{});
@@ -320,7 +372,7 @@ __global__ __launch_bounds__(kThreads) void diff_dlam_kernel(DiffArgs a, float* 
   for (int b = 0; b < a.B; ++b) {
     for (int n = threadIdx.x; n < a.N; n += kThreads) {
       const float* s = stat_at(stat, static_cast<int64_t>(b) * a.Hq + h, n, a.N);
-      t += -static_cast<double>(s[128]) - s[192];
+      t += -static_cast<double>(s[128]) - s[192] * minus_sign(a.lam[h]);
     }
   }
   sums[threadIdx.x] = t;
@@ -332,6 +384,17 @@ __global__ __launch_bounds__(kThreads) void diff_dlam_kernel(DiffArgs a, float* 
   if (threadIdx.x == 0) a.dlam[h] = static_cast<float>(-sums[0]);
 }
 
+int64_t stat_floats(int B, int Hq, int N) { return 4ll * B * Hq * padded(N); }
+
+// Parts of the queries that a key tile's workgroups share: as many as bring the card 768 workgroups (3 of its rounds of
+// 2 a CU, so that tiles that few queries see even out), of 8 query tiles at least.
+int dkv_parts(int B, int Hq, int Hk, int N, int M) {
+  const int64_t units = static_cast<int64_t>(B) * Hk * ((M + 127ll) / 128);
+  const int64_t want = 768 / units, most = static_cast<int64_t>(Hq / Hk) * ((N + 31) / 32) / 8;
+  const int64_t parts = want < most ? want : most;
+  return static_cast<int>(parts < 1 ? 1 : parts);
+}
+
 template <typename T, int D>
 hipError_t launch(const DiffArgs& a, hipStream_t stream) {
   float* stat = a.ws;
@@ -339,15 +402,22 @@ hipError_t launch(const DiffArgs& a, hipStream_t stream) {
   const int64_t row_units = static_cast<int64_t>(a.B) * a.Hk * row_tiles;
   diff_dq_kernel<T, D><<<grid_of(row_units), kThreads, 0, stream>>>(a, stat, row_tiles, row_units);
   const int key_tiles = static_cast<int>((a.M + 127ll) / 128);
-  const int64_t key_units = static_cast<int64_t>(a.B) * a.Hk * key_tiles;
-  diff_dkv_kernel<T, D><<<grid_of(key_units), kThreads, 0, stream>>>(a, stat, key_tiles, key_units);
+  const int parts = dkv_parts(a.B, a.Hq, a.Hk, a.N, a.M);
+  const int64_t keys = static_cast<int64_t>(a.B) * a.Hk * a.M, key_units = static_cast<int64_t>(a.B) * a.Hk * key_tiles * parts;
+  float* sums = stat + stat_floats(a.B, a.Hq, a.N);
+  diff_dkv_kernel<T, D><<<grid_of(key_units), kThreads, 0, stream>>>(a, stat, sums, key_tiles, parts, key_units);
+  if (parts > 1)
+    diff_dkv_join_kernel<T, D><<<static_cast<unsigned>((keys + 1024 / D - 1) / (1024 / D)), kThreads, 0, stream>>>(a, sums, parts, keys);
   diff_dlam_kernel<<<a.Hq, kThreads, 0, stream>>>(a, stat);
   return hipGetLastError();
 }
 
 }  // namespace
 
-int64_t diff_bwd_ws_bytes(int B, int Hq, int N) { return static_cast<int64_t>(B) * Hq * padded(N) * 16; }
+int64_t diff_bwd_ws_bytes(int B, int Hq, int Hk, int N, int M, int d) {
+  const int64_t parts = dkv_parts(B, Hq, Hk, N, M);
+  return 4 * (stat_floats(B, Hq, N) + (parts > 1 ? parts * B * Hk * M * 2 * d : 0));
+}
 
 hipError_t launch_diff_bwd(const DiffArgs& a, hipStream_t stream) {
   if (a.dtype == DA2_BF16) return a.d == 128 ? launch<bf16_t, 128>(a, stream) : launch<bf16_t, 64>(a, stream);

@@ -158,7 +158,7 @@ da2::DiffArgs diff_args(const da2_diff_problem* p, int32_t dtype) {
 
 int64_t diff_ws(const da2_diff_problem* p, bool train) {
   const int64_t f = da2::diff_fwd_ws_bytes(p->B, p->Hq, p->Hk, p->N, p->M, p->d);
-  return train ? std::max(f, da2::diff_bwd_ws_bytes(p->B, p->Hq, p->N)) : f;
+  return train ? std::max(f, da2::diff_bwd_ws_bytes(p->B, p->Hq, p->Hk, p->N, p->M, p->d)) : f;
 }
 
 // A stride of an extent of 1 is never multiplied by more than zero, but 64-row copies form row * stride in 32 bits.

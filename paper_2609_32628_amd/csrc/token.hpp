@@ -134,7 +134,7 @@ struct DiffArgs {
   float* dlam;
 };
 int64_t diff_fwd_ws_bytes(int B, int Hq, int Hk, int N, int M, int d);
-int64_t diff_bwd_ws_bytes(int B, int Hq, int N);
+int64_t diff_bwd_ws_bytes(int B, int Hq, int Hk, int N, int M, int d);
 hipError_t launch_diff_fwd(const DiffArgs& a, hipStream_t stream);
 hipError_t launch_diff_bwd(const DiffArgs& a, hipStream_t stream);
 
