@@ -149,11 +149,13 @@ __device__ inline int key_limit(const DiffArgs& a, const Visible& s, int n) {
 
 // Workgroup id -> unit of work, such that each XCD (ids go around the eight of
 // them) has consecutive units, which share a head's keys in its L2; -1: none.
-__device__ inline int64_t unit_of(int64_t id, int64_t total) {
-  const int64_t per = (total + 7) / 8, u = (id % 8) * per + id / 8;
+// Units, rows of a key head and workgroups are 32-bit numbers (the host checks):
+// a 64-bit division costs a short call as much as a key tile.
+__device__ inline int unit_of(uint32_t id, int total) {
+  const int per = (total + 7) / 8, u = static_cast<int>(id % 8) * per + static_cast<int>(id / 8);
   return u < total ? u : -1;
 }
-inline unsigned grid_of(int64_t total) { return static_cast<unsigned>((total + 7) / 8 * 8); }
+inline unsigned grid_of(int total) { return static_cast<unsigned>((total + 7) / 8 * 8); }
 
 __device__ inline float max16(const f32x16& v) {
   const float a = fmaxf(fmaxf(v[0], v[1]), v[2]), b = fmaxf(fmaxf(v[3], v[4]), v[5]);

@@ -70,17 +70,16 @@ __device__ inline f32x16 read16(const float* p) {
 // dK and dV of 128 keys: 4 waves with 32 keys each; 32 queries of one head at a time in LDS. A wave's keys are in
 // registers, its values in LDS: both in registers would leave one wave a SIMD at d = 128.
 template <typename T, int D>
-__global__ __launch_bounds__(kThreads, 2) void diff_dkv_kernel(DiffArgs a, float* stat, float* sums, int tiles, int parts, int64_t units) {
+__global__ __launch_bounds__(kThreads, 2) void diff_dkv_kernel(DiffArgs a, float* stat, float* sums, int tiles, int parts, int units) {
   constexpr int S = D / 32, Q = 32, BYTES = Q * Tile<D>::kRow, R = Tile<D>::kRowsPerCopy;
   __shared__ __align__(256) char lds[2][2][BYTES];  // [buffer][Q, dO]
   __shared__ __align__(256) char val[4 * BYTES];    // the workgroup's rows of V
   __shared__ __align__(16) float st[2][4][Q];
-  const int64_t unit = unit_of(blockIdx.x, units);
+  const int unit = unit_of(blockIdx.x, units);
   if (unit < 0) return;
   // the first keys are seen by most queries under a causal mask: they go first
-  const int part = static_cast<int>(unit % parts), tile = static_cast<int>(unit / parts % tiles);
-  const int64_t bh = unit / parts / tiles;
-  const int b = static_cast<int>(bh / a.Hk), hk = static_cast<int>(bh % a.Hk), G = a.Hq / a.Hk;
+  const int part = unit % parts, tile = unit / parts % tiles, bh = unit / parts / tiles;
+  const int b = bh / a.Hk, hk = bh % a.Hk, G = a.Hq / a.Hk;
   const int lane = threadIdx.x % 64, g = lane / 32, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64);
   const Visible vis = visible(a, b);
   const int key0 = tile * 128 + 32 * wave, key = key0 + lane % 32;
@@ -94,8 +93,7 @@ __global__ __launch_bounds__(kThreads, 2) void diff_dkv_kernel(DiffArgs a, float
   const int n_first = static_cast<int>(seen < 0 ? 0 : seen < a.N ? seen : a.N) / Q * Q;
   const int n_tiles = tile * 128 < vis.len && seen < a.N ? (a.N - n_first + Q - 1) / Q : 0;
   // this part of them, over all heads
-  const int64_t all = static_cast<int64_t>(G) * n_tiles;
-  const int begin = static_cast<int>(all * part / parts), total = static_cast<int>(all * (part + 1) / parts);
+  const int each = (G * n_tiles + parts - 1) / parts, begin = part * each, total = min(begin + each, G * n_tiles);
 
   if (begin < total) {
     s16x8 kf[2][S];
@@ -212,8 +210,8 @@ __global__ __launch_bounds__(kThreads) void diff_dkv_join_kernel(DiffArgs a, con
   constexpr int TPK = D / 4;
   const int64_t r = static_cast<int64_t>(blockIdx.x) * (kThreads / TPK) + threadIdx.x / TPK;
   if (r >= keys) return;
-  const int64_t bh = r / a.M;
-  const int kk = static_cast<int>(r - bh * a.M), b = static_cast<int>(bh / a.Hk), hk = static_cast<int>(bh % a.Hk);
+  const int bh = static_cast<uint32_t>(r) / static_cast<uint32_t>(a.M), kk = static_cast<uint32_t>(r) - bh * a.M;
+  const int b = bh / a.Hk, hk = bh % a.Hk;
   const int ch = threadIdx.x % TPK * 4;
   f32x4 k{}, v{};
   if (kk < visible(a, b).len)
@@ -236,24 +234,23 @@ __global__ __launch_bounds__(kThreads) void diff_dkv_join_kernel(DiffArgs a, con
 // del and dQ of 128 rows (a key head's query heads together, as in the forward pass): 4 waves with 32 rows each; 64 keys
 // at a time in LDS, twice over. The rows' statistics go to `stat`.
 template <typename T, int D>
-__global__ __launch_bounds__(kThreads, 2) void diff_dq_kernel(DiffArgs a, float* stat, int tiles, int64_t units) {
+__global__ __launch_bounds__(kThreads, 2) void diff_dq_kernel(DiffArgs a, float* stat, int tiles, int units) {
   constexpr int S = D / 32, K = 64, BYTES = K * Tile<D>::kRow, R = Tile<D>::kRowsPerCopy;
   __shared__ __align__(256) char lds[2][2][BYTES];  // [buffer][K, V]
-  const int64_t unit = unit_of(blockIdx.x, units);
+  const int unit = unit_of(blockIdx.x, units);
   if (unit < 0) return;
-  const int tile = tiles - 1 - static_cast<int>(unit % tiles);
-  const int64_t bh = unit / tiles;
-  const int b = static_cast<int>(bh / a.Hk), hk = static_cast<int>(bh % a.Hk), G = a.Hq / a.Hk;
+  const int tile = tiles - 1 - unit % tiles, bh = unit / tiles;
+  const int b = bh / a.Hk, hk = bh % a.Hk, G = a.Hq / a.Hk;
   const int lane = threadIdx.x % 64, g = lane / 32, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64);
-  const int64_t rows_all = static_cast<int64_t>(a.N) * G, row0 = static_cast<int64_t>(tile) * 128 + 32 * wave;
-  const auto token = [&](int64_t r) { return static_cast<int>((r < rows_all ? r : rows_all - 1) / G); };
-  const int64_t row = row0 + lane % 32;
-  const bool live = row < rows_all;
-  const int n = token(row), h = hk * G + static_cast<int>((live ? row : rows_all - 1) % G);
+  const uint32_t rows_all = static_cast<uint32_t>(a.N) * G, row0 = tile * 128u + 32 * wave;
+  const auto token = [&](uint32_t r) { return static_cast<int>(min(r, rows_all - 1) / static_cast<uint32_t>(G)); };
+  const bool live = row0 + lane % 32 < rows_all;
+  const uint32_t row = min(row0 + lane % 32, rows_all - 1);
+  const int n = token(row), h = hk * G + static_cast<int>(row) - n * G;
   const Visible vis = visible(a, b);
   const int limit = key_limit(a, vis, n);
   const int low = key_limit(a, vis, token(row0)), high = key_limit(a, vis, token(row0 + 31));
-  const int end = key_limit(a, vis, token(static_cast<int64_t>(tile) * 128 + 127));
+  const int end = key_limit(a, vis, token(tile * 128u + 127));
 
   s16x8 qf[2][S], of[2 * S];
   {
@@ -399,11 +396,12 @@ template <typename T, int D>
 hipError_t launch(const DiffArgs& a, hipStream_t stream) {
   float* stat = a.ws;
   const int row_tiles = static_cast<int>((static_cast<int64_t>(a.N) * (a.Hq / a.Hk) + 127) / 128);
-  const int64_t row_units = static_cast<int64_t>(a.B) * a.Hk * row_tiles;
+  const int row_units = a.B * a.Hk * row_tiles;
   diff_dq_kernel<T, D><<<grid_of(row_units), kThreads, 0, stream>>>(a, stat, row_tiles, row_units);
   const int key_tiles = static_cast<int>((a.M + 127ll) / 128);
   const int parts = dkv_parts(a.B, a.Hq, a.Hk, a.N, a.M);
-  const int64_t keys = static_cast<int64_t>(a.B) * a.Hk * a.M, key_units = static_cast<int64_t>(a.B) * a.Hk * key_tiles * parts;
+  const int64_t keys = static_cast<int64_t>(a.B) * a.Hk * a.M;  // at most 768 tiles of 128 where they are joined
+  const int key_units = a.B * a.Hk * key_tiles * parts;
   float* sums = stat + stat_floats(a.B, a.Hq, a.N);
   diff_dkv_kernel<T, D><<<grid_of(key_units), kThreads, 0, stream>>>(a, stat, sums, key_tiles, parts, key_units);
   if (parts > 1)

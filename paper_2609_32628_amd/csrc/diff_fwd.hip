@@ -39,16 +39,21 @@ Cut cut_of(int B, int Hq, int Hk, int N, int M) {
   c.few = rows <= 64;
   c.tiles = static_cast<int>(c.few ? (rows + 31) / 32 : (rows + 127) / 128);
   const int64_t units = static_cast<int64_t>(B) * Hk * c.tiles;
-  // two workgroups a CU; a part of fewer than 256 keys costs more to join than to walk
-  int64_t s = 512 / units, most = (M + 255) / 256;
+  // One workgroup a CU (two of few rows), and parts that take longer to walk than to join: 128 keys take a workgroup of
+  // 128 rows 2.5 us, and a launch and the parts' way through memory 10 us and more (150 rows of 24 heads against 2,000
+  // keys: 47 us whole, 36 in two parts; 1,024 against 1,024: 28 and 31).
+  int64_t s = (c.few ? 512 : 256) / units, most = c.few ? (M + 255) / 256 : M / 1024;
   s = s < most ? s : most;
   c.splits = static_cast<int>(s < 1 ? 1 : s);
   return c;
 }
 
-// One part of a row: its unnormalised outputs, maxima and sums.
+// Floats of a row's part of few rows: its unnormalised outputs, maxima and sums. Vectors of 4 of a 32-row part of many
+// rows: its statistics and its 2 D/32 accumulators.
 template <int D>
 constexpr int kPart = 2 * D + 4;
+template <int D>
+constexpr int kBlock = 64 * (1 + 2 * D / 32 * 4);
 
 // 32 rows (a lane's query is lane%32) against 32 keys of a K and a V tile in LDS.
 template <typename T, int D>
@@ -78,38 +83,53 @@ struct Rows32 {
       for (int s = 0; s < S; ++s)
         q[i][s] = *reinterpret_cast<const s16x8*>(row + i * (D / 2) + 16 * s + 8 * (lane / 32));
   }
-  // Keys [key, key + 32) at rows 32 j of the tiles kt and vt; limit: the lane's query sees the keys below it.
-  __device__ void step(uint32_t kt, uint32_t vt, int j, int key, int limit, bool mask, float c) {
-    s16x8 p[2][2];
+  // Scores of both maps with keys [key, key + 32), at rows 32 j of the tile kt; limit: the lane's query sees the keys
+  // below it.
+  __device__ void scores(f32x16 (&x)[2], uint32_t kt, int j, int key, int limit, bool mask) const {
+    x[0] = x[1] = f32x16{};
 #pragma unroll
-    for (int i = 0; i < 2; ++i) {
-      f32x16 x{};
+    for (int s = 0; s < S; ++s)
 #pragma unroll
-      for (int s = 0; s < S; ++s) x = mma<T>(rows.read(kt, j, i * S + s), q[i][s], x);
-      if (mask) {
-        const int left = limit - key - 16 * (lane / 32);
+      for (int i = 0; i < 2; ++i) x[i] = mma<T>(rows.read(kt, j, i * S + s), q[i][s], x[i]);
+    if (mask) {
+      const int left = limit - key - 16 * (lane / 32);
 #pragma unroll
-        for (int e = 0; e < 16; ++e) x[e] = e < left ? x[e] : -__builtin_inff();
-      }
-      // The maximum is a reference for the exponentials only: it follows when a score passes it by 2^8, which the
-      // weights' float32 sums and 16-bit values hold, so that the accumulators are rarely rescaled.
-      const float top = max_halves(max16(x)) * c;
-      if (__any(top > m[i] + 8.0f)) {
-        const float to = fmaxf(m[i], top), f = exp2_fast(m[i] - to);
+      for (int i = 0; i < 2; ++i)
+#pragma unroll
+        for (int e = 0; e < 16; ++e) x[i][e] = e < left ? x[i][e] : -__builtin_inff();
+    }
+  }
+  // The maximum is a reference for the exponentials only: it follows when a score passes it by 2^8, which the weights'
+  // float32 sums and 16-bit values hold, so that the accumulators are rarely rescaled.
+  __device__ void follow(const f32x16 (&x)[2], float c) {
+    float top[2];
+#pragma unroll
+    for (int i = 0; i < 2; ++i) top[i] = max_halves(max16(x[i])) * c;
+    if (__any(top[0] > m[0] + 8.0f || top[1] > m[1] + 8.0f)) {
+#pragma unroll
+      for (int i = 0; i < 2; ++i) {
+        const float to = fmaxf(m[i], top[i]), f = exp2_fast(m[i] - to);
         m[i] = to;
         l[i] *= f;
 #pragma unroll
         for (int t = 0; t < C; ++t) u[i][t] *= f;
       }
+    }
+  }
+  __device__ void weights(s16x8 (&p)[2][2], const f32x16 (&x)[2], float c) {
+#pragma unroll
+    for (int i = 0; i < 2; ++i) {
       float w[16];
 #pragma unroll
       for (int e = 0; e < 16; ++e) {
-        w[e] = exp2_fast(__builtin_fmaf(x[e], c, -m[i]));
+        w[e] = exp2_fast(__builtin_fmaf(x[i][e], c, -m[i]));
         l[i] += w[e];
       }
       p[i][0] = pack8<T>(w);
       p[i][1] = pack8<T>(w + 8);
     }
+  }
+  __device__ void values(const s16x8 (&p)[2][2], uint32_t vt, int j) {
 #pragma unroll
     for (int t = 0; t < C; ++t)
 #pragma unroll
@@ -118,6 +138,14 @@ struct Rows32 {
         u[0][t] = mma<T>(v, p[0][s], u[0][t]);
         u[1][t] = mma<T>(v, p[1][s], u[1][t]);
       }
+  }
+  __device__ void step(uint32_t kt, uint32_t vt, int j, int key, int limit, bool mask, float c) {
+    f32x16 x[2];
+    s16x8 p[2][2];
+    scores(x, kt, j, key, limit, mask);
+    follow(x, c);
+    weights(p, x, c);
+    values(p, vt, j);
   }
 };
 
@@ -131,13 +159,13 @@ __device__ inline void store_lse(const DiffArgs& a, int b, int h, int n, int i, 
       l > 0.0f ? kLn2 * (m + __builtin_amdgcn_logf(l)) : -__builtin_inff();
 }
 
-// Output of one row from its accumulators as columns (see store_columns).
+// Output of one row from its accumulators as columns (see store_columns) and its whole sums l.
 template <typename T, int D>
 __device__ inline void finish_rows(const DiffArgs& a, Rows32<T, D>& r, int b, int h, int n, bool live) {
   float inv[2];
 #pragma unroll
   for (int i = 0; i < 2; ++i) {
-    const float l = sum_halves(r.l[i]);
+    const float l = r.l[i];
     inv[i] = l > 0.0f ? 1.0f / l : 0.0f;
     if (a.lse && live && r.lane < 32) store_lse(a, b, h, n, i, r.m[i], l);
   }
@@ -159,27 +187,28 @@ __device__ inline void finish_element(const DiffArgs& a, int b, int h, int n, in
   row_ptr<T>(a.o, b, h, n)[ch] = static_cast<T>(u1 * i1 - u2 * (a.lam[h] * i2));
 }
 
-template <typename T, int D>
-__global__ __launch_bounds__(kThreads, 2) void diff_many_kernel(DiffArgs a, int tiles, int splits, int64_t units) {
-  constexpr int K = 64, BYTES = K * Tile<D>::kRow, R = Tile<D>::kRowsPerCopy;
+// HALVES: 1, or 2 where each wave's rows are shared by a second wave, which takes every other 32 keys.
+template <typename T, int D, int HALVES>
+__global__ __launch_bounds__(HALVES * kThreads, 2) void diff_many_kernel(DiffArgs a, int tiles, int splits, int units) {
+  constexpr int K = 64 * HALVES, WAVES = 4 * HALVES, BYTES = K * Tile<D>::kRow, R = Tile<D>::kRowsPerCopy, C = D / 32;
   __shared__ __align__(256) char lds[2][2][BYTES];  // [buffer][K, V]
-  const int64_t unit = unit_of(blockIdx.x, units);
+  const int unit = unit_of(blockIdx.x, units);
   if (unit < 0) return;
-  const int split = static_cast<int>(unit % splits);
+  const int split = unit % splits;
   // the last rows see most keys under a causal mask: they go first
-  const int tile = tiles - 1 - static_cast<int>(unit / splits % tiles);
-  const int64_t bh = unit / splits / tiles;
-  const int b = static_cast<int>(bh / a.Hk), hk = static_cast<int>(bh % a.Hk), G = a.Hq / a.Hk;
-  const int lane = threadIdx.x % 64, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64);
-  const int64_t rows = static_cast<int64_t>(a.N) * G, row0 = static_cast<int64_t>(tile) * 128 + 32 * wave;
-  const auto token = [&](int64_t r) { return static_cast<int>((r < rows ? r : rows - 1) / G); };
-  const int64_t row = row0 + lane % 32;
-  const bool live = row < rows;
-  const int n = token(row), h = hk * G + static_cast<int>((live ? row : rows - 1) % G);
+  const int tile = tiles - 1 - unit / splits % tiles;
+  const int bh = unit / splits / tiles;
+  const int b = bh / a.Hk, hk = bh % a.Hk, G = a.Hq / a.Hk;
+  const int lane = threadIdx.x % 64, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64), half = wave / 4;
+  const uint32_t rows = static_cast<uint32_t>(a.N) * G, row0 = tile * 128u + 32 * (wave % 4);
+  const auto token = [&](uint32_t r) { return static_cast<int>(min(r, rows - 1) / static_cast<uint32_t>(G)); };
+  const bool live = row0 + lane % 32 < rows;
+  const uint32_t row = min(row0 + lane % 32, rows - 1);
+  const int n = token(row), h = hk * G + static_cast<int>(row) - n * G;
   const Visible vis = visible(a, b);
   const int limit = key_limit(a, vis, n);
   const int low = key_limit(a, vis, token(row0)), high = key_limit(a, vis, token(row0 + 31));  // of the wave
-  int end = key_limit(a, vis, token(static_cast<int64_t>(tile) * 128 + 127));                 // of the workgroup
+  int end = key_limit(a, vis, token(tile * 128u + 127));                                      // of the workgroup
   int key = 0;
   if (splits > 1) {
     const int part = ((end + splits - 1) / splits + K - 1) / K * K;
@@ -193,8 +222,8 @@ __global__ __launch_bounds__(kThreads, 2) void diff_many_kernel(DiffArgs a, int 
   const float c = a.scale * kLog2e;
   const auto copy = [&](int at, int buf) {
 #pragma unroll
-    for (int i = 0; i < K / R / 4; ++i) {
-      const int first = (wave * (K / R / 4) + i) * R;
+    for (int i = 0; i < K / R / WAVES; ++i) {
+      const int first = (wave * (K / R / WAVES) + i) * R;
       copy_rows<D>(kp + at * a.k.sn, 2 * a.k.sn, first, vis.len - 1 - at, lane, lds_offset(lds[buf][0]) + first * Tile<D>::kRow);
       copy_rows<D>(vp + at * a.v.sn, 2 * a.v.sn, first, vis.len - 1 - at, lane, lds_offset(lds[buf][1]) + first * Tile<D>::kRow);
     }
@@ -204,46 +233,121 @@ __global__ __launch_bounds__(kThreads, 2) void diff_many_kernel(DiffArgs a, int 
     wait_copies();
     barrier();  // every wave's copies have arrived, and the other buffer has been read
     if (key + K < end) copy(key + K, buf ^ 1);
-    const uint32_t kt = lds_offset(lds[buf][0]), vt = lds_offset(lds[buf][1]);
+    const uint32_t kt = lds_offset(lds[buf][0]) + half * 32 * Tile<D>::kRow;
+    const uint32_t vt = lds_offset(lds[buf][1]) + half * 32 * Tile<D>::kRow;
 #pragma unroll
-    for (int j = 0; j < 2; ++j) {
-      const int at = key + 32 * j;
+    for (int j = 0; j < K / 32; j += HALVES) {
+      const int at = key + 32 * (j + half);
       if (at < min(high, end)) r.step(kt, vt, j, at, limit, at + 32 > low, c);
     }
   }
+#pragma unroll
+  for (int i = 0; i < 2; ++i) r.l[i] = sum_halves(r.l[i]);
+  // The second half's waves hand their sums to the first half's, one map after the other, in the room of the tiles.
+  if constexpr (HALVES == 2) {
+    f32x4* swap = reinterpret_cast<f32x4*>(lds) + (wave % 4) * (4 * C + 1) * 64 + lane;
+#pragma unroll
+    for (int i = 0; i < 2; ++i) {
+      __syncthreads();
+      if (half) {
+#pragma unroll
+        for (int t = 0; t < C; ++t)
+#pragma unroll
+          for (int e = 0; e < 4; ++e)
+            swap[(4 * t + e) * 64] = f32x4{r.u[i][t][4 * e], r.u[i][t][4 * e + 1], r.u[i][t][4 * e + 2], r.u[i][t][4 * e + 3]};
+        swap[4 * C * 64] = f32x4{r.m[i], r.l[i], 0.0f, 0.0f};
+      }
+      __syncthreads();
+      if (!half) {
+        const f32x4 other = swap[4 * C * 64];
+        const float m = fmaxf(r.m[i], other[0]), f = exp2_fast(r.m[i] - m), g = exp2_fast(other[0] - m);
+        r.m[i] = m;
+        r.l[i] = r.l[i] * f + other[1] * g;
+#pragma unroll
+        for (int t = 0; t < C; ++t)
+#pragma unroll
+          for (int e = 0; e < 4; ++e) {
+            const f32x4 y = swap[(4 * t + e) * 64];
+#pragma unroll
+            for (int x = 0; x < 4; ++x) r.u[i][t][4 * e + x] = r.u[i][t][4 * e + x] * f + y[x] * g;
+          }
+      }
+    }
+  }
+  if (half) return;
   if (splits == 1) {
     finish_rows(a, r, b, h, n, live);
     return;
   }
-  float* part = a.ws + ((bh * rows + (live ? row : rows - 1)) * splits + split) * kPart<D>;
+  // parts lie as the registers do, a wave's 1 KB at a time
+  f32x4* part = reinterpret_cast<f32x4*>(a.ws) + (static_cast<int64_t>(unit) * 4 + wave) * kBlock<D> + lane;
+  part[0] = f32x4{r.m[0], r.l[0], r.m[1], r.l[1]};
 #pragma unroll
-  for (int i = 0; i < 2; ++i) {
-    const float l = sum_halves(r.l[i]);
-    if (live && lane < 32) {
-      part[2 * D + 2 * i] = r.m[i];
-      part[2 * D + 2 * i + 1] = l;
+  for (int t = 0; t < C; ++t)
+#pragma unroll
+    for (int i = 0; i < 2; ++i)
+#pragma unroll
+      for (int e = 0; e < 4; ++e)
+        part[64 * (1 + (t * 2 + i) * 4 + e)] = f32x4{r.u[i][t][4 * e], r.u[i][t][4 * e + 1], r.u[i][t][4 * e + 2], r.u[i][t][4 * e + 3]};
+}
+
+// The parts of 32 rows joined: a wave takes one tile of 32 channels.
+template <typename T, int D>
+__global__ __launch_bounds__(kThreads) void diff_many_join_kernel(DiffArgs a, int tiles, int splits, int blocks) {
+  constexpr int C = D / 32;
+  const int lane = threadIdx.x % 64, w = blockIdx.x * 4 + threadIdx.x / 64, t = w % C, block = w / C;  // block: 32 rows
+  if (block >= blocks) return;
+  const int group = block % 4, bh = block / 4 / tiles, tile = tiles - 1 - block / 4 % tiles;
+  const int b = bh / a.Hk, hk = bh % a.Hk, G = a.Hq / a.Hk;
+  const uint32_t rows = static_cast<uint32_t>(a.N) * G, row0 = tile * 128u + 32 * group;
+  const bool live = row0 + lane % 32 < rows;
+  const uint32_t row = min(row0 + lane % 32, rows - 1);
+  const int n = row / static_cast<uint32_t>(G), h = hk * G + static_cast<int>(row) - n * G;
+  const auto part = [&](int s) {
+    return reinterpret_cast<const f32x4*>(a.ws) + ((static_cast<int64_t>(block / 4) * splits + s) * 4 + group) * kBlock<D> + lane;
+  };
+  float m[2] = {kNoMax, kNoMax}, l[2] = {0.0f, 0.0f};
+  for (int s = 0; s < splits; ++s) {
+    const f32x4 st = part(s)[0];
+#pragma unroll
+    for (int i = 0; i < 2; ++i) {
+      const float to = fmaxf(m[i], st[2 * i]);
+      l[i] = l[i] * exp2_fast(m[i] - to) + st[2 * i + 1] * exp2_fast(st[2 * i] - to);
+      m[i] = to;
     }
-#pragma unroll
-    for (int t = 0; t < D / 32; ++t)
-#pragma unroll
-      for (int e = 0; e < 16; e += 4)
-        if (live)
-          *reinterpret_cast<float4*>(part + i * D + 32 * t + 2 * e + 4 * (lane / 32)) =
-              make_float4(r.u[i][t][e], r.u[i][t][e + 1], r.u[i][t][e + 2], r.u[i][t][e + 3]);
   }
+  if (a.lse && live && t == 0 && lane < 32)
+#pragma unroll
+    for (int i = 0; i < 2; ++i) store_lse(a, b, h, n, i, m[i], l[i]);
+  float x[16] = {};
+  const float f[2] = {l[0] > 0.0f ? 1.0f / l[0] : 0.0f, l[1] > 0.0f ? -a.lam[h] / l[1] : 0.0f};
+  for (int s = 0; s < splits; ++s) {
+    const f32x4 st = part(s)[0];
+#pragma unroll
+    for (int i = 0; i < 2; ++i) {
+      const float g = exp2_fast(st[2 * i] - m[i]) * f[i];
+#pragma unroll
+      for (int e = 0; e < 4; ++e) {
+        const f32x4 y = part(s)[64 * (1 + (t * 2 + i) * 4 + e)];
+#pragma unroll
+        for (int k = 0; k < 4; ++k) x[4 * e + k] = __builtin_fmaf(y[k], g, x[4 * e + k]);
+      }
+    }
+  }
+  store_columns(row_ptr<T>(a.o, b, h, n) + 32 * t, x, live);
 }
 
 template <typename T, int D>
-__global__ __launch_bounds__(kThreads, 1) void diff_few_kernel(DiffArgs a, int tiles, int splits, int64_t units) {
+__global__ __launch_bounds__(kThreads, 1) void diff_few_kernel(DiffArgs a, int tiles, int splits, int units) {
   constexpr int K = 128, BYTES = 32 * Tile<D>::kRow, R = Tile<D>::kRowsPerCopy;
   __shared__ __align__(256) char lds[4][2][2][BYTES];  // [wave][buffer][K, V]
   __shared__ float stat[4][2][32][2];                 // [wave][map][row][m, l]
-  const int64_t unit = unit_of(blockIdx.x, units);
+  const int unit = unit_of(blockIdx.x, units);
   if (unit < 0) return;
-  const int split = static_cast<int>(unit % splits);
-  const int tile = static_cast<int>(unit / splits % tiles);
-  const int64_t bh = unit / splits / tiles;
-  const int b = static_cast<int>(bh / a.Hk), hk = static_cast<int>(bh % a.Hk), G = a.Hq / a.Hk;
+  const int split = unit % splits;
+  const int tile = unit / splits % tiles;
+  const int bh = unit / splits / tiles;
+  const int b = bh / a.Hk, hk = bh % a.Hk, G = a.Hq / a.Hk;
   const int lane = threadIdx.x % 64, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64);
   const int rows = a.N * G, row0 = 32 * tile, live_rows = min(32, rows - row0);
   const int row = row0 + min(lane % 32, live_rows - 1);
@@ -316,7 +420,7 @@ __global__ __launch_bounds__(kThreads, 1) void diff_few_kernel(DiffArgs a, int t
       finish_element<T>(a, b, hh, nn, ch, u[0], u[1], l[0], l[1]);
       if (a.lse && ch < 2) store_lse(a, b, hh, nn, ch, ch ? m[1] : m[0], ch ? l[1] : l[0]);
     } else {
-      float* part = a.ws + ((bh * rows + at) * splits + split) * kPart<D>;
+      float* part = a.ws + ((static_cast<int64_t>(bh) * rows + at) * splits + split) * kPart<D>;
       part[ch] = u[0];
       part[D + ch] = u[1];
       if (ch < 2) {
@@ -329,14 +433,14 @@ __global__ __launch_bounds__(kThreads, 1) void diff_few_kernel(DiffArgs a, int t
 
 // The parts of each row joined: D threads a row.
 template <typename T, int D>
-__global__ __launch_bounds__(kThreads) void diff_join_kernel(DiffArgs a, int splits, int64_t rows_all) {
-  const int64_t r = static_cast<int64_t>(blockIdx.x) * (kThreads / D) + threadIdx.x / D;
+__global__ __launch_bounds__(kThreads) void diff_join_kernel(DiffArgs a, int splits, uint32_t rows_all) {
+  const uint32_t r = blockIdx.x * (kThreads / D) + threadIdx.x / D;
   if (r >= rows_all) return;
   const int ch = threadIdx.x % D, G = a.Hq / a.Hk;
-  const int64_t rows = static_cast<int64_t>(a.N) * G, bh = r / rows, row = r - bh * rows;
-  const int b = static_cast<int>(bh / a.Hk), n = static_cast<int>(row / G);
-  const int h = static_cast<int>(bh % a.Hk) * G + static_cast<int>(row % G);
-  const float* part = a.ws + r * splits * kPart<D>;
+  const uint32_t rows = static_cast<uint32_t>(a.N) * G, bh = r / rows, row = r - bh * rows;
+  const int b = bh / a.Hk, n = row / G;
+  const int h = bh % a.Hk * G + row % G;
+  const float* part = a.ws + static_cast<int64_t>(r) * splits * kPart<D>;
   float m[2] = {kNoMax, kNoMax}, l[2] = {0.0f, 0.0f}, u[2] = {0.0f, 0.0f};
   for (int s = 0; s < splits; ++s)
 #pragma unroll
@@ -355,16 +459,25 @@ __global__ __launch_bounds__(kThreads) void diff_join_kernel(DiffArgs a, int spl
 template <typename T, int D>
 hipError_t launch(const DiffArgs& a, hipStream_t stream) {
   const Cut c = cut_of(a.B, a.Hq, a.Hk, a.N, a.M);
-  const int64_t units = static_cast<int64_t>(a.B) * a.Hk * c.tiles * c.splits;
+  const int units = a.B * a.Hk * c.tiles * c.splits;
   if (c.few) {
     diff_few_kernel<T, D><<<grid_of(units), kThreads, 0, stream>>>(a, c.tiles, c.splits, units);
   } else {
-    diff_many_kernel<T, D><<<grid_of(units), kThreads, 0, stream>>>(a, c.tiles, c.splits, units);
+    // the second wave for a row pays where 4-wave workgroups leave SIMDs with one wave or none, or a causal mask leaves
+    // the last of them alone: 192 tiles of 2,048 keys 67 -> 50 us, 384 causal ones of up to 4,096 168 -> 114, but 384
+    // without a mask 177 -> 197
+    if (units > (a.causal ? 512 : 256)) {
+      diff_many_kernel<T, D, 1><<<grid_of(units), kThreads, 0, stream>>>(a, c.tiles, c.splits, units);
+    } else {
+      diff_many_kernel<T, D, 2><<<grid_of(units), 2 * kThreads, 0, stream>>>(a, c.tiles, c.splits, units);
+    }
   }
-  if (c.splits > 1) {
-    const int64_t rows = static_cast<int64_t>(a.B) * a.Hq * a.N;
-    diff_join_kernel<T, D><<<static_cast<unsigned>((rows + kThreads / D - 1) / (kThreads / D)), kThreads, 0, stream>>>(
-        a, c.splits, rows);
+  if (c.splits > 1 && !c.few) {
+    const int blocks = units / c.splits * 4;
+    diff_many_join_kernel<T, D><<<(blocks * (D / 32) + 3) / 4, kThreads, 0, stream>>>(a, c.tiles, c.splits, blocks);
+  } else if (c.splits > 1) {
+    const uint32_t rows = static_cast<uint32_t>(a.B) * a.Hq * a.N;  // at most 512 tiles of 32
+    diff_join_kernel<T, D><<<(rows + kThreads / D - 1) / (kThreads / D), kThreads, 0, stream>>>(a, c.splits, rows);
   }
   return hipGetLastError();
 }
@@ -373,7 +486,9 @@ hipError_t launch(const DiffArgs& a, hipStream_t stream) {
 
 int64_t diff_fwd_ws_bytes(int B, int Hq, int Hk, int N, int M, int d) {
   const Cut c = cut_of(B, Hq, Hk, N, M);
-  return c.splits == 1 ? 0 : 4ll * B * Hq * N * c.splits * (2 * d + 4);
+  if (c.splits == 1) return 0;
+  if (c.few) return 4ll * B * Hq * N * c.splits * (2 * d + 4);
+  return 16ll * B * Hk * c.tiles * c.splits * 4 * (d == 128 ? kBlock<128> : kBlock<64>);
 }
 
 hipError_t launch_diff_fwd(const DiffArgs& a, hipStream_t stream) {

@@ -84,11 +84,11 @@ __device__ inline void turn(float& a, float& b, float c, float s) {
 template <typename T, int V, bool HALF>
 __global__ __launch_bounds__(kThreads) void rope_kernel(RopeArgs a, int units, int heads) {
   constexpr int P = HALF ? V : (V > 1 ? V / 2 : 1);  // pairs of a unit
-  const int64_t id = static_cast<int64_t>(blockIdx.x) * kThreads + threadIdx.x;
-  const int64_t token = id / units;
-  if (token >= static_cast<int64_t>(a.B) * a.N) return;
+  const uint32_t id = blockIdx.x * kThreads + threadIdx.x;  // below 2^32, as the host checks
+  const uint32_t token = id / static_cast<uint32_t>(units);
+  if (token >= static_cast<uint64_t>(a.B) * a.N) return;
   const int u = static_cast<int>(id - token * units);
-  const int b = static_cast<int>(token / a.N), n = static_cast<int>(token - static_cast<int64_t>(b) * a.N);
+  const int b = token / static_cast<uint32_t>(a.N), n = token - static_cast<uint32_t>(b) * a.N;
   // channels of the unit inside a block: i (and j, the pairs' second halves)
   const int turning = HALF ? a.rot / 2 / V : (V > 1 ? (a.rot + V - 1) / V : a.rot / 2);
   const bool moves = u >= turning;  // channels beyond rot
