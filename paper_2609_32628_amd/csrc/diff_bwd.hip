@@ -231,18 +231,20 @@ __global__ __launch_bounds__(kThreads) void diff_dkv_join_kernel(DiffArgs a, con
   *reinterpret_cast<Tx4*>(static_cast<T*>(a.dv.p) + b * a.dv.sb + hk * a.dv.sh + kk * a.dv.sn + ch) = vo;
 }
 
-// del and dQ of 128 rows (a key head's query heads together, as in the forward pass): 4 waves with 32 rows each; 64 keys
-// at a time in LDS, twice over. The rows' statistics go to `stat`.
-template <typename T, int D>
-__global__ __launch_bounds__(kThreads, 2) void diff_dq_kernel(DiffArgs a, float* stat, int tiles, int units) {
-  constexpr int S = D / 32, K = 64, BYTES = K * Tile<D>::kRow, R = Tile<D>::kRowsPerCopy;
+// del and dQ of 128 rows (a key head's query heads together, as in the forward pass): 4 waves with 32 rows each, or twice
+// as many where each wave's rows are shared by a second one that takes every other 32 keys (HALVES = 2). The keys go
+// through LDS twice, 64 HALVES at a time. The rows' statistics go to `stat`.
+template <typename T, int D, int HALVES>
+__global__ __launch_bounds__(HALVES * kThreads, 2) void diff_dq_kernel(DiffArgs a, float* stat, int tiles, int units) {
+  constexpr int S = D / 32, K = 64 * HALVES, WAVES = 4 * HALVES, BYTES = K * Tile<D>::kRow, R = Tile<D>::kRowsPerCopy;
   __shared__ __align__(256) char lds[2][2][BYTES];  // [buffer][K, V]
+  __shared__ float sums[HALVES == 2 ? 4 : 1][2][64];
   const int unit = unit_of(blockIdx.x, units);
   if (unit < 0) return;
   const int tile = tiles - 1 - unit % tiles, bh = unit / tiles;
   const int b = bh / a.Hk, hk = bh % a.Hk, G = a.Hq / a.Hk;
-  const int lane = threadIdx.x % 64, g = lane / 32, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64);
-  const uint32_t rows_all = static_cast<uint32_t>(a.N) * G, row0 = tile * 128u + 32 * wave;
+  const int lane = threadIdx.x % 64, g = lane / 32, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64), half = wave / 4;
+  const uint32_t rows_all = static_cast<uint32_t>(a.N) * G, row0 = tile * 128u + 32 * (wave % 4);
   const auto token = [&](uint32_t r) { return static_cast<int>(min(r, rows_all - 1) / static_cast<uint32_t>(G)); };
   const bool live = row0 + lane % 32 < rows_all;
   const uint32_t row = min(row0 + lane % 32, rows_all - 1);
@@ -279,8 +281,8 @@ __global__ __launch_bounds__(kThreads, 2) void diff_dq_kernel(DiffArgs a, float*
   const float c = a.scale * kLog2e;
   const auto copy = [&](int at, int buf) {
 #pragma unroll
-    for (int i = 0; i < K / R / 4; ++i) {
-      const int r0 = (wave * (K / R / 4) + i) * R;
+    for (int i = 0; i < K / R / WAVES; ++i) {
+      const int r0 = (wave * (K / R / WAVES) + i) * R;
       copy_rows<D>(kp + at * a.k.sn, 2 * a.k.sn, r0, vis.len - 1 - at, lane, lds_offset(lds[buf][0]) + r0 * Tile<D>::kRow);
       copy_rows<D>(vp + at * a.v.sn, 2 * a.v.sn, r0, vis.len - 1 - at, lane, lds_offset(lds[buf][1]) + r0 * Tile<D>::kRow);
     }
@@ -295,7 +297,7 @@ __global__ __launch_bounds__(kThreads, 2) void diff_dq_kernel(DiffArgs a, float*
       if (key + K < end) copy(key + K, buf ^ 1);
       const uint32_t kt = lds_offset(lds[buf][0]), vt = lds_offset(lds[buf][1]);
 #pragma unroll 1
-      for (int j = 0; j < 2; ++j) {
+      for (int j = half; j < K / 32; j += HALVES) {
         const int at = key + 32 * j;
         if (at >= high) continue;
         f32x16 dp{};
@@ -343,13 +345,47 @@ __global__ __launch_bounds__(kThreads, 2) void diff_dq_kernel(DiffArgs a, float*
   walk(std::integral_constant<int, 0>{});
 #pragma unroll
   for (int i = 0; i < 2; ++i) d[i] = sum_halves(d[i]);
-  if (live && lane < 32) put_stat(stat_at(stat, bhn, n, a.N), lse[0], lse[1], d[0], d[1], a.lam[h], c);
+  if constexpr (HALVES == 2) {
+    if (half)
+#pragma unroll
+      for (int i = 0; i < 2; ++i) sums[wave % 4][i][lane] = d[i];
+    __syncthreads();
+    if (!half)
+#pragma unroll
+      for (int i = 0; i < 2; ++i) sums[wave][i][lane] = d[i] += sums[wave][i][lane];
+    __syncthreads();
+    if (half)
+#pragma unroll
+      for (int i = 0; i < 2; ++i) d[i] = sums[wave % 4][i][lane];
+  }
+  if (!half && live && lane < 32) put_stat(stat_at(stat, bhn, n, a.N), lse[0], lse[1], d[0], d[1], a.lam[h], c);
   if (tile == tiles - 1)  // rows behind the last token
-    for (int x = threadIdx.x; x < G * static_cast<int>(padded(a.N) - a.N); x += kThreads)
+    for (int x = threadIdx.x; x < G * static_cast<int>(padded(a.N) - a.N); x += HALVES * kThreads)
       put_stat(stat_at(stat, static_cast<int64_t>(b) * a.Hq + hk * G + x % G, a.N + x / G, a.N), kNever, kNever, 0.0f, 0.0f, 1.0f, 1.0f);
   wait_copies();
   barrier();  // the tiles have been read
   walk(std::integral_constant<int, 1>{});
+  if constexpr (HALVES == 2) {
+    f32x4* swap = reinterpret_cast<f32x4*>(lds) + (wave % 4) * 4 * S * 64 + lane;
+    __syncthreads();
+#pragma unroll
+    for (int t = 0; t < S; ++t)
+#pragma unroll
+      for (int e = 0; e < 4; ++e) {
+        f32x16& q = dq[t / (S / 2)][t % (S / 2)];
+        if (half) swap[(4 * t + e) * 64] = f32x4{q[4 * e], q[4 * e + 1], q[4 * e + 2], q[4 * e + 3]};
+      }
+    __syncthreads();
+    if (half) return;
+#pragma unroll
+    for (int t = 0; t < S; ++t)
+#pragma unroll
+      for (int e = 0; e < 4; ++e) {
+        const f32x4 y = swap[(4 * t + e) * 64];
+#pragma unroll
+        for (int x = 0; x < 4; ++x) dq[t / (S / 2)][t % (S / 2)][4 * e + x] += y[x];
+      }
+  }
   const float f[2] = {a.scale, -a.lam[h] * a.scale};
   T* out = static_cast<T*>(a.dq.p) + b * a.dq.sb + h * a.dq.sh + n * a.dq.sn;
 #pragma unroll
@@ -397,7 +433,13 @@ hipError_t launch(const DiffArgs& a, hipStream_t stream) {
   float* stat = a.ws;
   const int row_tiles = static_cast<int>((static_cast<int64_t>(a.N) * (a.Hq / a.Hk) + 127) / 128);
   const int row_units = a.B * a.Hk * row_tiles;
-  diff_dq_kernel<T, D><<<grid_of(row_units), kThreads, 0, stream>>>(a, stat, row_tiles, row_units);
+  // as in the forward pass: 192 tiles of 2,048 keys 237 -> 207 us for the backward pass, 384 causal ones of up to 4,096
+  // 518 -> 415, 384 without a mask 655 -> 699
+  if (row_units > (a.causal ? 512 : 256)) {
+    diff_dq_kernel<T, D, 1><<<grid_of(row_units), kThreads, 0, stream>>>(a, stat, row_tiles, row_units);
+  } else {
+    diff_dq_kernel<T, D, 2><<<grid_of(row_units), 2 * kThreads, 0, stream>>>(a, stat, row_tiles, row_units);
+  }
   const int key_tiles = static_cast<int>((a.M + 127ll) / 128);
   const int parts = dkv_parts(a.B, a.Hq, a.Hk, a.N, a.M);
   const int64_t keys = static_cast<int64_t>(a.B) * a.Hk * a.M;  // at most 768 tiles of 128 where they are joined
