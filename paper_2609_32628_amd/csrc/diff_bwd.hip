@@ -67,15 +67,38 @@ __device__ inline f32x16 read16(const float* p) {
   return x;
 }
 
+// dlambda of a head: minus the sum of its rows' del2, in float64 and in a fixed order. 256 threads.
+__device__ inline void sum_dlam(const DiffArgs& a, float* stat, int h, double* sums) {
+  double t = 0.0;
+  for (int b = 0; b < a.B; ++b)
+#pragma unroll 4
+    for (int n = threadIdx.x; n < a.N; n += kThreads) {
+      const float* s = stat_at(stat, static_cast<int64_t>(b) * a.Hq + h, n, a.N);
+      t += -static_cast<double>(s[128]) - s[192] * minus_sign(a.lam[h]);
+    }
+  sums[threadIdx.x] = t;
+  __syncthreads();
+  for (int o = kThreads / 2; o > 0; o >>= 1) {
+    if (threadIdx.x < o) sums[threadIdx.x] += sums[threadIdx.x + o];
+    __syncthreads();
+  }
+  if (threadIdx.x == 0) a.dlam[h] = static_cast<float>(-sums[0]);
+}
+
 // dK and dV of 128 keys: 4 waves with 32 keys each; 32 queries of one head at a time in LDS. A wave's keys are in
-// registers, its values in LDS: both in registers would leave one wave a SIMD at d = 128.
+// registers, its values in LDS: both in registers would leave one wave a SIMD at d = 128. The first workgroups, a
+// multiple of 8, sum dlambda beside them.
 template <typename T, int D>
-__global__ __launch_bounds__(kThreads, 2) void diff_dkv_kernel(DiffArgs a, float* stat, float* sums, int tiles, int parts, int units) {
+__global__ __launch_bounds__(kThreads, 2) void diff_dkv_kernel(DiffArgs a, float* stat, float* sums, int tiles, int parts, int units, int lambdas) {
   constexpr int S = D / 32, Q = 32, BYTES = Q * Tile<D>::kRow, R = Tile<D>::kRowsPerCopy;
   __shared__ __align__(256) char lds[2][2][BYTES];  // [buffer][Q, dO]
   __shared__ __align__(256) char val[4 * BYTES];    // the workgroup's rows of V
   __shared__ __align__(16) float st[2][4][Q];
-  const int unit = unit_of(blockIdx.x, units);
+  if (static_cast<int>(blockIdx.x) < lambdas) {
+    if (static_cast<int>(blockIdx.x) < a.Hq) sum_dlam(a, stat, blockIdx.x, reinterpret_cast<double*>(lds));
+    return;
+  }
+  const int unit = unit_of(blockIdx.x - lambdas, units);
   if (unit < 0) return;
   // the first keys are seen by most queries under a causal mask: they go first
   const int part = unit % parts, tile = unit / parts % tiles, bh = unit / parts / tiles;
@@ -397,33 +420,15 @@ __global__ __launch_bounds__(HALVES * kThreads, 2) void diff_dq_kernel(DiffArgs 
   }
 }
 
-// dlambda of a head: minus the sum of its rows' del2, in float64 and in a fixed order.
-__global__ __launch_bounds__(kThreads) void diff_dlam_kernel(DiffArgs a, float* stat) {
-  __shared__ double sums[kThreads];
-  const int h = blockIdx.x;
-  double t = 0.0;
-  for (int b = 0; b < a.B; ++b) {
-    for (int n = threadIdx.x; n < a.N; n += kThreads) {
-      const float* s = stat_at(stat, static_cast<int64_t>(b) * a.Hq + h, n, a.N);
-      t += -static_cast<double>(s[128]) - s[192] * minus_sign(a.lam[h]);
-    }
-  }
-  sums[threadIdx.x] = t;
-  __syncthreads();
-  for (int o = kThreads / 2; o > 0; o >>= 1) {
-    if (threadIdx.x < o) sums[threadIdx.x] += sums[threadIdx.x + o];
-    __syncthreads();
-  }
-  if (threadIdx.x == 0) a.dlam[h] = static_cast<float>(-sums[0]);
-}
-
 int64_t stat_floats(int B, int Hq, int N) { return 4ll * B * Hq * padded(N); }
 
-// Parts of the queries that a key tile's workgroups share: as many as bring the card 768 workgroups (3 of its rounds of
-// 2 a CU, so that tiles that few queries see even out), of 8 query tiles at least.
-int dkv_parts(int B, int Hq, int Hk, int N, int M) {
+// Parts of the queries that a key tile's workgroups share: as many as bring the card 512 workgroups, two a CU, and half
+// as many again under a causal mask, so that tiles that few queries see even out; of 8 query tiles at least. (128 tiles
+// of a causal step: 288 us for the backward pass in 2 parts, 212 in 4, 191 in 6, 218 in 12; 192 tiles of 1,024 queries
+// without a mask 111 in 2, 121 in 4.)
+int dkv_parts(int B, int Hq, int Hk, int N, int M, bool causal) {
   const int64_t units = static_cast<int64_t>(B) * Hk * ((M + 127ll) / 128);
-  const int64_t want = 768 / units, most = static_cast<int64_t>(Hq / Hk) * ((N + 31) / 32) / 8;
+  const int64_t want = (causal ? 768 : 512) / units, most = static_cast<int64_t>(Hq / Hk) * ((N + 31) / 32) / 8;
   const int64_t parts = want < most ? want : most;
   return static_cast<int>(parts < 1 ? 1 : parts);
 }
@@ -441,21 +446,21 @@ hipError_t launch(const DiffArgs& a, hipStream_t stream) {
     diff_dq_kernel<T, D, 2><<<grid_of(row_units), 2 * kThreads, 0, stream>>>(a, stat, row_tiles, row_units);
   }
   const int key_tiles = static_cast<int>((a.M + 127ll) / 128);
-  const int parts = dkv_parts(a.B, a.Hq, a.Hk, a.N, a.M);
+  const int parts = dkv_parts(a.B, a.Hq, a.Hk, a.N, a.M, a.causal);
   const int64_t keys = static_cast<int64_t>(a.B) * a.Hk * a.M;  // at most 768 tiles of 128 where they are joined
   const int key_units = a.B * a.Hk * key_tiles * parts;
   float* sums = stat + stat_floats(a.B, a.Hq, a.N);
-  diff_dkv_kernel<T, D><<<grid_of(key_units), kThreads, 0, stream>>>(a, stat, sums, key_tiles, parts, key_units);
+  const int lambdas = static_cast<int>(grid_of(a.Hq));
+  diff_dkv_kernel<T, D><<<lambdas + grid_of(key_units), kThreads, 0, stream>>>(a, stat, sums, key_tiles, parts, key_units, lambdas);
   if (parts > 1)
     diff_dkv_join_kernel<T, D><<<static_cast<unsigned>((keys + 1024 / D - 1) / (1024 / D)), kThreads, 0, stream>>>(a, sums, parts, keys);
-  diff_dlam_kernel<<<a.Hq, kThreads, 0, stream>>>(a, stat);
   return hipGetLastError();
 }
 
 }  // namespace
 
 int64_t diff_bwd_ws_bytes(int B, int Hq, int Hk, int N, int M, int d) {
-  const int64_t parts = dkv_parts(B, Hq, Hk, N, M);
+  const int64_t parts = dkv_parts(B, Hq, Hk, N, M, true);  // the most, whatever the mask
   return 4 * (stat_floats(B, Hq, N) + (parts > 1 ? parts * B * Hk * M * 2 * d : 0));
 }
 
