@@ -54,12 +54,14 @@ __device__ inline RowAt row_at(const NormArgs& a, int64_t r, int grp, bool group
 // 16 bytes of a row from element j on, as they lie in memory, and their values, zeros from element C on. No branch depends
 // on the lane, and nothing is done with the bytes before they are needed, so that all chunks of a thread and the next
 // row's are in flight together: lanes behind the row read its last 16 bytes, and where C is no whole number of chunks
-// (TAIL), the last chunk is those, shifted down.
+// (TAIL), the last chunk is those, shifted down. Only a thread's last chunk (`last`, a constant) may end behind the row.
 template <bool TAIL, typename T>
-__device__ inline uint4 fetch(const T* row, int j, int C) {
+__device__ inline uint4 fetch(const T* row, int j, int C, bool last) {
   constexpr int V = kVec<T>;
   uint4 c;
-  if (!TAIL || C >= V) {
+  if (!last) {
+    __builtin_memcpy(&c, row + j, 16);
+  } else if (!TAIL || C >= V) {
     __builtin_memcpy(&c, row + min(j, C - V), 16);
   } else {  // a row of less than a chunk: one element at a time, the last one again behind it
     T e[V];
@@ -70,10 +72,10 @@ __device__ inline uint4 fetch(const T* row, int j, int C) {
   return c;
 }
 template <bool TAIL, typename T>
-__device__ inline void unpack(const uint4& c, int j, int C, float* x) {
+__device__ inline void unpack(const uint4& c, int j, int C, bool last, float* x) {
   constexpr int V = kVec<T>;
   uint32_t w0 = c.x, w1 = c.y, w2 = c.z, w3 = c.w;
-  if (TAIL && C >= V) {
+  if (TAIL && last && C >= V) {
     const int off = min(max(j + V - C, 0), V) * static_cast<int>(sizeof(T));  // bytes that go
     if constexpr (sizeof(T) == 2) {
       const bool odd = off & 2;
@@ -95,17 +97,18 @@ __device__ inline void unpack(const uint4& c, int j, int C, float* x) {
   const uint4 z = make_uint4(w0, w1, w2, w3);
   const Chunk<T> e = __builtin_bit_cast(Chunk<T>, z);
 #pragma unroll
-  for (int i = 0; i < V; ++i) x[i] = (TAIL && C < V ? j + i < C : j < C) ? static_cast<float>(e.v[i]) : 0.0f;
+  for (int i = 0; i < V; ++i) x[i] = !last || (TAIL && C < V ? j + i < C : j < C) ? static_cast<float>(e.v[i]) : 0.0f;
 }
 
 // V weights (or biases) of float32 or 16 bits from element j on as floats; behind C they are any.
 template <bool TAIL, int V>
-__device__ inline void load_weights(const void* w, int dtype, int64_t base, int j, int C, float* x) {
+__device__ inline void load_weights(const void* w, int dtype, int64_t base, int j, int C, bool last, float* x) {
   const int es = dtype == DA2_FP32 ? 4 : 2;
   const char* p = static_cast<const char*>(w) + base * es;
-  uint32_t bits[V];  // TAIL: an element each; else as they lie in memory, 16-bit ones in the first V / 2
-  if constexpr (!TAIL) {
-    p += min(j, C - V) * es;
+  uint32_t bits[V];  // as they lie in memory, 16-bit ones in the first V / 2; or an element each
+  const bool each = TAIL && last;
+  if (!each) {
+    p += (last ? min(j, C - V) : j) * es;
     __builtin_memcpy(bits, p, 2 * V);
     __builtin_memcpy(bits + V / 2, p + (es == 4 ? 2 * V : 0), 2 * V);
   } else if (es == 4) {
@@ -117,7 +120,7 @@ __device__ inline void load_weights(const void* w, int dtype, int64_t base, int 
   }
 #pragma unroll
   for (int i = 0; i < V; ++i) {
-    const uint32_t h = TAIL ? bits[i] : bits[i / 2] >> (16 * (i % 2));
+    const uint32_t h = each ? bits[i] : bits[i / 2] >> (16 * (i % 2));
     if (dtype == DA2_FP32) {
       x[i] = __uint_as_float(bits[i]);
     } else if (dtype == DA2_BF16) {
@@ -169,7 +172,7 @@ __device__ inline void row_sum(float (&v)[N], float* lds) {
 // with a workgroup for each four rows.)
 constexpr int fwd_waves(int n, int tpr) { return n <= 8 ? 6 : n <= 16 || (n <= 24 && tpr <= 64) ? 4 : 3; }
 constexpr int bwd_waves(int n) { return n <= 8 ? 4 : n <= 16 ? 3 : 2; }
-constexpr int64_t resident(int waves, int block) { return 256ll * 4 * 64 * waves / block; }
+constexpr int64_t resident(int waves, int block) { return 256ll * (256 * waves / block); }
 
 template <int TPR>
 constexpr int block_of() {
@@ -190,7 +193,7 @@ __global__ __launch_bounds__(block_of<TPR>(), fwd_waves(K * kVec<T>, TPR)) void 
     if (r >= rows) return;
     next = row_at(a, r, grp, grouped);
 #pragma unroll
-    for (int k = 0; k < K; ++k) raw[k] = fetch<TAIL>(static_cast<const T*>(a.x.p) + next.x, (lane + k * TPR) * V, a.C);
+    for (int k = 0; k < K; ++k) raw[k] = fetch<TAIL>(static_cast<const T*>(a.x.p) + next.x, (lane + k * TPR) * V, a.C, k == K - 1);
   };
   ask(static_cast<int64_t>(blockIdx.x) * RPB + threadIdx.x / TPR);
   float f[K][V], bias[K][V];
@@ -201,8 +204,8 @@ __global__ __launch_bounds__(block_of<TPR>(), fwd_waves(K * kVec<T>, TPR)) void 
       f[k][i] = 1.0f - a.plus;
       bias[k][i] = 0.0f;
     }
-    if (a.w) load_weights<TAIL, V>(a.w, a.wdtype, w0, (lane + k * TPR) * V, a.C, f[k]);
-    if (a.b) load_weights<TAIL, V>(a.b, a.wdtype, w0, (lane + k * TPR) * V, a.C, bias[k]);
+    if (a.w) load_weights<TAIL, V>(a.w, a.wdtype, w0, (lane + k * TPR) * V, a.C, k == K - 1, f[k]);
+    if (a.b) load_weights<TAIL, V>(a.b, a.wdtype, w0, (lane + k * TPR) * V, a.C, k == K - 1, bias[k]);
 #pragma unroll
     for (int i = 0; i < V; ++i) f[k][i] += a.plus;
   }
@@ -210,7 +213,7 @@ __global__ __launch_bounds__(block_of<TPR>(), fwd_waves(K * kVec<T>, TPR)) void 
     const bool live = r0 + threadIdx.x / TPR < rows;  // every thread takes part in the sums
     float v[K][V], mean = 0.0f;
 #pragma unroll
-    for (int k = 0; k < K; ++k) unpack<TAIL, T>(raw[k], (lane + k * TPR) * V, a.C, v[k]);
+    for (int k = 0; k < K; ++k) unpack<TAIL, T>(raw[k], (lane + k * TPR) * V, a.C, k == K - 1, v[k]);
     at = next;
     ask(r0 + step + threadIdx.x / TPR);
     if (a.kind == DA2_NORM_LAYER) {
@@ -228,7 +231,7 @@ __global__ __launch_bounds__(block_of<TPR>(), fwd_waves(K * kVec<T>, TPR)) void 
       const int n = a.C - (lane + k * TPR) * V;
 #pragma unroll
       for (int i = 0; i < V; ++i) {
-        v[k][i] = i < n ? v[k][i] - mean : 0.0f;
+        v[k][i] = k < K - 1 || i < n ? v[k][i] - mean : 0.0f;
         q[0] = __builtin_fmaf(v[k][i], v[k][i], q[0]);
       }
     }
@@ -246,7 +249,7 @@ __global__ __launch_bounds__(block_of<TPR>(), fwd_waves(K * kVec<T>, TPR)) void 
       float o[V];
 #pragma unroll
       for (int i = 0; i < V; ++i) o[i] = __builtin_fmaf(v[k][i] * rstd, f[k][i], bias[k][i]);
-      store_part(y + j, a.C - j, o);
+      store_part(y + j, k < K - 1 ? V : a.C - j, o);
     }
   }
 }
@@ -292,14 +295,14 @@ __device__ inline void norm_long_row(const NormArgs& a, int64_t r, int grp, bool
     const int n = static_cast<int>(a.C - j);
     float f[V];
     load_part(x + j, n, v);
-    if (a.w) load_weights<true, V>(a.w, a.wdtype, w0, static_cast<int>(j), a.C, f);
+    if (a.w) load_weights<true, V>(a.w, a.wdtype, w0, static_cast<int>(j), a.C, j + V > a.C, f);
 #pragma unroll
     for (int i = 0; i < V; ++i) {
       v[i] = (v[i] - mean) * rstd;
       if (a.w) v[i] *= f[i] + a.plus;
     }
     if (a.b) {
-      load_weights<true, V>(a.b, a.wdtype, w0, static_cast<int>(j), a.C, f);
+      load_weights<true, V>(a.b, a.wdtype, w0, static_cast<int>(j), a.C, j + V > a.C, f);
 #pragma unroll
       for (int i = 0; i < V; ++i) v[i] += f[i];
     }
@@ -329,7 +332,7 @@ __global__ __launch_bounds__(block_of<TPR>(), SUMS ? bwd_waves(K * kVec<T>) : 2)
     const int j = (lane + k * TPR) * V;
 #pragma unroll
     for (int i = 0; i < V; ++i) f[k][i] = 1.0f - a.plus;
-    if (a.w) load_weights<TAIL, V>(a.w, a.wdtype, w0, j, a.C, f[k]);
+    if (a.w) load_weights<TAIL, V>(a.w, a.wdtype, w0, j, a.C, k == K - 1, f[k]);
 #pragma unroll
     for (int i = 0; i < V; ++i) f[k][i] += a.plus;
   }
@@ -351,8 +354,8 @@ __global__ __launch_bounds__(block_of<TPR>(), SUMS ? bwd_waves(K * kVec<T>) : 2)
     const T* dy = static_cast<const T*>(a.dy.p) + next.dy;
 #pragma unroll
     for (int k = 0; k < K; ++k) {
-      xr[k] = fetch<TAIL>(x, (lane + k * TPR) * V, a.C);
-      gr[k] = fetch<TAIL>(dy, (lane + k * TPR) * V, a.C);
+      xr[k] = fetch<TAIL>(x, (lane + k * TPR) * V, a.C, k == K - 1);
+      gr[k] = fetch<TAIL>(dy, (lane + k * TPR) * V, a.C, k == K - 1);
     }
     mean = a.rstats[2 * next.row];
     rstd = a.rstats[2 * next.row + 1];
@@ -363,8 +366,8 @@ __global__ __launch_bounds__(block_of<TPR>(), SUMS ? bwd_waves(K * kVec<T>) : 2)
     float xh[K][V], g[K][V];
 #pragma unroll
     for (int k = 0; k < K; ++k) {
-      unpack<TAIL, T>(xr[k], (lane + k * TPR) * V, a.C, xh[k]);
-      unpack<TAIL, T>(gr[k], (lane + k * TPR) * V, a.C, g[k]);
+      unpack<TAIL, T>(xr[k], (lane + k * TPR) * V, a.C, k == K - 1, xh[k]);
+      unpack<TAIL, T>(gr[k], (lane + k * TPR) * V, a.C, k == K - 1, g[k]);
 #pragma unroll
       for (int i = 0; i < V; ++i) {
         xh[k][i] = (xh[k][i] - mean) * rstd;
@@ -399,7 +402,7 @@ __global__ __launch_bounds__(block_of<TPR>(), SUMS ? bwd_waves(K * kVec<T>) : 2)
       float o[V];
 #pragma unroll
       for (int i = 0; i < V; ++i) o[i] = scale * (g[k][i] - __builtin_fmaf(xh[k][i], m1, m0));
-      store_part(dx + j, a.C - j, o);
+      store_part(dx + j, k < K - 1 ? V : a.C - j, o);
     }
   }
   if constexpr (SUMS) {
@@ -470,7 +473,7 @@ __device__ inline void norm_bwd_long_row(const NormArgs& a, int64_t r, int grp, 
     load_part(dy + j, n, g);
 #pragma unroll
     for (int i = 0; i < V; ++i) f[i] = 1.0f - a.plus;
-    if (a.w) load_weights<true, V>(a.w, a.wdtype, w0, static_cast<int>(j), a.C, f);
+    if (a.w) load_weights<true, V>(a.w, a.wdtype, w0, static_cast<int>(j), a.C, j + V > a.C, f);
 #pragma unroll
     for (int i = 0; i < V; ++i) {
       xh[i] = i < n ? (xh[i] - mean) * rstd : 0.0f;
