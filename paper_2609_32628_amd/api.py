@@ -10,7 +10,6 @@ that their tensors' shapes and types belong together and that all of them are
 on one GPU, and raise ValueError before the call otherwise. They run on the
 tensors' GPU, whichever device is current.
 """
-import contextlib
 import ctypes
 from dataclasses import dataclass
 
@@ -184,21 +183,22 @@ NORM_KINDS = {"layer": DA2_NORM_LAYER, "rms": DA2_NORM_RMS}
 
 def _rows(name, x, shape=None, dtype=None):
     """Descriptor of a [B, H, N, C] tensor, checked against the shape and type it must have."""
-    if x.dim() != 4 or (x.stride(3) != 1 and x.shape[3] > 1):
+    st = x.stride()
+    if len(st) != 4 or (st[3] != 1 and x.shape[3] > 1):
         raise ValueError(f"{name}: expected a [B, H, N, C] tensor with its last dimension contiguous")
-    if x.dtype not in DTYPES or (dtype is not None and x.dtype != dtype):
+    dt = DTYPES.get(x.dtype)
+    if dt is None or (dtype is not None and x.dtype != dtype):
         raise ValueError(f"{name}: unsupported dtype {x.dtype}" + (f", expected {dtype}" if dtype else ""))
-    if shape is not None and tuple(x.shape) != tuple(shape):
+    if shape is not None and x.shape != shape:
         raise ValueError(f"{name}: expected shape {tuple(shape)}, got {tuple(x.shape)}")
-    sb, sh, sn, _ = x.stride()
-    return Tensor(sb, sh, sn, DTYPES[x.dtype], 0)
+    return Tensor(st[0], st[1], st[2], dt, 0)
 
 
 def _plain(name, x, shape, dtype):
     """Address of a contiguous tensor of the given shape and type (None: a null pointer)."""
     if x is None:
         return None
-    if tuple(x.shape) != tuple(shape) or x.dtype != dtype or not x.is_contiguous():
+    if x.shape != shape or x.dtype != dtype or not x.is_contiguous():
         raise ValueError(f"{name}: expected a contiguous {dtype} tensor of shape {tuple(shape)}")
     return x.data_ptr()
 
@@ -207,32 +207,50 @@ def _addr(x):
     return None if x is None else x.data_ptr()
 
 
-def _on(stream, *tensors):
-    """The stream's handle, and a context in which the tensors' GPU is the current device."""
-    dev = tensors[0].device
-    if dev.type != "cuda" or any(t is not None and t.device != dev for t in tensors):
-        raise ValueError("expected all tensors on one GPU")
-    if stream is not None and stream.device != dev:
-        raise ValueError(f"the stream belongs to {stream.device}, the tensors to {dev}")
-    s = torch.cuda.current_stream(dev) if stream is None else stream
-    here = torch.cuda.current_device() == dev.index
-    return s.cuda_stream, contextlib.nullcontext() if here else torch.cuda.device(dev)
+def _bytes(ws):
+    return 0 if ws is None else ws.numel() * ws.element_size()
 
 
-def _norm_desc(X, w, b, kind, eps, plus_one):
-    """Rows and NormDesc of a norm over X's last dimension with weights [C] or [B, C]."""
+def _run(call, stream, tensors, *args):
+    """Makes the call on the GPU that holds all the tensors and on its current stream (or the given one)."""
+    dev = tensors[0].get_device()
+    for t in tensors:
+        if t is not None and t.get_device() != dev:
+            raise ValueError("expected all tensors on one GPU")
+    if dev < 0:
+        raise ValueError("expected tensors on a GPU")
+    if stream is None:
+        s = torch._C._cuda_getCurrentRawStream(dev)
+    elif stream.device.index == dev:
+        s = stream.cuda_stream
+    else:
+        raise ValueError(f"the stream belongs to {stream.device}, the tensors to cuda:{dev}")
+    f = getattr(lib(), call)
+    if torch._C._cuda_getDevice() == dev:
+        check(call, f(*args, s))
+    else:
+        with torch.cuda.device(dev):
+            check(call, f(*args, s))
+
+
+def _norm_desc(X, given, kind, eps, plus_one):
+    """Rows and NormDesc of a norm over X's last dimension with weights [C] or [B, C] (``given``: by name)."""
     B, H, N, C = X.shape
-    stride, wdtype = 0, X.dtype
-    given = [(n, t) for n, t in (("w", w), ("b", b)) if t is not None]
+    stride, wdtype, first = 0, X.dtype, None
     for name, t in given:
-        if t.dtype not in DTYPES or tuple(t.shape) not in ((C,), (B, C)) or (C > 1 and t.stride(-1) != 1):
-            raise ValueError(f"{name}: expected [C] or [B, C] weights with C contiguous")
-        if t.shape != given[0][1].shape or t.dtype != given[0][1].dtype or t.stride() != given[0][1].stride():
+        if t is None:
+            continue
+        if first is None:
+            st, first, wdtype = t.stride(), t, t.dtype
+            if wdtype not in DTYPES or t.shape not in ((C,), (B, C)) or (C > 1 and st[-1] != 1):
+                raise ValueError(f"{name}: expected [C] or [B, C] weights with C contiguous")
+            # one sample's weights serve all its rows whatever their stride
+            if len(st) == 2 and B > 1:
+                stride = st[0]
+                if stride < C:
+                    raise ValueError(f"{name}: the samples' weights overlap")
+        elif t.shape != first.shape or t.dtype != wdtype or t.stride() != st:
             raise ValueError("weights and bias (and their gradients) must share shape, strides and dtype")
-        # one sample's weights serve all its rows whatever their stride
-        stride, wdtype = (t.stride(0) if t.dim() == 2 and B > 1 else 0), t.dtype
-        if t.dim() == 2 and B > 1 and stride < C:
-            raise ValueError(f"{name}: the samples' weights overlap")
     return Rows(B, H, N, C), NormDesc(NORM_KINDS[kind], DTYPES[wdtype], int(plus_one), 0, stride, float(eps))
 
 
@@ -241,11 +259,9 @@ def da2_norm(X, Y, w=None, b=None, kind="layer", eps=1e-6, plus_one=False, stats
     sample. ``stats``: float32 [B, H, N, 2] for da2_norm_bwd. Y may be X."""
     x = _rows("X", X)
     y = _rows("Y", Y, X.shape, X.dtype)
-    r, n = _norm_desc(X, w, b, kind, eps, plus_one)
+    r, n = _norm_desc(X, (("w", w), ("b", b)), kind, eps, plus_one)
     st = _plain("stats", stats, X.shape[:3] + (2,), torch.float32)
-    s, dev = _on(stream, X, Y, w, b, stats)
-    with dev:
-        check("da2_norm", lib().da2_norm(X.data_ptr(), x, r, n, _addr(w), _addr(b), Y.data_ptr(), y, st, s))
+    _run("da2_norm", stream, (X, Y, w, b, stats), X.data_ptr(), x, r, n, _addr(w), _addr(b), Y.data_ptr(), y, st)
     return Y
 
 
@@ -264,16 +280,13 @@ def da2_norm_bwd(dY, X, stats, dX=None, w=None, dw=None, db=None, kind="layer", 
     x = _rows("X", X)
     dy = _rows("dY", dY, X.shape, X.dtype)
     dx = None if dX is None else _rows("dX", dX, X.shape, X.dtype)
-    given = [t for t in (w, dw, db) if t is not None]
-    r, n = _norm_desc(X, given[0] if given else None, given[-1] if given else None, kind, 0.0, plus_one)
-    if len(given) == 3:
-        _norm_desc(X, w, dw, kind, 0.0, plus_one)
+    r, n = _norm_desc(X, (("w", w), ("dw", dw), ("db", db)), kind, 0.0, plus_one)
     st = _plain("stats", stats, X.shape[:3] + (2,), torch.float32)
-    s, dev = _on(stream, X, dY, stats, dX, w, dw, db, ws)
-    with dev:
-        check("da2_norm_bwd", lib().da2_norm_bwd(
-            dY.data_ptr(), dy, X.data_ptr(), x, r, n, _addr(w), st, _addr(dX), dx, _addr(dw), _addr(db), _addr(ws),
-            0 if ws is None else ws.numel() * ws.element_size(), s))
+    _run("da2_norm_bwd", stream, (X, dY, stats, dX, w, dw, db, ws), dY.data_ptr(), dy, X.data_ptr(), x, r, n, _addr(w),
+         st, _addr(dX), dx, _addr(dw), _addr(db), _addr(ws), _bytes(ws))
+
+
+_I32x3 = ctypes.c_int32 * 3
 
 
 @dataclass
@@ -291,7 +304,7 @@ class Rope:
         n = len(self.rot_axis)
         if not 1 <= n <= 3:
             raise ValueError("rot_axis: expected 1 to 3 axes")
-        return RopeDesc(ROPE_LAYOUTS[self.layout], self.block, n, (ctypes.c_int32 * 3)(*self.rot_axis))
+        return RopeDesc(ROPE_LAYOUTS[self.layout], self.block, n, _I32x3(*self.rot_axis))
 
 
 def da2_rope_plan(block, rot_axis, layout="interleaved", base=10000.0, scaling="none", factor=1.0, orig_len=4096,
@@ -322,18 +335,15 @@ def da2_rope(rope, Q, Qo, K=None, Ko=None, pos=None, grid=None, inverse=False, s
         ko = _rows("Ko", Ko, K.shape, Q.dtype)
     axes, stride = len(rope.rot_axis), 0
     if pos is not None:
-        if tuple(pos.shape) not in ((B, N, axes), (1, N, axes)) or pos.dtype != torch.int32:
+        if pos.shape not in ((B, N, axes), (1, N, axes)) or pos.dtype != torch.int32:
             raise ValueError(f"pos: expected int32 [{B} or 1, {N}, {axes}]")
         if not pos[0].is_contiguous():
             raise ValueError("pos: expected each sample's positions contiguous")
         stride = pos.stride(0) if pos.shape[0] > 1 else 0
     t = _plain("turns", rope.turns, (sum(rope.rot_axis) // 2,), torch.float64)
     gh, gw = grid if grid is not None else (0, 0)
-    s, dev = _on(stream, Q, Qo, K, Ko, pos, rope.turns)
-    with dev:
-        check("da2_rope", lib().da2_rope(
-            rope.desc(), t, rope.scale, _addr(pos), stride, RopeRows(B, Hq, Hk, N, d, gh, gw, int(inverse)),
-            Q.data_ptr(), q, Qo.data_ptr(), qo, _addr(K), k, _addr(Ko), ko, s))
+    _run("da2_rope", stream, (Q, Qo, K, Ko, pos, rope.turns), rope.desc(), t, rope.scale, _addr(pos), stride,
+         RopeRows(B, Hq, Hk, N, d, gh, gw, int(inverse)), Q.data_ptr(), q, Qo.data_ptr(), qo, _addr(K), k, _addr(Ko), ko)
 
 
 def _diff_problem(Q, K, causal=False, scale=None):
@@ -344,10 +354,6 @@ def _diff_problem(Q, K, causal=False, scale=None):
     if K.shape[0] != B or K.shape[3] != d or Hk == 0 or Hq % Hk:
         raise ValueError(f"Q {tuple(Q.shape)} and K {tuple(K.shape)} do not belong together")
     return DiffProblem(B, Hq, Hk, N, M, d, int(causal), 0, (d / 2) ** -0.5 if scale is None else float(scale))
-
-
-def _bytes(ws):
-    return 0 if ws is None else ws.numel() * ws.element_size()
 
 
 def da2_diff_ws_bytes(Q, K, train=False):
@@ -376,11 +382,8 @@ def da2_diff_attn(Q, K, V, lam, O, ws=None, lse=None, kv_lens=None, q_start=None
     p, q, k, v, (l, kl, qs) = _diff_inputs(Q, K, V, lam, kv_lens, q_start, causal, scale)
     o = _rows("O", O, Q.shape, Q.dtype)
     ls = _plain("lse", lse, (p.B, p.Hq, 2, p.N), torch.float32)
-    s, dev = _on(stream, Q, K, V, lam, O, ws, lse, kv_lens, q_start)
-    with dev:
-        check("da2_diff_attn", lib().da2_diff_attn(
-            p, Q.data_ptr(), q, K.data_ptr(), k, V.data_ptr(), v, l, kl, qs, O.data_ptr(), o, ls, _addr(ws),
-            _bytes(ws), s))
+    _run("da2_diff_attn", stream, (Q, K, V, lam, O, ws, lse, kv_lens, q_start), p, Q.data_ptr(), q, K.data_ptr(), k,
+         V.data_ptr(), v, l, kl, qs, O.data_ptr(), o, ls, _addr(ws), _bytes(ws))
     return O
 
 
@@ -392,8 +395,6 @@ def da2_diff_attn_bwd(Q, K, V, lam, lse, dO, dQ, dK, dV, dlam, ws, kv_lens=None,
     dk, dv = (_rows(n, t, K.shape, Q.dtype) for n, t in (("dK", dK), ("dV", dV)))
     ls = _plain("lse", lse, (p.B, p.Hq, 2, p.N), torch.float32)
     dl = _plain("dlam", dlam, (p.Hq,), torch.float32)
-    s, dev = _on(stream, Q, K, V, lam, lse, dO, dQ, dK, dV, dlam, ws, kv_lens, q_start)
-    with dev:
-        check("da2_diff_attn_bwd", lib().da2_diff_attn_bwd(
-            p, Q.data_ptr(), q, K.data_ptr(), k, V.data_ptr(), v, l, kl, qs, ls, dO.data_ptr(), do, dQ.data_ptr(), dq,
-            dK.data_ptr(), dk, dV.data_ptr(), dv, dl, _addr(ws), _bytes(ws), s))
+    _run("da2_diff_attn_bwd", stream, (Q, K, V, lam, lse, dO, dQ, dK, dV, dlam, ws, kv_lens, q_start), p, Q.data_ptr(), q,
+         K.data_ptr(), k, V.data_ptr(), v, l, kl, qs, ls, dO.data_ptr(), do, dQ.data_ptr(), dq, dK.data_ptr(), dk,
+         dV.data_ptr(), dv, dl, _addr(ws), _bytes(ws))
