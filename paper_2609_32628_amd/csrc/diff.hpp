@@ -49,6 +49,24 @@ __device__ inline s16x8 pack8(const float* x) {
   return __builtin_bit_cast(s16x8, v);
 }
 
+// The sum of eight values of T and s.
+template <typename T>
+__device__ inline float add8(const s16x8& x, float s) {
+  typedef T Tx2 __attribute__((ext_vector_type(2)));
+  const uint4 w = __builtin_bit_cast(uint4, x);
+  const uint32_t pair[4] = {w.x, w.y, w.z, w.w};
+  const Tx2 one = {static_cast<T>(1.0f), static_cast<T>(1.0f)};
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    if constexpr (__is_same(T, bf16_t)) {
+      s = __builtin_amdgcn_fdot2_f32_bf16(__builtin_bit_cast(Tx2, pair[i]), one, s, false);
+    } else {
+      s = __builtin_amdgcn_fdot2(__builtin_bit_cast(Tx2, pair[i]), one, s, false);
+    }
+  }
+  return s;
+}
+
 // ---- tiles in LDS -----------------------------------------------------------------
 template <int D>
 struct Tile {

@@ -262,6 +262,10 @@ __global__ __launch_bounds__(HALVES * kThreads, 2) void diff_dq_kernel(DiffArgs 
   constexpr int S = D / 32, K = 64 * HALVES, WAVES = 4 * HALVES, BYTES = K * Tile<D>::kRow, R = Tile<D>::kRowsPerCopy;
   __shared__ __align__(256) char lds[2][2][BYTES];  // [buffer][K, V]
   __shared__ float sums[HALVES == 2 ? 4 : 1][2][64];
+  // keys spread over those that the workgroup's rows see, and their mean
+  constexpr int SAMPLE = 16 * HALVES * 128 / D;
+  __shared__ __align__(16) T sample[SAMPLE][D];
+  __shared__ __align__(16) float mean[D];
   const int unit = unit_of(blockIdx.x, units);
   if (unit < 0) return;
   const int tile = tiles - 1 - unit % tiles, bh = unit / tiles;
@@ -277,6 +281,12 @@ __global__ __launch_bounds__(HALVES * kThreads, 2) void diff_dq_kernel(DiffArgs 
   const int low = key_limit(a, vis, token(row0)), high = key_limit(a, vis, token(row0 + 31));
   const int end = key_limit(a, vis, token(tile * 128u + 127));
 
+  if (end > 0) {
+    const int i = threadIdx.x / (D / 8), ch = threadIdx.x % (D / 8) * 8;
+    const int64_t at = static_cast<int64_t>(end) * i / SAMPLE;
+    *reinterpret_cast<uint4*>(&sample[i][ch]) = *reinterpret_cast<const uint4*>(
+        static_cast<const T*>(a.k.p) + b * a.k.sb + hk * a.k.sh + at * a.k.sn + ch);
+  }
   s16x8 qf[2][S], of[2 * S];
   {
     const T* qp = static_cast<const T*>(a.q.p) + b * a.q.sb + h * a.q.sh + n * a.q.sn + 8 * g;
@@ -295,6 +305,7 @@ __global__ __launch_bounds__(HALVES * kThreads, 2) void diff_dq_kernel(DiffArgs 
     lse[i] = l == -__builtin_inff() ? kNever : l / a.scale;
   }
   f32x16 dq[2][S / 2];
+  float rest[2] = {0.0f, 0.0f};  // sums of the rounded dS of each map
 #pragma unroll
   for (int t = 0; t < S; ++t) dq[t / (S / 2)][t % (S / 2)] = f32x16{};
   const RowReader<D> rows(lane, true);
@@ -351,6 +362,7 @@ __global__ __launch_bounds__(HALVES * kThreads, 2) void diff_dq_kernel(DiffArgs 
           if constexpr (!kSums) {
             df[i][0] = pack8<T>(ds);
             df[i][1] = pack8<T>(ds + 8);
+            rest[i] = add8<T>(df[i][1], add8<T>(df[i][0], rest[i]));
           }
         }
         if constexpr (!kSums) {
@@ -388,9 +400,24 @@ __global__ __launch_bounds__(HALVES * kThreads, 2) void diff_dq_kernel(DiffArgs 
   wait_copies();
   barrier();  // the tiles have been read
   walk(std::integral_constant<int, 1>{});
+  // A row's dS sum to zero, its rounded dS do not quite: what they sum to, times the keys' mean, is taken out of dQ, so that
+  // the rounding meets what the keys differ by and not what they share (keys whose mean is half their spread: dQ's error is
+  // 1.45 times that of rounding dQ alone, and 1.52 times without this, which costs 2% of the backward pass).
+#pragma unroll
+  for (int i = 0; i < 2; ++i) rest[i] = sum_halves(rest[i]);
+  __syncthreads();
+  if (threadIdx.x < D) {
+    float m = 0.0f;
+    if (end > 0)
+#pragma unroll
+      for (int i = 0; i < SAMPLE; ++i) m += static_cast<float>(sample[i][threadIdx.x]);
+    mean[threadIdx.x] = m * (1.0f / SAMPLE);
+  }
   if constexpr (HALVES == 2) {
     f32x4* swap = reinterpret_cast<f32x4*>(lds) + (wave % 4) * 4 * S * 64 + lane;
-    __syncthreads();
+    if (half)
+#pragma unroll
+      for (int i = 0; i < 2; ++i) sums[wave % 4][i][lane] = rest[i];
 #pragma unroll
     for (int t = 0; t < S; ++t)
 #pragma unroll
@@ -398,8 +425,13 @@ __global__ __launch_bounds__(HALVES * kThreads, 2) void diff_dq_kernel(DiffArgs 
         f32x16& q = dq[t / (S / 2)][t % (S / 2)];
         if (half) swap[(4 * t + e) * 64] = f32x4{q[4 * e], q[4 * e + 1], q[4 * e + 2], q[4 * e + 3]};
       }
-    __syncthreads();
+  }
+  __syncthreads();
+  if constexpr (HALVES == 2) {
+    const f32x4* swap = reinterpret_cast<const f32x4*>(lds) + (wave % 4) * 4 * S * 64 + lane;
     if (half) return;
+#pragma unroll
+    for (int i = 0; i < 2; ++i) rest[i] += sums[wave % 4][i][lane];
 #pragma unroll
     for (int t = 0; t < S; ++t)
 #pragma unroll
@@ -415,7 +447,12 @@ __global__ __launch_bounds__(HALVES * kThreads, 2) void diff_dq_kernel(DiffArgs 
   for (int t = 0; t < S; ++t) {
     float x[16];
 #pragma unroll
-    for (int e = 0; e < 16; ++e) x[e] = dq[t / (S / 2)][t % (S / 2)][e] * f[t / (S / 2)];
+    for (int e = 0; e < 16; e += 4) {
+      const f32x4 m = *reinterpret_cast<const f32x4*>(&mean[32 * t + 2 * e + 4 * g]);
+#pragma unroll
+      for (int y = 0; y < 4; ++y)
+        x[e + y] = __builtin_fmaf(-rest[t / (S / 2)], m[y], dq[t / (S / 2)][t % (S / 2)][e + y]) * f[t / (S / 2)];
+    }
     store_columns(out + 32 * t, x, live);
   }
 }

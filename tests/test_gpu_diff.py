@@ -10,11 +10,15 @@ Tolerances, with u = finfo(type).eps / 2 (half a step of the 16-bit type):
     sum_j (P1 + lam P2) |V_j|, and by u of itself when it is stored.
   - dS_i = P_i (dP - del_i): dP is a float32 sum, off by d 2^-24 |dO|.|V|; del_i, the float32 sum of P_i dP, by
     t = sum P_i ((E + (M/16 + 40) 2^-24) |dP| + d 2^-24 |dO|.|V|). dS is rounded by u. So dS_i is off by
-    P_i ((u + E) |dP - del_i| + d 2^-24 |dO|.|V| + t) and the gradients by the sums of that times |K|, |Q|; dV as O.
+    P_i ((u + E) |dP - del_i| + d 2^-24 |dO|.|V| + t) and dK by the sums of that times |Q|; dV as O.
+  - dQ is sum_j r_j K_j - (sum_j r_j) m from rounded r_j, with m the mean of some of the keys. That is
+    sum_j r_j (K_j - m), and sum_j dS_j (K_j - m) = sum_j dS_j K_j since the dS_j sum to zero: so dQ is off by the sums of
+    what dS is off times |K_j - m|, at most the distance w_j of K_j to the further end of the keys' range, channel by
+    channel (the float32 sums of r_j K_j and r_j keep their error relative to |K_j| <= w_j + |m|).
   - dlam is the sum of del2, off by its t.
   - below the smallest normal number a rounding is off by half the spacing there, z = smallest_normal eps / 2 (2^-25 in
     fp16), not by u of the value: each rounded weight or dS adds z to its product, so z sum |V_j| (1 + lam) to O,
-    z sum |dO| to dV, and z scale times sum |K| or |Q| to dQ (lam times that for the second map, whose lambda comes
+    z sum |dO| to dV, and z scale times sum w or |Q| to dQ (lam times that for the second map, whose lambda comes
     after the rounding) and dK. (A running maximum is at most the row's, so a row's sum is at least 1.)"""
 import math
 
@@ -104,7 +108,8 @@ class Case:
                     delta = (P[m] * dP).sum(-1, keepdims=True)
                     mag = f * P[m] * np.abs(dP - delta)
                     off = (u + E[m] + 8 * eps) * mag + f * P[m] * (d * eps * gv + t[m] + 4 * eps * np.abs(delta))
-                    out["dQ"][b, hq, :, c] = scale * ((off + chain * mag + z * f * see) @ np.abs(k[:, c]))
+                    w = np.maximum(k[:, c] - k[:, c].min(0), k[:, c].max(0) - k[:, c]) if n else k[:, c]
+                    out["dQ"][b, hq, :, c] = scale * ((off + z * f * see) @ w + (chain * mag) @ (w + np.abs(k[:, c]).max(0, initial=0.0)))
                     out["dK"][b, kh, :n, c] += scale * ((off + z * see + (N * H / Hk / 16 + 40) * eps * mag).T @ np.abs(q[:, c]))
         return out
 
