@@ -19,7 +19,6 @@ namespace da2 {
 namespace {
 
 constexpr int kThreads = 256;
-constexpr int DEEP = 4;
 
 // n elements (16 bytes, or one) at p as floats, and back.
 template <typename T, int V>
@@ -107,44 +106,32 @@ __global__ __launch_bounds__(kThreads) void rope_kernel(RopeArgs a, int units, i
   }
   float c[P], s[P];
   if (!moves) angles<P>(a, b, n, pair, c, s);
-  // The heads' blocks of channels, several in flight (in place too: a thread's chunks are its own).
-  const int blocks = a.d / a.block, h0 = blockIdx.y * heads, h1 = min(h0 + heads, a.Hq + a.Hk);
-  const auto row = [&](int h, const T*& x, T*& y) {
-    const bool is_q = h < a.Hq;
-    const View& in = is_q ? a.q : a.k;
-    const OutView& out = is_q ? a.qo : a.ko;
-    const int hh = is_q ? h : h - a.Hq;
-    x = static_cast<const T*>(in.p) + b * in.sb + hh * in.sh + n * in.sn;
-    y = static_cast<T*>(out.p) + b * out.sb + hh * out.sh + n * out.sn;
-  };
+  const int blocks = a.d / a.block, h1 = min(static_cast<int>(blockIdx.y + 1) * heads, a.Hq + a.Hk);
   constexpr bool PAIR = HALF || V == 1;  // the pairs' second halves are a chunk of their own
   for (int k = 0; k < blocks; ++k) {
-    for (int h = h0; h < h1; h += DEEP) {
-      float v[DEEP][V], w[DEEP][V];
-      T* y[DEEP];
+    for (int h = blockIdx.y * heads; h < h1; ++h) {
+      const bool is_q = h < a.Hq;
+      if (moves && (is_q ? a.q_in_place : a.k_in_place)) continue;
+      const View& in = is_q ? a.q : a.k;
+      const OutView& out = is_q ? a.qo : a.ko;
+      const int hh = is_q ? h : h - a.Hq;
+      const T* x = static_cast<const T*>(in.p) + b * in.sb + hh * in.sh + n * in.sn + k * a.block;
+      T* y = static_cast<T*>(out.p) + b * out.sb + hh * out.sh + n * out.sn + k * a.block;
+      float v[V], w[V];
+      get<T, V>(x + i, v);
+      if (!moves) {
+        if constexpr (PAIR) {
+          get<T, V>(x + j, w);
 #pragma unroll
-      for (int q = 0; q < DEEP; ++q) {
-        const T* x;
-        row(min(h + q, h1 - 1), x, y[q]);
-        get<T, V>(x + k * a.block + i, v[q]);
-        if (PAIR && !moves) get<T, V>(x + k * a.block + j, w[q]);
-      }
+          for (int e = 0; e < V; ++e) turn(v[e], w[e], c[e], s[e]);
+          put<T, V>(y + j, w);
+        } else {
 #pragma unroll
-      for (int q = 0; q < DEEP; ++q) {
-        if (h + q >= h1 || (moves && (h + q < a.Hq ? a.q_in_place : a.k_in_place))) continue;
-        if (!moves) {
-          if constexpr (PAIR) {
-#pragma unroll
-            for (int e = 0; e < V; ++e) turn(v[q][e], w[q][e], c[e], s[e]);
-            put<T, V>(y[q] + k * a.block + j, w[q]);
-          } else {
-#pragma unroll
-            for (int e = 0; e < P; ++e)
-              if (2 * (pair + e) < a.rot) turn(v[q][2 * e], v[q][2 * e + 1], c[e], s[e]);
-          }
+          for (int e = 0; e < P; ++e)
+            if (2 * (pair + e) < a.rot) turn(v[2 * e], v[2 * e + 1], c[e], s[e]);
         }
-        put<T, V>(y[q] + k * a.block + i, v[q]);
       }
+      put<T, V>(y + i, v);
     }
   }
 }
@@ -162,9 +149,10 @@ hipError_t launch(const RopeArgs& a, hipStream_t stream) {
   }
   const int all = a.Hq + a.Hk;
   const int64_t threads = static_cast<int64_t>(a.B) * a.N * units;
-  // a thread keeps its angles for as many heads as leave the card 2^18 threads (a
-  // wave for each slot of 256 CUs x 16)
-  int64_t heads = threads * all >> 18;
+  // A thread keeps its angles for as many heads as leave the card 2^20 threads, four rounds of its 256 CUs x 16 waves (24
+  // heads of 32,760 tokens: 83 us with a quarter of that, 82 with 2^20 or twice that; 40 heads of 8,000 tokens: 31, 29
+  // and 38).
+  int64_t heads = threads * all >> 20;
   heads = heads < 1 ? 1 : heads > all ? all : heads;
   const int64_t chunks = (all + heads - 1) / heads;
   const int64_t blocks = (threads + kThreads - 1) / kThreads;
