@@ -39,10 +39,12 @@ Cut cut_of(int B, int Hq, int Hk, int N, int M) {
   c.few = rows <= 64;
   c.tiles = static_cast<int>(c.few ? (rows + 31) / 32 : (rows + 127) / 128);
   const int64_t units = static_cast<int64_t>(B) * Hk * c.tiles;
-  // One workgroup a CU (two of few rows), and parts that take longer to walk than to join: 128 keys take a workgroup of
-  // 128 rows 2.5 us, and a launch and the parts' way through memory 5 us and more (32 tiles against 2,000 keys: 47 us
-  // whole, 34 in three parts; 64 against 1,024: 28, and 31 in two).
-  int64_t s = (c.few ? 512 : 256) / units, most = c.few ? (M + 255) / 256 : units > 32 ? (M + 512) / 1024 : M / 512;
+  // One workgroup a CU, which is what LDS holds of few rows, and parts that take longer to walk than to join. Few rows (one
+  // sample of 32,768 keys, 8 key heads: 41 us with half as many workgroups, 44 with one a CU, 64 with two; 8 samples of
+  // 8,192, 12 heads: 113, 74 and 80): 256 keys. Many rows: 128 keys take a workgroup of 128 rows 2.5 us, and a launch and
+  // the parts' way through memory 5 us and more (32 tiles against 2,000 keys: 47 us whole, 34 in three parts; 64 against
+  // 1,024: 28, and 31 in two).
+  int64_t s = 256 / units, most = c.few ? (M + 255) / 256 : units > 32 ? (M + 512) / 1024 : M / 512;
   s = s < most ? s : most;
   c.splits = static_cast<int>(s < 1 ? 1 : s);
   return c;
