@@ -191,6 +191,17 @@ __device__ inline float sum_halves(float v) {
   return __uint_as_float(r[0]) + __uint_as_float(r[1]);
 }
 
+__device__ inline float wave_max_f32(float v) {
+#pragma unroll
+  for (int o = 32; o > 0; o >>= 1) v = fmaxf(v, __shfl_xor(v, o, 64));
+  return v;
+}
+__device__ inline float wave_sum_f32(float v) {
+#pragma unroll
+  for (int o = 32; o > 0; o >>= 1) v += __shfl_xor(v, o, 64);
+  return v;
+}
+
 // Stores rows given as accumulator columns: lane%32 is the row (its address `row`), x[i] of lane half g is channel
 // 8 (i/4) + 4 g + i%4 of 32. The halves trade quads, so that each lane stores 16 bytes.
 template <typename T>

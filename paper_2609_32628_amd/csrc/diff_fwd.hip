@@ -433,29 +433,58 @@ __global__ __launch_bounds__(kThreads, 1) void diff_few_kernel(DiffArgs a, int t
   }
 }
 
-// The parts of each row joined: D threads a row.
+// The parts of a row joined, a workgroup a row: the parts' factors from their statistics, a part a thread; then D/2
+// threads (4 channels of a map each) add up every WAYS-th part, and their sums are added in order.
+constexpr int kMostParts = 256;  // as cut_of gives them
 template <typename T, int D>
-__global__ __launch_bounds__(kThreads) void diff_join_kernel(DiffArgs a, int splits, uint32_t rows_all) {
-  const uint32_t r = blockIdx.x * (kThreads / D) + threadIdx.x / D;
-  if (r >= rows_all) return;
-  const int ch = threadIdx.x % D, G = a.Hq / a.Hk;
+__global__ __launch_bounds__(kThreads) void diff_join_kernel(DiffArgs a, int splits) {
+  constexpr int TPP = D / 2, WAYS = kThreads / TPP;
+  __shared__ float factor[2][kMostParts], wave_max[2][4], wave_sum[2][4];
+  __shared__ __align__(16) f32x4 sums[WAYS][TPP];
+  const uint32_t r = blockIdx.x;
+  const int G = a.Hq / a.Hk, tid = threadIdx.x, lane = tid % 64, wave = tid / 64;
   const uint32_t rows = static_cast<uint32_t>(a.N) * G, bh = r / rows, row = r - bh * rows;
-  const int b = bh / a.Hk, n = row / G;
-  const int h = bh % a.Hk * G + row % G;
+  const int b = bh / a.Hk, n = row / G, h = bh % a.Hk * G + row % G;
   const float* part = a.ws + static_cast<int64_t>(r) * splits * kPart<D>;
-  float m[2] = {kNoMax, kNoMax}, l[2] = {0.0f, 0.0f}, u[2] = {0.0f, 0.0f};
-  for (int s = 0; s < splits; ++s)
+  const bool mine = tid < splits;
+  f32x4 st = {kNoMax, 0.0f, kNoMax, 0.0f};
+  if (mine) st = *reinterpret_cast<const f32x4*>(part + tid * kPart<D> + 2 * D);
+  float m[2], l[2];
 #pragma unroll
-    for (int i = 0; i < 2; ++i) m[i] = fmaxf(m[i], part[s * kPart<D> + 2 * D + 2 * i]);
-  for (int s = 0; s < splits; ++s, part += kPart<D>)
+  for (int i = 0; i < 2; ++i) {
+    const float t = wave_max_f32(st[2 * i]);
+    if (lane == 0) wave_max[i][wave] = t;
+  }
+  __syncthreads();
 #pragma unroll
-    for (int i = 0; i < 2; ++i) {
-      const float f = exp2_fast(part[2 * D + 2 * i] - m[i]);
-      l[i] += f * part[2 * D + 2 * i + 1];
-      u[i] += f * part[i * D + ch];
+  for (int i = 0; i < 2; ++i) {
+    m[i] = fmaxf(fmaxf(wave_max[i][0], wave_max[i][1]), fmaxf(wave_max[i][2], wave_max[i][3]));
+    const float f = exp2_fast(st[2 * i] - m[i]);
+    if (mine) factor[i][tid] = f;
+    const float t = wave_sum_f32(mine ? f * st[2 * i + 1] : 0.0f);
+    if (lane == 0) wave_sum[i][wave] = t;
+  }
+  __syncthreads();
+#pragma unroll
+  for (int i = 0; i < 2; ++i) l[i] = (wave_sum[i][0] + wave_sum[i][1]) + (wave_sum[i][2] + wave_sum[i][3]);
+  const int at = tid % TPP, way = tid / TPP, map = at / (D / 4);
+  f32x4 u{};
+#pragma unroll 4
+  for (int s = way; s < splits; s += WAYS)
+    u += factor[map][s] * *reinterpret_cast<const f32x4*>(part + static_cast<int64_t>(s) * kPart<D> + 4 * at);
+  sums[way][at] = u;
+  __syncthreads();
+  if (tid < D / 4) {
+    f32x4 u1 = sums[0][tid], u2 = sums[0][D / 4 + tid];
+#pragma unroll
+    for (int w = 1; w < WAYS; ++w) {
+      u1 += sums[w][tid];
+      u2 += sums[w][D / 4 + tid];
     }
-  finish_element<T>(a, b, h, n, ch, u[0], u[1], l[0], l[1]);
-  if (a.lse && ch < 2) store_lse(a, b, h, n, ch, ch ? m[1] : m[0], ch ? l[1] : l[0]);
+#pragma unroll
+    for (int i = 0; i < 4; ++i) finish_element<T>(a, b, h, n, 4 * tid + i, u1[i], u2[i], l[0], l[1]);
+  }
+  if (a.lse && tid < 2) store_lse(a, b, h, n, tid, tid ? m[1] : m[0], tid ? l[1] : l[0]);
 }
 
 template <typename T, int D>
@@ -478,8 +507,7 @@ hipError_t launch(const DiffArgs& a, hipStream_t stream) {
     const int blocks = units / c.splits * 4;
     diff_many_join_kernel<T, D><<<(blocks * (D / 32) + 3) / 4, kThreads, 0, stream>>>(a, c.tiles, c.splits, blocks);
   } else if (c.splits > 1) {
-    const uint32_t rows = static_cast<uint32_t>(a.B) * a.Hq * a.N;  // at most 512 tiles of 32
-    diff_join_kernel<T, D><<<(rows + kThreads / D - 1) / (kThreads / D), kThreads, 0, stream>>>(a, c.splits, rows);
+    diff_join_kernel<T, D><<<static_cast<unsigned>(a.B) * a.Hq * a.N, kThreads, 0, stream>>>(a, c.splits);  // at most 256 tiles of 32 rows
   }
   return hipGetLastError();
 }
