@@ -19,6 +19,7 @@
 // the order of workgroups and nothing has to be cleared. In multiply-adds of d
 // per pair: 2 for del, 3 for dQ, 4 for dK and dV, where one pass over both sides
 // (which would need sums in memory) takes 5 beside del.
+#include <algorithm>
 #include <type_traits>
 
 #include "diff.hpp"
@@ -67,18 +68,19 @@ __device__ inline f32x16 read16(const float* p) {
   return x;
 }
 
-// dlambda of a head: minus the sum of its rows' del2, in float64 and in a fixed order. 256 threads.
+// dlambda of a head: minus the sum of its rows' del2, in float64 and in a fixed order.
+template <int THREADS>
 __device__ inline void sum_dlam(const DiffArgs& a, float* stat, int h, double* sums) {
   double t = 0.0;
   for (int b = 0; b < a.B; ++b)
 #pragma unroll 4
-    for (int n = threadIdx.x; n < a.N; n += kThreads) {
+    for (int n = threadIdx.x; n < a.N; n += THREADS) {
       const float* s = stat_at(stat, static_cast<int64_t>(b) * a.Hq + h, n, a.N);
       t += -static_cast<double>(s[128]) - s[192] * minus_sign(a.lam[h]);
     }
   sums[threadIdx.x] = t;
   __syncthreads();
-  for (int o = kThreads / 2; o > 0; o >>= 1) {
+  for (int o = THREADS / 2; o > 0; o >>= 1) {
     if (threadIdx.x < o) sums[threadIdx.x] += sums[threadIdx.x + o];
     __syncthreads();
   }
@@ -86,16 +88,17 @@ __device__ inline void sum_dlam(const DiffArgs& a, float* stat, int h, double* s
 }
 
 // dK and dV of 128 keys: 4 waves with 32 keys each; 32 queries of one head at a time in LDS. A wave's keys are in
-// registers, its values in LDS: both in registers would leave one wave a SIMD at d = 128. The first workgroups, a
-// multiple of 8, sum dlambda beside them.
-template <typename T, int D>
-__global__ __launch_bounds__(kThreads, 2) void diff_dkv_kernel(DiffArgs a, float* stat, float* sums, int tiles, int parts, int units, int lambdas) {
+// registers, its values in LDS: both in registers would leave one wave a SIMD at d = 128. HALVES = 2: twice the waves,
+// the second four with the same keys and every other tile of queries. The first workgroups, a multiple of 8, sum dlambda
+// beside them.
+template <typename T, int D, int HALVES>
+__global__ __launch_bounds__(HALVES * kThreads, 2) void diff_dkv_kernel(DiffArgs a, float* stat, float* sums, int tiles, int parts, int units, int lambdas) {
   constexpr int S = D / 32, Q = 32, BYTES = Q * Tile<D>::kRow, R = Tile<D>::kRowsPerCopy;
-  __shared__ __align__(256) char lds[2][2][BYTES];  // [buffer][Q, dO]
-  __shared__ __align__(256) char val[4 * BYTES];    // the workgroup's rows of V
-  __shared__ __align__(16) float st[2][4][Q];
+  __shared__ __align__(256) char lds[2][HALVES][2][BYTES];  // [buffer][half][Q, dO]
+  __shared__ __align__(256) char val[4 * BYTES];            // the workgroup's rows of V
+  __shared__ __align__(16) float st[2][HALVES][4][Q];
   if (static_cast<int>(blockIdx.x) < lambdas) {
-    if (static_cast<int>(blockIdx.x) < a.Hq) sum_dlam(a, stat, blockIdx.x, reinterpret_cast<double*>(lds));
+    if (static_cast<int>(blockIdx.x) < a.Hq) sum_dlam<HALVES * kThreads>(a, stat, blockIdx.x, reinterpret_cast<double*>(lds));
     return;
   }
   const int unit = unit_of(blockIdx.x - lambdas, units);
@@ -103,7 +106,8 @@ __global__ __launch_bounds__(kThreads, 2) void diff_dkv_kernel(DiffArgs a, float
   // the first keys are seen by most queries under a causal mask: they go first
   const int part = unit % parts, tile = unit / parts % tiles, bh = unit / parts / tiles;
   const int b = bh / a.Hk, hk = bh % a.Hk, G = a.Hq / a.Hk;
-  const int lane = threadIdx.x % 64, g = lane / 32, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64);
+  const int lane = threadIdx.x % 64, g = lane / 32, half = __builtin_amdgcn_readfirstlane(threadIdx.x / kThreads);
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64) % 4;
   const Visible vis = visible(a, b);
   const int key0 = tile * 128 + 32 * wave, key = key0 + lane % 32;
 
@@ -128,7 +132,7 @@ __global__ __launch_bounds__(kThreads, 2) void diff_dkv_kernel(DiffArgs a, float
     }
     const T* vp = static_cast<const T*>(a.v.p) + b * a.v.sb + hk * a.v.sh + static_cast<int64_t>(tile) * 128 * a.v.sn;
 #pragma unroll
-    for (int i = 0; i < Q / R; ++i)  // each wave its own rows
+    for (int i = half; i < Q / R; i += HALVES)  // each wave its own rows
       copy_rows<D>(vp, 2 * a.v.sn, Q * wave + i * R, vis.len - 1 - tile * 128, lane, lds_offset(val) + wave * BYTES + i * 1024);
     const uint32_t vt = lds_offset(val) + wave * BYTES;
     const RowReader<D> rows(lane, true), keys(lane, false);
@@ -141,35 +145,36 @@ __global__ __launch_bounds__(kThreads, 2) void diff_dkv_kernel(DiffArgs a, float
       // 2 Q / R copies of 1 KB: each wave takes its share of Q's and of dO's rows
 #pragma unroll
       for (int i = wave; i < Q / R; i += 4) {
-        copy_rows<D>(qp, 2 * a.q.sn, i * R, a.N - 1 - n0, lane, lds_offset(lds[buf][0]) + i * 1024);
-        copy_rows<D>(op, 2 * a.dout.sn, i * R, a.N - 1 - n0, lane, lds_offset(lds[buf][1]) + i * 1024);
+        copy_rows<D>(qp, 2 * a.q.sn, i * R, a.N - 1 - n0, lane, lds_offset(lds[buf][half][0]) + i * 1024);
+        copy_rows<D>(op, 2 * a.dout.sn, i * R, a.N - 1 - n0, lane, lds_offset(lds[buf][half][1]) + i * 1024);
       }
       if (wave == 0 && lane < Q)  // four times 32 floats
         copy_1k(stat_at(stat, static_cast<int64_t>(b) * a.Hq + h, n0, a.N), (lane / 8) * 256 + (lane % 8) * 16,
-                __builtin_amdgcn_readfirstlane(lds_offset(st[buf])));
+                __builtin_amdgcn_readfirstlane(lds_offset(st[buf][half])));
     };
-    copy(begin, 0);
-    for (int at = begin, buf = 0; at < total; ++at, buf ^= 1) {
+    if (begin + half < total) copy(begin + half, 0);
+    for (int at = begin + half, buf = 0; at - half < total; at += HALVES, buf ^= 1) {
       wait_copies();
       barrier();  // every wave's copies have arrived, and the other buffer has been read
-      if (at + 1 < total) copy(at + 1, buf ^ 1);
+      if (at + HALVES < total) copy(at + HALVES, buf ^ 1);
+      if (HALVES == 2 && at >= total) continue;  // the last tile is the first half's
       const int n = n_first + at % n_tiles * Q;
       // the wave's first key is seen by none of the 32 queries
       if (a.causal && key0 > vis.start + n + 31) continue;
       const float minus = minus_sign(load_uniform(a.lam + hk * G + at / n_tiles));
-      const uint32_t qt = lds_offset(lds[buf][0]), ot = lds_offset(lds[buf][1]);
+      const uint32_t qt = lds_offset(lds[buf][half][0]), ot = lds_offset(lds[buf][half][1]);
       // query n + 16 g + e sees the key from e = first on
       const int64_t behind = key - vis.start - n - 16 * g;
       const int first = static_cast<int>(behind < 0 ? 0 : behind < 16 ? behind : 16);
       const bool hidden = a.causal && key0 + 31 > vis.start + n;  // the wave's last key from some of the queries
-      f32x16 dp = read16(&st[buf][2][16 * g]);  // dP - del1
+      f32x16 dp = read16(&st[buf][half][2][16 * g]);  // dP - del1
 #pragma unroll
       for (int s = 0; s < 2 * S; ++s) dp = mma<T>(rows.read(ot, 0, s), keys.read(vt, 0, s), dp);
       s16x8 df[2][2];
       float w[16];
 #pragma unroll
       for (int i = 0; i < 2; ++i) {
-        f32x16 x = read16(&st[buf][i][16 * g]);
+        f32x16 x = read16(&st[buf][half][i][16 * g]);
 #pragma unroll
         for (int s = 0; s < S; ++s) x = mma<T>(rows.read(qt, 0, i * S + s), kf[i][s], x);
         if (hidden)
@@ -177,7 +182,7 @@ __global__ __launch_bounds__(kThreads, 2) void diff_dkv_kernel(DiffArgs a, float
           for (int e = 0; e < 16; ++e) x[e] = e < first ? -__builtin_inff() : x[e];
         float d[16];
         if (i) {  // (-sgn lambda) (dP - del2)
-          const f32x16 y = read16(&st[buf][3][16 * g]);
+          const f32x16 y = read16(&st[buf][half][3][16 * g]);
 #pragma unroll
           for (int e = 0; e < 16; ++e) dp[e] = __builtin_fmaf(dp[e], minus, y[e]);
         }
@@ -201,6 +206,35 @@ __global__ __launch_bounds__(kThreads, 2) void diff_dkv_kernel(DiffArgs a, float
         }
       }
     }
+  }
+  if constexpr (HALVES == 2) {
+    // the second half's sums, dV's first, go to the first half's waves in the room of the tiles
+    f32x4* swap = reinterpret_cast<f32x4*>(lds) + wave * 4 * S * 64 + lane;
+#pragma unroll
+    for (int pass = 0; pass < 2; ++pass) {
+      wait_copies();
+      __syncthreads();
+#pragma unroll
+      for (int t = 0; t < S; ++t)
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+          const f32x16& x = pass ? dk[t / (S / 2)][t % (S / 2)] : dv[t];
+          if (half) swap[(4 * t + e) * 64] = f32x4{x[4 * e], x[4 * e + 1], x[4 * e + 2], x[4 * e + 3]};
+        }
+      __syncthreads();
+#pragma unroll
+      for (int t = 0; t < S; ++t)
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+          f32x16& x = pass ? dk[t / (S / 2)][t % (S / 2)] : dv[t];
+          if (!half) {
+            const f32x4 y = swap[(4 * t + e) * 64];
+#pragma unroll
+            for (int k = 0; k < 4; ++k) x[4 * e + k] += y[k];
+          }
+        }
+    }
+    if (half) return;
   }
   // accumulator register e: key 8 (e/4) + 4 g + e%4, lane%32: channel
 #pragma unroll
@@ -459,15 +493,19 @@ __global__ __launch_bounds__(HALVES * kThreads, 2) void diff_dq_kernel(DiffArgs 
 
 int64_t stat_floats(int B, int Hq, int N) { return 4ll * B * Hq * padded(N); }
 
-// Parts of the queries that a key tile's workgroups share: as many as bring the card 512 workgroups, two a CU, and half
-// as many again under a causal mask, so that tiles that few queries see even out; of 8 query tiles at least. (128 tiles
-// of a causal step: 288 us for the backward pass in 2 parts, 212 in 4, 191 in 6, 218 in 12; 192 tiles of 1,024 queries
-// without a mask 111 in 2, 121 in 4.)
-int dkv_parts(int B, int Hq, int Hk, int N, int M, bool causal) {
+// How a key tile's queries are shared out where the tiles alone leave CUs idle: without a causal mask over two sets of
+// waves of a workgroup, then over as many workgroups as bring the card one a CU; with one, over 4-wave workgroups until
+// the card has 768, so that tiles that few queries see even out; of 8 query tiles at least. (Backward pass: 192 tiles of
+// 1,024 queries 111 us in two parts and 106 with two sets of waves; 384 without a mask 638 and 672; 128 tiles of a causal
+// step 288 us in 2 parts, 212 in 4, 191 in 6, 218 in 12, and with two sets of waves 199 at best.)
+struct Share {
+  int halves, parts;
+};
+Share dkv_share(int B, int Hq, int Hk, int N, int M, bool causal) {
   const int64_t units = static_cast<int64_t>(B) * Hk * ((M + 127ll) / 128);
-  const int64_t want = (causal ? 768 : 512) / units, most = static_cast<int64_t>(Hq / Hk) * ((N + 31) / 32) / 8;
+  const int64_t want = (causal ? 768 : 256) / units, most = static_cast<int64_t>(Hq / Hk) * ((N + 31) / 32) / 8;
   const int64_t parts = want < most ? want : most;
-  return static_cast<int>(parts < 1 ? 1 : parts);
+  return {!causal && units <= 256 ? 2 : 1, static_cast<int>(parts < 1 ? 1 : parts)};
 }
 
 template <typename T, int D>
@@ -483,12 +521,17 @@ hipError_t launch(const DiffArgs& a, hipStream_t stream) {
     diff_dq_kernel<T, D, 2><<<grid_of(row_units), 2 * kThreads, 0, stream>>>(a, stat, row_tiles, row_units);
   }
   const int key_tiles = static_cast<int>((a.M + 127ll) / 128);
-  const int parts = dkv_parts(a.B, a.Hq, a.Hk, a.N, a.M, a.causal);
+  const Share share = dkv_share(a.B, a.Hq, a.Hk, a.N, a.M, a.causal);
+  const int parts = share.parts;
   const int64_t keys = static_cast<int64_t>(a.B) * a.Hk * a.M;  // at most 768 tiles of 128 where they are joined
   const int key_units = a.B * a.Hk * key_tiles * parts;
   float* sums = stat + stat_floats(a.B, a.Hq, a.N);
   const int lambdas = static_cast<int>(grid_of(a.Hq));
-  diff_dkv_kernel<T, D><<<lambdas + grid_of(key_units), kThreads, 0, stream>>>(a, stat, sums, key_tiles, parts, key_units, lambdas);
+  if (share.halves == 1) {
+    diff_dkv_kernel<T, D, 1><<<lambdas + grid_of(key_units), kThreads, 0, stream>>>(a, stat, sums, key_tiles, parts, key_units, lambdas);
+  } else {
+    diff_dkv_kernel<T, D, 2><<<lambdas + grid_of(key_units), 2 * kThreads, 0, stream>>>(a, stat, sums, key_tiles, parts, key_units, lambdas);
+  }
   if (parts > 1)
     diff_dkv_join_kernel<T, D><<<static_cast<unsigned>((keys + 1024 / D - 1) / (1024 / D)), kThreads, 0, stream>>>(a, sums, parts, keys);
   return hipGetLastError();
@@ -497,7 +540,7 @@ hipError_t launch(const DiffArgs& a, hipStream_t stream) {
 }  // namespace
 
 int64_t diff_bwd_ws_bytes(int B, int Hq, int Hk, int N, int M, int d) {
-  const int64_t parts = dkv_parts(B, Hq, Hk, N, M, true);  // the most, whatever the mask
+  const int64_t parts = std::max(dkv_share(B, Hq, Hk, N, M, false).parts, dkv_share(B, Hq, Hk, N, M, true).parts);
   return 4 * (stat_floats(B, Hq, N) + (parts > 1 ? parts * B * Hk * M * 2 * d : 0));
 }
 
