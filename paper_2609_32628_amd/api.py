@@ -157,16 +157,24 @@ def alloc(p, scope="head", device="cuda", fmt4="nvfp4", with16=False):
                    ws_draft=raw(s["ws_draft_bytes"]), ws_rank=raw(s["ws_rank_bytes"]))
 
 
-def attention(Q, K, V, buf, lam, budgets, O, stream=None, num16=0, fmt4=None):
+def attention(Q, K, V, buf, lam, budgets, O, stream=None, num16=0, fmt4=None, qk_norm=None, rope=None):
     """The four calls in order: draft map, ranking, operand preparation,
     attention. budgets = (num8, num4, den); num16/den go to the 16-bit path;
     fmt4 ("nvfp4" or "mxfp4", default: the buffers' encoding) is the encoding
-    of the 4-bit path."""
+    of the 4-bit path. qk_norm = (w_q, w_k), weights [d] or None each: the heads
+    of Q and K are RMS-normalised first; rope, a Rope over one axis (the token
+    numbers) or three (the problem's grid): they are rotated next. Both work in
+    place, on Q and K themselves."""
     p = buf.p
     fmt4 = buf.fmt4 if fmt4 is None else fmt4
     if fmt4 != buf.fmt4 or (num16 > 0 and not buf.with16):
         raise ValueError(f"buffers sized for fmt4={buf.fmt4}, with16={buf.with16}; asked for fmt4={fmt4}, "
                          f"num16={num16}")
+    if qk_norm is not None:
+        da2_norm(Q, Q, qk_norm[0], kind="rms", stream=stream)
+        da2_norm(K, K, qk_norm[1], kind="rms", stream=stream)
+    if rope is not None:
+        da2_rope(rope, Q, Q, K, K, grid=None if len(rope.rot_axis) == 1 else (p.Hg, p.Wg), inverse=False, stream=stream)
     da2_draft_map(Q, K, buf.layout, p, lam, buf.A, buf.stats, buf.ws_draft, stream)
     da2_rank_assign(buf.A, p, num16, *budgets, buf.scope, buf.cls, buf.lists, buf.ws_rank, stream)
     da2_prep_operands(Q, K, V, buf.layout, p, int(num16 > 0), fmt4, buf.stats, buf.ops, None, stream)

@@ -192,6 +192,13 @@ def test_split_keys(B, H, Hk, N, M, d, dtype):
     assert out["O"].isfinite().all()
 
 
+@pytest.mark.parametrize("N,H,Hk,d", [(1, 8, 2, 128), (100, 2, 2, 64)])
+def test_split_keys_of_short_and_empty_samples(N, H, Hk, d):
+    """Parts that hold no key, and a sample without keys."""
+    check(Case(4, H, Hk, N, 5000, d, "bf16", True, [5000, 0, 1, 300], seed=6), grads=False)
+    check(Case(4, H, Hk, N, 5000, d, "bf16", False, [0, 0, 0, 2], seed=7), grads=False)
+
+
 def test_large_and_peaked_scores():
     """Scores far apart: the maximum moves by much more than 2^8 on the way, upwards and downwards, and a row's weight
     lies on one key."""
