@@ -364,8 +364,9 @@ __global__ __launch_bounds__(HALVES * kThreads, 2) void diff_dq_kernel(DiffArgs 
       barrier();
       if (key + K < end) copy(key + K, buf ^ 1);
       const uint32_t kt = lds_offset(lds[buf][0]), vt = lds_offset(lds[buf][1]);
-#pragma unroll 1
-      for (int j = half; j < K / 32; j += HALVES) {
+#pragma unroll
+      for (int jj = 0; jj < K / 32; jj += HALVES) {
+        const int j = jj + half;
         const int at = key + 32 * j;
         if (at >= high) continue;
         f32x16 dp{};
