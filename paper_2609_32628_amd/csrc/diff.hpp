@@ -147,6 +147,14 @@ __device__ inline void copy_rows(const void* base, int64_t row_bytes, int row, i
 __device__ inline void wait_copies() { asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)" ::: "memory"); }
 __device__ inline void barrier() { asm volatile("s_barrier" ::: "memory"); }
 
+// A workgroup's shape by how many waves share a row's keys, every SHARE-th 32 of a tile each: 4 waves with 128 rows and
+// 64-key tiles (1), 8 waves with 128 rows (2) or 64 rows (4) and 128-key tiles.
+template <int SHARE>
+struct Many {
+  static constexpr int kGroups = SHARE == 1 ? 4 : 8 / SHARE;  // of 32 rows
+  static constexpr int kRows = 32 * kGroups, kWaves = kGroups * SHARE, kKeys = SHARE == 1 ? 64 : 128;
+};
+
 // ---- which keys a query sees ------------------------------------------------------
 struct Visible {
   int len;        // valid keys of the sample

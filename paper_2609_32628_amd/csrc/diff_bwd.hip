@@ -288,24 +288,25 @@ __global__ __launch_bounds__(kThreads) void diff_dkv_join_kernel(DiffArgs a, con
   *reinterpret_cast<Tx4*>(static_cast<T*>(a.dv.p) + b * a.dv.sb + hk * a.dv.sh + kk * a.dv.sn + ch) = vo;
 }
 
-// del and dQ of 128 rows (a key head's query heads together, as in the forward pass): 4 waves with 32 rows each, or twice
-// as many where each wave's rows are shared by a second one that takes every other 32 keys (HALVES = 2). The keys go
-// through LDS twice, 64 HALVES at a time. The rows' statistics go to `stat`.
-template <typename T, int D, int HALVES>
-__global__ __launch_bounds__(HALVES * kThreads, 2) void diff_dq_kernel(DiffArgs a, float* stat, int tiles, int units) {
-  constexpr int S = D / 32, K = 64 * HALVES, WAVES = 4 * HALVES, BYTES = K * Tile<D>::kRow, R = Tile<D>::kRowsPerCopy;
+// del and dQ of 128 or 64 rows (a key head's query heads together, in workgroups as in the forward pass). The keys go
+// through LDS twice. The rows' statistics go to `stat`.
+template <typename T, int D, int SHARE>
+__global__ __launch_bounds__(64 * Many<SHARE>::kWaves, 2) void diff_dq_kernel(DiffArgs a, float* stat, int tiles, int units) {
+  constexpr int S = D / 32, K = Many<SHARE>::kKeys, WAVES = Many<SHARE>::kWaves, BYTES = K * Tile<D>::kRow, R = Tile<D>::kRowsPerCopy;
+  constexpr int GROUPS = Many<SHARE>::kGroups, ROWS = Many<SHARE>::kRows;
   __shared__ __align__(256) char lds[2][2][BYTES];  // [buffer][K, V]
-  __shared__ float sums[HALVES == 2 ? 4 : 1][2][64];
+  __shared__ float sums[SHARE][GROUPS][2][64];
   // keys spread over those that the workgroup's rows see, and their mean
-  constexpr int SAMPLE = 16 * HALVES * 128 / D;
+  constexpr int SAMPLE = 4 * WAVES * 128 / D;
   __shared__ __align__(16) T sample[SAMPLE][D];
   __shared__ __align__(16) float mean[D];
   const int unit = unit_of(blockIdx.x, units);
   if (unit < 0) return;
   const int tile = tiles - 1 - unit % tiles, bh = unit / tiles;
   const int b = bh / a.Hk, hk = bh % a.Hk, G = a.Hq / a.Hk;
-  const int lane = threadIdx.x % 64, g = lane / 32, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64), half = wave / 4;
-  const uint32_t rows_all = static_cast<uint32_t>(a.N) * G, row0 = tile * 128u + 32 * (wave % 4);
+  const int lane = threadIdx.x % 64, g = lane / 32, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64);
+  const int group = wave % GROUPS, share = wave / GROUPS;
+  const uint32_t rows_all = static_cast<uint32_t>(a.N) * G, row0 = static_cast<uint32_t>(tile) * ROWS + 32 * group;
   const auto token = [&](uint32_t r) { return static_cast<int>(min(r, rows_all - 1) / static_cast<uint32_t>(G)); };
   const bool live = row0 + lane % 32 < rows_all;
   const uint32_t row = min(row0 + lane % 32, rows_all - 1);
@@ -313,7 +314,7 @@ __global__ __launch_bounds__(HALVES * kThreads, 2) void diff_dq_kernel(DiffArgs 
   const Visible vis = visible(a, b);
   const int limit = key_limit(a, vis, n);
   const int low = key_limit(a, vis, token(row0)), high = key_limit(a, vis, token(row0 + 31));
-  const int end = key_limit(a, vis, token(tile * 128u + 127));
+  const int end = key_limit(a, vis, token(static_cast<uint32_t>(tile) * ROWS + ROWS - 1));
 
   if (end > 0) {
     const int i = threadIdx.x / (D / 8), ch = threadIdx.x % (D / 8) * 8;
@@ -365,8 +366,8 @@ __global__ __launch_bounds__(HALVES * kThreads, 2) void diff_dq_kernel(DiffArgs 
       if (key + K < end) copy(key + K, buf ^ 1);
       const uint32_t kt = lds_offset(lds[buf][0]), vt = lds_offset(lds[buf][1]);
 #pragma unroll
-      for (int jj = 0; jj < K / 32; jj += HALVES) {
-        const int j = jj + half;
+      for (int jj = 0; jj < K / 32; jj += SHARE) {
+        const int j = jj + share;
         const int at = key + 32 * j;
         if (at >= high) continue;
         f32x16 dp{};
@@ -415,22 +416,23 @@ __global__ __launch_bounds__(HALVES * kThreads, 2) void diff_dq_kernel(DiffArgs 
   walk(std::integral_constant<int, 0>{});
 #pragma unroll
   for (int i = 0; i < 2; ++i) d[i] = sum_halves(d[i]);
-  if constexpr (HALVES == 2) {
-    if (half)
+  const auto add_up = [&](float (&v)[2]) {  // over the waves of a row, in order; each gets the sum
+    if constexpr (SHARE > 1) {
 #pragma unroll
-      for (int i = 0; i < 2; ++i) sums[wave % 4][i][lane] = d[i];
-    __syncthreads();
-    if (!half)
+      for (int i = 0; i < 2; ++i) sums[share][group][i][lane] = v[i];
+      __syncthreads();
 #pragma unroll
-      for (int i = 0; i < 2; ++i) sums[wave][i][lane] = d[i] += sums[wave][i][lane];
-    __syncthreads();
-    if (half)
+      for (int i = 0; i < 2; ++i) {
+        v[i] = sums[0][group][i][lane];
 #pragma unroll
-      for (int i = 0; i < 2; ++i) d[i] = sums[wave % 4][i][lane];
-  }
-  if (!half && live && lane < 32) put_stat(stat_at(stat, bhn, n, a.N), lse[0], lse[1], d[0], d[1], a.lam[h], c);
+        for (int o = 1; o < SHARE; ++o) v[i] += sums[o][group][i][lane];
+      }
+    }
+  };
+  add_up(d);
+  if (!share && live && lane < 32) put_stat(stat_at(stat, bhn, n, a.N), lse[0], lse[1], d[0], d[1], a.lam[h], c);
   if (tile == tiles - 1)  // rows behind the last token
-    for (int x = threadIdx.x; x < G * static_cast<int>(padded(a.N) - a.N); x += HALVES * kThreads)
+    for (int x = threadIdx.x; x < G * static_cast<int>(padded(a.N) - a.N); x += 64 * WAVES)
       put_stat(stat_at(stat, static_cast<int64_t>(b) * a.Hq + hk * G + x % G, a.N + x / G, a.N), kNever, kNever, 0.0f, 0.0f, 1.0f, 1.0f);
   wait_copies();
   barrier();  // the tiles have been read
@@ -448,33 +450,36 @@ __global__ __launch_bounds__(HALVES * kThreads, 2) void diff_dq_kernel(DiffArgs 
       for (int i = 0; i < SAMPLE; ++i) m += static_cast<float>(sample[i][threadIdx.x]);
     mean[threadIdx.x] = m * (1.0f / SAMPLE);
   }
-  if constexpr (HALVES == 2) {
-    f32x4* swap = reinterpret_cast<f32x4*>(lds) + (wave % 4) * 4 * S * 64 + lane;
-    if (half)
+  add_up(rest);
+  if constexpr (SHARE > 1) {
+    f32x4* swap = reinterpret_cast<f32x4*>(lds) + lane;
+    constexpr int PER = 4 * S * 64;
+    if (share) {
+      f32x4* to = swap + ((share - 1) * GROUPS + group) * PER;
 #pragma unroll
-      for (int i = 0; i < 2; ++i) sums[wave % 4][i][lane] = rest[i];
+      for (int t = 0; t < S; ++t)
 #pragma unroll
-    for (int t = 0; t < S; ++t)
-#pragma unroll
-      for (int e = 0; e < 4; ++e) {
-        f32x16& q = dq[t / (S / 2)][t % (S / 2)];
-        if (half) swap[(4 * t + e) * 64] = f32x4{q[4 * e], q[4 * e + 1], q[4 * e + 2], q[4 * e + 3]};
-      }
+        for (int e = 0; e < 4; ++e) {
+          const f32x16& q = dq[t / (S / 2)][t % (S / 2)];
+          to[(4 * t + e) * 64] = f32x4{q[4 * e], q[4 * e + 1], q[4 * e + 2], q[4 * e + 3]};
+        }
+    }
   }
   __syncthreads();
-  if constexpr (HALVES == 2) {
-    const f32x4* swap = reinterpret_cast<const f32x4*>(lds) + (wave % 4) * 4 * S * 64 + lane;
-    if (half) return;
+  if (share) return;
+  if constexpr (SHARE > 1) {
+    const f32x4* swap = reinterpret_cast<const f32x4*>(lds) + lane;
+    constexpr int PER = 4 * S * 64;
 #pragma unroll
-    for (int i = 0; i < 2; ++i) rest[i] += sums[wave % 4][i][lane];
+    for (int o = 0; o < SHARE - 1; ++o)
 #pragma unroll
-    for (int t = 0; t < S; ++t)
+      for (int t = 0; t < S; ++t)
 #pragma unroll
-      for (int e = 0; e < 4; ++e) {
-        const f32x4 y = swap[(4 * t + e) * 64];
+        for (int e = 0; e < 4; ++e) {
+          const f32x4 y = swap[(o * GROUPS + group) * PER + (4 * t + e) * 64];
 #pragma unroll
-        for (int x = 0; x < 4; ++x) dq[t / (S / 2)][t % (S / 2)][4 * e + x] += y[x];
-      }
+          for (int x = 0; x < 4; ++x) dq[t / (S / 2)][t % (S / 2)][4 * e + x] += y[x];
+        }
   }
   const float f[2] = {a.scale, -a.lam[h] * a.scale};
   T* out = static_cast<T*>(a.dq.p) + b * a.dq.sb + h * a.dq.sh + n * a.dq.sn;
@@ -512,14 +517,18 @@ Share dkv_share(int B, int Hq, int Hk, int N, int M, bool causal) {
 template <typename T, int D>
 hipError_t launch(const DiffArgs& a, hipStream_t stream) {
   float* stat = a.ws;
-  const int row_tiles = static_cast<int>((static_cast<int64_t>(a.N) * (a.Hq / a.Hk) + 127) / 128);
-  const int row_units = a.B * a.Hk * row_tiles;
+  const int64_t rows = static_cast<int64_t>(a.N) * (a.Hq / a.Hk);
+  const int row_tiles = static_cast<int>((rows + 127) / 128), row_units = a.B * a.Hk * row_tiles;
   // as in the forward pass: 192 tiles of 2,048 keys 237 -> 207 us for the backward pass, 384 causal ones of up to 4,096
-  // 518 -> 415, 384 without a mask 655 -> 699
+  // 518 -> 415, 384 without a mask 655 -> 699; half the rows: 64 tiles of 1,024 keys 88 -> 71, 126 of 777 keys of 64
+  // channels 60 -> 51, 192 of 1,024 keys 104 -> 119
   if (row_units > (a.causal ? 512 : 256)) {
     diff_dq_kernel<T, D, 1><<<grid_of(row_units), kThreads, 0, stream>>>(a, stat, row_tiles, row_units);
-  } else {
+  } else if (row_units > 128) {
     diff_dq_kernel<T, D, 2><<<grid_of(row_units), 2 * kThreads, 0, stream>>>(a, stat, row_tiles, row_units);
+  } else {
+    const int tiles = static_cast<int>((rows + 63) / 64), n = a.B * a.Hk * tiles;
+    diff_dq_kernel<T, D, 4><<<grid_of(n), 2 * kThreads, 0, stream>>>(a, stat, tiles, n);
   }
   const int key_tiles = static_cast<int>((a.M + 127ll) / 128);
   const Share share = dkv_share(a.B, a.Hq, a.Hk, a.N, a.M, a.causal);

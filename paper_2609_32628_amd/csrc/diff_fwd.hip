@@ -189,10 +189,10 @@ __device__ inline void finish_element(const DiffArgs& a, int b, int h, int n, in
   row_ptr<T>(a.o, b, h, n)[ch] = static_cast<T>(u1 * i1 - u2 * (a.lam[h] * i2));
 }
 
-// HALVES: 1, or 2 where each wave's rows are shared by a second wave, which takes every other 32 keys.
-template <typename T, int D, int HALVES>
-__global__ __launch_bounds__(HALVES * kThreads, 2) void diff_many_kernel(DiffArgs a, int tiles, int splits, int units) {
-  constexpr int K = 64 * HALVES, WAVES = 4 * HALVES, BYTES = K * Tile<D>::kRow, R = Tile<D>::kRowsPerCopy, C = D / 32;
+template <typename T, int D, int SHARE>
+__global__ __launch_bounds__(64 * Many<SHARE>::kWaves, 2) void diff_many_kernel(DiffArgs a, int tiles, int splits, int units) {
+  constexpr int GROUPS = Many<SHARE>::kGroups, ROWS = Many<SHARE>::kRows;
+  constexpr int K = Many<SHARE>::kKeys, WAVES = Many<SHARE>::kWaves, BYTES = K * Tile<D>::kRow, R = Tile<D>::kRowsPerCopy, C = D / 32;
   __shared__ __align__(256) char lds[2][2][BYTES];  // [buffer][K, V]
   const int unit = unit_of(blockIdx.x, units);
   if (unit < 0) return;
@@ -201,8 +201,9 @@ __global__ __launch_bounds__(HALVES * kThreads, 2) void diff_many_kernel(DiffArg
   const int tile = tiles - 1 - unit / splits % tiles;
   const int bh = unit / splits / tiles;
   const int b = bh / a.Hk, hk = bh % a.Hk, G = a.Hq / a.Hk;
-  const int lane = threadIdx.x % 64, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64), half = wave / 4;
-  const uint32_t rows = static_cast<uint32_t>(a.N) * G, row0 = tile * 128u + 32 * (wave % 4);
+  const int lane = threadIdx.x % 64, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64);
+  const int group = wave % GROUPS, share = wave / GROUPS;
+  const uint32_t rows = static_cast<uint32_t>(a.N) * G, row0 = static_cast<uint32_t>(tile) * ROWS + 32 * group;
   const auto token = [&](uint32_t r) { return static_cast<int>(min(r, rows - 1) / static_cast<uint32_t>(G)); };
   const bool live = row0 + lane % 32 < rows;
   const uint32_t row = min(row0 + lane % 32, rows - 1);
@@ -210,7 +211,7 @@ __global__ __launch_bounds__(HALVES * kThreads, 2) void diff_many_kernel(DiffArg
   const Visible vis = visible(a, b);
   const int limit = key_limit(a, vis, n);
   const int low = key_limit(a, vis, token(row0)), high = key_limit(a, vis, token(row0 + 31));  // of the wave
-  int end = key_limit(a, vis, token(tile * 128u + 127));                                      // of the workgroup
+  int end = key_limit(a, vis, token(static_cast<uint32_t>(tile) * ROWS + ROWS - 1));                                      // of the workgroup
   int key = 0;
   if (splits > 1) {
     const int part = ((end + splits - 1) / splits + K - 1) / K * K;
@@ -235,54 +236,59 @@ __global__ __launch_bounds__(HALVES * kThreads, 2) void diff_many_kernel(DiffArg
     wait_copies();
     barrier();  // every wave's copies have arrived, and the other buffer has been read
     if (key + K < end) copy(key + K, buf ^ 1);
-    const uint32_t kt = lds_offset(lds[buf][0]) + half * 32 * Tile<D>::kRow;
-    const uint32_t vt = lds_offset(lds[buf][1]) + half * 32 * Tile<D>::kRow;
+    const uint32_t kt = lds_offset(lds[buf][0]) + share * 32 * Tile<D>::kRow;
+    const uint32_t vt = lds_offset(lds[buf][1]) + share * 32 * Tile<D>::kRow;
 #pragma unroll
-    for (int j = 0; j < K / 32; j += HALVES) {
-      const int at = key + 32 * (j + half);
+    for (int j = 0; j < K / 32; j += SHARE) {
+      const int at = key + 32 * (j + share);
       if (at < min(high, end)) r.step(kt, vt, j, at, limit, at + 32 > low, c);
     }
   }
 #pragma unroll
   for (int i = 0; i < 2; ++i) r.l[i] = sum_halves(r.l[i]);
-  // The second half's waves hand their sums to the first half's, one map after the other, in the room of the tiles.
-  if constexpr (HALVES == 2) {
-    f32x4* swap = reinterpret_cast<f32x4*>(lds) + (wave % 4) * (4 * C + 1) * 64 + lane;
+  // The other waves of a row hand their sums to the first, one map after the other, in the room of the tiles.
+  if constexpr (SHARE > 1) {
+    f32x4* swap = reinterpret_cast<f32x4*>(lds) + lane;
+    constexpr int PER = (4 * C + 1) * 64;
 #pragma unroll
     for (int i = 0; i < 2; ++i) {
       __syncthreads();
-      if (half) {
+      if (share) {
+        f32x4* to = swap + ((share - 1) * GROUPS + group) * PER;
 #pragma unroll
         for (int t = 0; t < C; ++t)
 #pragma unroll
           for (int e = 0; e < 4; ++e)
-            swap[(4 * t + e) * 64] = f32x4{r.u[i][t][4 * e], r.u[i][t][4 * e + 1], r.u[i][t][4 * e + 2], r.u[i][t][4 * e + 3]};
-        swap[4 * C * 64] = f32x4{r.m[i], r.l[i], 0.0f, 0.0f};
+            to[(4 * t + e) * 64] = f32x4{r.u[i][t][4 * e], r.u[i][t][4 * e + 1], r.u[i][t][4 * e + 2], r.u[i][t][4 * e + 3]};
+        to[4 * C * 64] = f32x4{r.m[i], r.l[i], 0.0f, 0.0f};
       }
       __syncthreads();
-      if (!half) {
-        const f32x4 other = swap[4 * C * 64];
-        const float m = fmaxf(r.m[i], other[0]), f = exp2_fast(r.m[i] - m), g = exp2_fast(other[0] - m);
-        r.m[i] = m;
-        r.l[i] = r.l[i] * f + other[1] * g;
+      if (!share)
 #pragma unroll
-        for (int t = 0; t < C; ++t)
+        for (int o = 0; o < SHARE - 1; ++o) {
+          const f32x4* from = swap + (o * GROUPS + group) * PER;
+          const f32x4 other = from[4 * C * 64];
+          const float m = fmaxf(r.m[i], other[0]), f = exp2_fast(r.m[i] - m), g = exp2_fast(other[0] - m);
+          r.m[i] = m;
+          r.l[i] = r.l[i] * f + other[1] * g;
 #pragma unroll
-          for (int e = 0; e < 4; ++e) {
-            const f32x4 y = swap[(4 * t + e) * 64];
+          for (int t = 0; t < C; ++t)
 #pragma unroll
-            for (int x = 0; x < 4; ++x) r.u[i][t][4 * e + x] = r.u[i][t][4 * e + x] * f + y[x] * g;
-          }
-      }
+            for (int e = 0; e < 4; ++e) {
+              const f32x4 y = from[(4 * t + e) * 64];
+#pragma unroll
+              for (int x = 0; x < 4; ++x) r.u[i][t][4 * e + x] = r.u[i][t][4 * e + x] * f + y[x] * g;
+            }
+        }
     }
   }
-  if (half) return;
+  if (share) return;
   if (splits == 1) {
     finish_rows(a, r, b, h, n, live);
     return;
   }
   // parts lie as the registers do, a wave's 1 KB at a time
-  f32x4* part = reinterpret_cast<f32x4*>(a.ws) + (static_cast<int64_t>(unit) * 4 + wave) * kBlock<D> + lane;
+  f32x4* part = reinterpret_cast<f32x4*>(a.ws) + (static_cast<int64_t>(unit) * GROUPS + group) * kBlock<D> + lane;
   part[0] = f32x4{r.m[0], r.l[0], r.m[1], r.l[1]};
 #pragma unroll
   for (int t = 0; t < C; ++t)
@@ -494,13 +500,17 @@ hipError_t launch(const DiffArgs& a, hipStream_t stream) {
   if (c.few) {
     diff_few_kernel<T, D><<<grid_of(units), kThreads, 0, stream>>>(a, c.tiles, c.splits, units);
   } else {
-    // the second wave for a row pays where 4-wave workgroups leave SIMDs with one wave or none, or a causal mask leaves
+    // Waves that share a row's keys pay where 4-wave workgroups leave SIMDs with one wave or none, or a causal mask leaves
     // the last of them alone: 192 tiles of 2,048 keys 67 -> 50 us, 384 causal ones of up to 4,096 168 -> 114, but 384
-    // without a mask 177 -> 197
+    // without a mask 177 -> 197. Four of them, on half the rows, pay while each half still finds a CU of its own: 64 tiles
+    // of 1,024 keys 28 -> 25 us, 126 of 777 keys of 64 channels 18.2 -> 14.7, but 192 of 1,024 keys 29 -> 47.
     if (units > (a.causal ? 512 : 256)) {
       diff_many_kernel<T, D, 1><<<grid_of(units), kThreads, 0, stream>>>(a, c.tiles, c.splits, units);
-    } else {
+    } else if (units > 128 || c.splits > 1) {
       diff_many_kernel<T, D, 2><<<grid_of(units), 2 * kThreads, 0, stream>>>(a, c.tiles, c.splits, units);
+    } else {
+      const int tiles = static_cast<int>((static_cast<int64_t>(a.N) * (a.Hq / a.Hk) + 63) / 64), n = a.B * a.Hk * tiles;
+      diff_many_kernel<T, D, 4><<<grid_of(n), 2 * kThreads, 0, stream>>>(a, tiles, 1, n);
     }
   }
   if (c.splits > 1 && !c.few) {

@@ -182,6 +182,13 @@ def test_padded_batches_and_empty_rows(d, causal):
     check(Case(2, 1, 1, 200, 130, d, "bf16", causal, None, [-150, 100], seed=4))
 
 
+@pytest.mark.parametrize("d,dtype", [(64, "fp16"), (128, "bf16")])
+@pytest.mark.parametrize("H,causal", [(64, False), (65, False), (128, False), (129, False), (65, True), (256, True), (257, True)])
+def test_many_tiles(H, causal, d, dtype):
+    """Two tiles of 128 rows a head: on both sides of the counts of tiles at which other workgroups take the rows."""
+    check(Case(1, H, H, 150, 170, d, dtype, causal, seed=H))
+
+
 @pytest.mark.parametrize("dtype", ["bf16", "fp16"])
 @pytest.mark.parametrize("B,H,Hk,N,M,d", [(1, 12, 4, 1, 1000, 64), (3, 8, 2, 1, 4097, 128), (1, 1, 1, 5, 2500, 128), (2, 4, 4, 16, 3000, 64),
                                           (1, 2, 2, 100, 2000, 128), (1, 40, 20, 33, 1100, 64)])
