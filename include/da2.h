@@ -509,7 +509,8 @@ int32_t da2_diff_ws_bytes(const da2_diff_problem* p, int32_t train, int64_t* byt
  *   ws      device scratch of da2_diff_ws_bytes(p, 0); may be NULL when that is 0
  * Scores, softmax statistics and sums are float32; the weights are rounded to
  * the tensors' type for the product with V. Keys that a query's mask hides must
- * be finite where another query of the call sees them.
+ * be finite where another query of the call sees them; what lies where no query
+ * of the call sees it is not used.
  * Errors: INVALID_ARG, UNSUPPORTED (d, float32), WORKSPACE. */
 int32_t da2_diff_attn(const da2_diff_problem* p, const void* Q, const da2_tensor* q, const void* K,
                       const da2_tensor* k, const void* V, const da2_tensor* v, const float* lambda,
@@ -517,7 +518,9 @@ int32_t da2_diff_attn(const da2_diff_problem* p, const void* Q, const da2_tensor
                       float* lse, void* ws, int64_t ws_bytes, void* stream);
 
 /* Gradients of da2_diff_attn, from its inputs and what it wrote to lse. Rows
- * that see no key give nothing; keys beyond kv_lens get zeros.
+ * that see no key give nothing, but their Q and dO must be finite like all
+ * others; keys that no query sees get zeros. The gradients of the scores are
+ * rounded to the tensors' type for the products with K and Q.
  *   dO      device [B,Hq,N,d]; dQ device out like Q; dK, dV device out like K
  *           and V (summed over the query heads that share them)
  *   dlambda device out float32 [Hq]

@@ -164,6 +164,8 @@ __device__ inline Visible visible(const DiffArgs& a, int b) {
   Visible s;
   s.len = a.kv_lens ? min(max(a.kv_lens[b], 0), a.M) : a.M;
   s.start = a.q_start ? a.q_start[b] : static_cast<int64_t>(s.len) - a.N;
+  // keys that no query sees are not there: in a tile, a weight of zero would still meet what they hold
+  if (a.causal && s.start + a.N < s.len) s.len = static_cast<int>(s.start + a.N < 0 ? 0 : s.start + a.N);
   return s;
 }
 // Query n sees the keys below this.

@@ -189,6 +189,23 @@ def test_many_tiles(H, causal, d, dtype):
     check(Case(1, H, H, 150, 170, d, dtype, causal, seed=H))
 
 
+@pytest.mark.parametrize("N,M,start", [(1, 300, [40, 0, -5]), (70, 300, [3, -50, -100]), (200, 500, [100, 0, 250]), (33, 3000, [1500, 7, 2900])])
+@pytest.mark.parametrize("d", [64, 128])
+def test_keys_that_no_query_sees(d, N, M, start):
+    """A cache whose room behind the last query's position was never written: it may hold anything."""
+    case = Case(3, 4, 2, N, M, d, "bf16", True, None, start, seed=25)
+    want = check(case)
+    for b, s in enumerate(start):
+        case.K[b, :, max(s + N, 0):] = float("nan")
+        case.V[b, :, max(s + N, 0):] = float("inf")
+    out = {n: torch.full_like(x, float("nan")) for n, x in want.items()}
+    ws = torch.empty(api.da2_diff_ws_bytes(case.Q, case.K, True), dtype=torch.uint8, device="cuda")
+    api.da2_diff_attn(case.Q, case.K, case.V, case.lam, out["O"], ws, out["lse"], **case.how())
+    api.da2_diff_attn_bwd(case.Q, case.K, case.V, case.lam, out["lse"], case.dO, out["dQ"], out["dK"], out["dV"], out["dlam"],
+                          ws, **case.how())
+    assert all(torch.equal(out[n], want[n]) for n in want)
+
+
 @pytest.mark.parametrize("dtype", ["bf16", "fp16"])
 @pytest.mark.parametrize("B,H,Hk,N,M,d", [(1, 12, 4, 1, 1000, 64), (3, 8, 2, 1, 4097, 128), (1, 1, 1, 5, 2500, 128), (2, 4, 4, 16, 3000, 64),
                                           (1, 2, 2, 100, 2000, 128), (1, 40, 20, 33, 1100, 64)])
