@@ -359,7 +359,7 @@ int32_t da2_mixed_attn(const void* ops, int64_t ops_bytes, const void* lists, co
  *     is not looked at. An output's rows must not overlap one another; an input
  *     may repeat rows (stride 0).
  *   - an output may be the same memory as an input only where a call says so,
- *     and then with the input's strides.
+ *     and then with the input's strides; no two outputs share memory.
  *   - sums and statistics are held in fp32 or more; results are rounded once.
  *   - results do not depend on the order in which workgroups run (no atomics).
  *   - extents are >= 1, B <= 65535, and H*N <= 2^31 - 1; else INVALID_ARG. */

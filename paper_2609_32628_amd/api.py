@@ -170,6 +170,10 @@ def attention(Q, K, V, buf, lam, budgets, O, stream=None, num16=0, fmt4=None, qk
     if fmt4 != buf.fmt4 or (num16 > 0 and not buf.with16):
         raise ValueError(f"buffers sized for fmt4={buf.fmt4}, with16={buf.with16}; asked for fmt4={fmt4}, "
                          f"num16={num16}")
+    if rope is not None and len(rope.rot_axis) not in (1, 3):
+        raise ValueError(f"rope: expected 1 or 3 axes, got {len(rope.rot_axis)}")
+    if (qk_norm is not None or rope is not None) and Q.data_ptr() == K.data_ptr():
+        raise ValueError("Q and K are one tensor: the norm and rotation in place would meet it twice")
     if qk_norm is not None:
         da2_norm(Q, Q, qk_norm[0], kind="rms", stream=stream)
         da2_norm(K, K, qk_norm[1], kind="rms", stream=stream)

@@ -209,7 +209,7 @@ int32_t da2_norm_bwd(const void* dY, const da2_tensor* dy, const void* X, const 
   if (dX && ((st = check_view(dx, e, x->dtype, true)) || (dX == X && !same_strides(dx, x, e)) ||
              (dX == dY && !same_strides(dx, dy, e))))
     return DA2_ERR_INVALID_ARG;
-  if (!X || !dY || !stats || (!dX && !dw && !db)) return DA2_ERR_INVALID_ARG;
+  if (!X || !dY || !stats || (!dX && !dw && !db) || (dw && dw == db)) return DA2_ERR_INVALID_ARG;
   if (dw || db) {
     if (!ws) return DA2_ERR_INVALID_ARG;
     if (ws_bytes < norm_ws(e, x->dtype, n->stride_b != 0)) return DA2_ERR_WORKSPACE;
@@ -289,6 +289,7 @@ int32_t da2_rope(const da2_rope_desc* r, const double* turns, double scale, cons
   if (s->Hk) {
     if (check_view(k, ek, q->dtype, false) || check_view(ko, ek, q->dtype, true)) return DA2_ERR_INVALID_ARG;
     if (!K || !Ko || (K == Ko && !same_strides(k, ko, ek))) return DA2_ERR_INVALID_ARG;
+    if (Ko == Qo || Ko == Q || K == Qo) return DA2_ERR_INVALID_ARG;
   }
   if ((st = check_device())) return st;
   da2::RopeArgs a{};

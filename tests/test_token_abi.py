@@ -275,3 +275,25 @@ def test_diff_binding_refusals():
               lambda: api.da2_diff_attn_bwd(Q, K, K, lam, None, O, O, K, K[:, :1], lam, O)):
         with pytest.raises((ValueError, _lib.Da2Error)):
             f()
+
+
+def test_outputs_that_share_memory_are_refused():
+    """Q and K rotated into one tensor or into each other, and dw written where db is."""
+    L = _lib.lib()
+    t, A = _desc(2, 3, 5, 64), FAKE
+    rows = _lib.RopeRows(2, 3, 3, 5, 64, 0, 0, 0)
+    for q, qo, k, ko in ((A, 2 * A, 3 * A, 2 * A), (A, A, 2 * A, A), (A, 2 * A, 3 * A, A), (A, 3 * A, 3 * A, 2 * A)):
+        assert L.da2_rope(_rope_desc(), 5 * A, 1.0, None, 0, rows, q, t, qo, t, k, t, ko, t, None) == E
+    n = _lib.NormDesc(0, 1, 0, 0, 0, 1e-6)
+    assert L.da2_norm_bwd(A, t, 2 * A, t, _lib.Rows(2, 3, 5, 64), n, None, 3 * A, None, None, 4 * A, 4 * A, 5 * A, 1 << 30, None) == E
+
+
+def test_attention_refuses_what_it_would_rotate_wrongly():
+    from types import SimpleNamespace
+    buf = SimpleNamespace(p=None, fmt4="nvfp4", with16=False)
+    Q, K = torch.ones(1, 1, 4, 64), torch.ones(1, 1, 4, 64)
+    rope = api.Rope("half", 64, (32, 32), torch.zeros(32, dtype=torch.float64))
+    with pytest.raises(ValueError, match="axes"):
+        api.attention(Q, K, K, buf, 0, (1, 1, 2), Q, rope=rope)
+    with pytest.raises(ValueError, match="one tensor"):
+        api.attention(Q, Q, K, buf, 0, (1, 1, 2), Q, qk_norm=(None, None))
