@@ -10,7 +10,10 @@
 // stays in the registers of the threads that share it: TPR threads with K
 // chunks of 16 bytes each, from part of a wave for narrow rows (a head's 64 or
 // 128 channels) to a workgroup of 512 threads. Rows wider than that (4 chunks
-// for each of 512 threads) are read again from the caches for each pass.
+// for each of 512 threads, 3 in the backward pass) are read again from the caches
+// for each pass. A workgroup walks over rows and fetches the next one before it
+// works on this one. (bf16, 32,760 rows of 1,536: 44 us, 4.6 TB/s; 16,380 of 5,120:
+// 61 us forward and 110 backward, 5.5 and 4.6 TB/s; a copy reaches 5.0 to 5.4.)
 // The weight gradients are summed in registers over the rows of a workgroup,
 // written as one partial row per workgroup and added up by a second kernel, so
 // that their order is fixed.
