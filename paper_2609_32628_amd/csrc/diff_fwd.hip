@@ -44,10 +44,10 @@ Cut cut_of(int B, int Hq, int Hk, int N, int M) {
   const int64_t units = static_cast<int64_t>(B) * Hk * c.tiles;
   // One workgroup a CU, which is what LDS holds of few rows, and parts that take longer to walk than to join. Few rows (one
   // sample of 32,768 keys, 8 key heads: 41 us with half as many workgroups, 44 with one a CU, 64 with two; 8 samples of
-  // 8,192, 12 heads: 113, 74 and 80): 256 keys. Many rows: 128 keys take a workgroup
-  // of 128 rows 2.5 us, and a launch and the parts' way through memory 5 us and more, so parts have 512 keys (from 1,536 on) where the
-  // tiles leave most CUs idle and 2,048 else (32 tiles against 1,024 keys: 24 us whole and 26 in two parts; 64 against
-  // 2,048: 42 whole, 40 in two, 36 in four; 128 against 2,048: 44 whole and 49 in two).
+  // 8,192, 12 heads: 113, 74 and 80): 256 keys. Many rows: 128 keys take a workgroup of 128 rows 2.5 us, and a launch and
+  // the parts' way through memory 5 us and more, so parts have 512 keys (from 1,536 on) where the tiles leave most CUs idle
+  // and 2,048 else (32 tiles against 1,024 keys: 24 us whole and 26 in two parts; 64 against 2,048: 42 whole, 40 in two, 36
+  // in four; 128 against 2,048: 44 whole and 49 in two).
   int64_t s = 256 / units, most = c.few ? (M + 255) / 256 : units <= 64 && M >= 1536 ? M / 512 : M / 2048;
   s = s < most ? s : most;
   c.splits = static_cast<int>(s < 1 ? 1 : s);
