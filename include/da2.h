@@ -362,6 +362,7 @@ int32_t da2_mixed_attn(const void* ops, int64_t ops_bytes, const void* lists, co
  *     and then with the input's strides; no two outputs share memory.
  *   - sums and statistics are held in fp32 or more; results are rounded once.
  *   - results do not depend on the order in which workgroups run (no atomics).
+ *   - calls that run at the same time need workspaces of their own.
  *   - extents are >= 1, B <= 65535, and H*N <= 2^31 - 1; else INVALID_ARG. */
 
 /* Rows of a token tensor. */

@@ -17,7 +17,7 @@
 //   - few rows (up to 64): 4 waves with the same 32 rows walk the 32-key quarters
 //     of 128-key tiles, each its own, and are joined at the end.
 // Where that leaves CUs idle the keys are split over workgroups; a second kernel
-// joins the parts. (bf16, 16,380 tokens of 12 heads, d = 128: 2.26 ms, 1.09 PFLOP/s,
+// joins the parts. (bf16, 16,380 tokens of 12 heads, d = 128: 2.3 ms, 1.08 PFLOP/s,
 // bound by products and exponentials, which share the issue slots; one token over
 // 16 caches of up to 16,384 keys, 8 key heads: 161 us, 5.1 TB/s.)
 #include "diff.hpp"
