@@ -521,7 +521,9 @@ int32_t da2_diff_attn(const da2_diff_problem* p, const void* Q, const da2_tensor
 /* Gradients of da2_diff_attn, from its inputs and what it wrote to lse. Rows
  * that see no key give nothing, but their Q and dO must be finite like all
  * others; keys that no query sees get zeros. The gradients of the scores are
- * rounded to the tensors' type for the products with K and Q.
+ * rounded to the tensors' type for the products with K and Q, and the weights
+ * for that with dO; in fp16 scaled by powers of two, so that they neither fall
+ * below its normal numbers nor pass its largest one before the results do.
  *   dO      device [B,Hq,N,d]; dQ device out like Q; dK, dV device out like K
  *           and V (summed over the query heads that share them)
  *   dlambda device out float32 [Hq]

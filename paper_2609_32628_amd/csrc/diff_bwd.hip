@@ -20,6 +20,16 @@
 // per pair: 2 for del, 3 for dQ, 4 for dK and dV, where one pass over both sides
 // (which would need sums in memory) takes 5 beside del. (bf16, 2 x 2,048 causal
 // tokens, 12 heads on 4 key heads, d = 128: dQ 111 us, dK and dV 84, joined in 16.)
+//
+// The weights and score gradients are rounded to 16 bits for their products. In
+// fp16 that would lose them: a weight is about one over the number of keys, and dS
+// that times dO, so over 4,096 keys a dO of 1e-4 leaves dS a few bits of fp16's
+// subnormal numbers (error of dQ 2.4%, of dQ's own rounding 0.2%), and one of 1e4
+// overflows. So fp16 products take them times a power of two, which their float32
+// sums give back: dS of a row in dQ by the row's largest |dP|; in dK and dV, whose
+// sums run over rows, dS by a key head's largest |dP| and the weights by its
+// largest |lambda|. |dS| is at most 2 P |dP| (times |lambda| in the second map),
+// so they stay below 2^15.
 #include <algorithm>
 #include <type_traits>
 
@@ -57,6 +67,12 @@ constexpr float kNever = __builtin_inff();
 // for the copies issued before it.
 __device__ inline float load_uniform(const float* p) { return *(const __attribute__((address_space(4))) float*)p; }
 
+// Whether products of T take scaled weights and score gradients.
+template <typename T>
+constexpr bool kScaled = __is_same(T, fp16_t);
+// e with |x| < 2^e and, unless that leaves the range in which 2^e and 2^-e are floats with room to spare, 2^e <= 2 |x|.
+__device__ inline int exponent_above(float x) { return min(max(__builtin_amdgcn_frexp_expf(x), -100), 100); }
+
 // 16 floats of LDS, the same for all lanes of a half.
 __device__ inline f32x16 read16(const float* p) {
   f32x16 x;
@@ -88,16 +104,41 @@ __device__ inline void sum_dlam(const DiffArgs& a, float* stat, int h, double* s
   if (threadIdx.x == 0) a.dlam[h] = static_cast<float>(-sums[0]);
 }
 
+// The largest values of a key head's n tops, into the first of as many slots. For more of them than dK and dV's workgroups
+// have threads: a loop over them there takes registers that the loop over the queries needs.
+constexpr int kMostTops = kThreads;
+__global__ __launch_bounds__(kThreads) void diff_tops_kernel(const float2* tops, int n, float2* out) {
+  __shared__ float most[2][kThreads / 64];
+  const float2* top = tops + static_cast<int64_t>(blockIdx.x) * n;
+  float t = 0.0f, l = 0.0f;
+  for (int i = threadIdx.x; i < n; i += kThreads) {
+    t = fmaxf(t, top[i].x);
+    l = fmaxf(l, top[i].y);
+  }
+  t = wave_max_f32(t);
+  l = wave_max_f32(l);
+  if (threadIdx.x % 64 == 0) {
+    most[0][threadIdx.x / 64] = t;
+    most[1][threadIdx.x / 64] = l;
+  }
+  __syncthreads();
+  if (threadIdx.x == 0)
+    out[blockIdx.x] = make_float2(fmaxf(fmaxf(most[0][0], most[0][1]), fmaxf(most[0][2], most[0][3])),
+                                  fmaxf(fmaxf(most[1][0], most[1][1]), fmaxf(most[1][2], most[1][3])));
+}
+
 // dK and dV of 128 keys: 4 waves with 32 keys each; 32 queries of one head at a time in LDS. A wave's keys are in
 // registers, its values in LDS: both in registers would leave one wave a SIMD at d = 128. HALVES = 2: twice the waves,
 // the second four with the same keys and every other tile of queries. The first workgroups, a multiple of 8, sum dlambda
 // beside them.
 template <typename T, int D, int HALVES>
-__global__ __launch_bounds__(HALVES * kThreads, 2) void diff_dkv_kernel(DiffArgs a, float* stat, float* sums, int tiles, int parts, int units, int lambdas) {
+__global__ __launch_bounds__(HALVES * kThreads, D == 64 && HALVES == 1 ? 3 : 2) void diff_dkv_kernel(
+    DiffArgs a, float* stat, const float2* tops, int n_tops, float* sums, int tiles, int parts, int units, int lambdas) {
   constexpr int S = D / 32, Q = 32, BYTES = Q * Tile<D>::kRow, R = Tile<D>::kRowsPerCopy;
   __shared__ __align__(256) char lds[2][HALVES][2][BYTES];  // [buffer][half][Q, dO]
   __shared__ __align__(256) char val[4 * BYTES];            // the workgroup's rows of V
   __shared__ __align__(16) float st[2][HALVES][4][Q];
+  __shared__ float most[2][4 * HALVES];  // |dP| and |lambda|, by wave
   if (static_cast<int>(blockIdx.x) < lambdas) {
     if (static_cast<int>(blockIdx.x) < a.Hq) sum_dlam<HALVES * kThreads>(a, stat, blockIdx.x, reinterpret_cast<double*>(lds));
     return;
@@ -115,6 +156,27 @@ __global__ __launch_bounds__(HALVES * kThreads, 2) void diff_dkv_kernel(DiffArgs
   f32x16 dv[S], dk[2][S / 2];
 #pragma unroll
   for (int t = 0; t < S; ++t) dv[t] = dk[t / (S / 2)][t % (S / 2)] = f32x16{};
+
+  if constexpr (kScaled<T>) {
+    const float2 x = tops[static_cast<int64_t>(bh) * n_tops + min(static_cast<int>(threadIdx.x), n_tops - 1)];
+    const float t = wave_max_f32(x.x), l = wave_max_f32(x.y);
+    if (lane == 0) {
+      most[0][threadIdx.x / 64] = t;
+      most[1][threadIdx.x / 64] = l;
+    }
+    __syncthreads();
+  }
+  // Exponents of the scales of the weights and of dS; read again where they are needed, which spares registers.
+  const auto scales = [&](int& kw, int& ks) {
+    float t = most[0][0], l = most[1][0];
+#pragma unroll
+    for (int i = 1; i < 4 * HALVES; ++i) {
+      t = fmaxf(t, most[0][i]);
+      l = fmaxf(l, most[1][i]);
+    }
+    kw = 14 - min(max(exponent_above(l), 0), 20);  // 1 + |lambda| < 2^(15 - kw)
+    ks = kw - exponent_above(t);
+  };
 
   // queries that see the tile's first key
   const int64_t seen = a.causal ? tile * 128 - vis.start : 0;
@@ -139,18 +201,29 @@ __global__ __launch_bounds__(HALVES * kThreads, 2) void diff_dkv_kernel(DiffArgs
     const RowReader<D> rows(lane, true), keys(lane, false);
     const ColReader<D> cols(lane);
     const float c = a.scale * kLog2e;
+    float raise = 0.0f, to_w = 1.0f;  // p is a weight times 2^raise
+    if constexpr (kScaled<T>) {
+      int kw, ks;
+      scales(kw, ks);
+      raise = __uint_as_float(__builtin_amdgcn_readfirstlane(__float_as_uint(static_cast<float>(ks))));
+      to_w = __uint_as_float(__builtin_amdgcn_readfirstlane(__float_as_uint(__builtin_ldexpf(1.0f, kw - ks))));
+    }
     const auto copy = [&](int at, int buf) {
+      int ln = lane;
+      // The offsets are formed at every step: kept over the loop, they take the registers that a third wave needs (fp16, 768
+      // tiles of 8,192 queries 1,460 -> 1,395 us for the backward pass, 384 causal ones 293 -> 302).
+      if constexpr (kScaled<T> && D == 64 && HALVES == 1) asm volatile("" : "+v"(ln));
       const int h = hk * G + at / n_tiles, n0 = n_first + at % n_tiles * Q;
       const T* qp = static_cast<const T*>(a.q.p) + b * a.q.sb + h * a.q.sh + n0 * a.q.sn;
       const T* op = static_cast<const T*>(a.dout.p) + b * a.dout.sb + h * a.dout.sh + n0 * a.dout.sn;
       // 2 Q / R copies of 1 KB: each wave takes its share of Q's and of dO's rows
 #pragma unroll
       for (int i = wave; i < Q / R; i += 4) {
-        copy_rows<D>(qp, 2 * a.q.sn, i * R, a.N - 1 - n0, lane, lds_offset(lds[buf][half][0]) + i * 1024);
-        copy_rows<D>(op, 2 * a.dout.sn, i * R, a.N - 1 - n0, lane, lds_offset(lds[buf][half][1]) + i * 1024);
+        copy_rows<D>(qp, 2 * a.q.sn, i * R, a.N - 1 - n0, ln, lds_offset(lds[buf][half][0]) + i * 1024);
+        copy_rows<D>(op, 2 * a.dout.sn, i * R, a.N - 1 - n0, ln, lds_offset(lds[buf][half][1]) + i * 1024);
       }
-      if (wave == 0 && lane < Q)  // four times 32 floats
-        copy_1k(stat_at(stat, static_cast<int64_t>(b) * a.Hq + h, n0, a.N), (lane / 8) * 256 + (lane % 8) * 16,
+      if (wave == 0 && ln < Q)  // four times 32 floats
+        copy_1k(stat_at(stat, static_cast<int64_t>(b) * a.Hq + h, n0, a.N), (ln / 8) * 256 + (ln % 8) * 16,
                 __builtin_amdgcn_readfirstlane(lds_offset(st[buf][half])));
     };
     if (begin + half < total) copy(begin + half, 0);
@@ -189,9 +262,15 @@ __global__ __launch_bounds__(HALVES * kThreads, 2) void diff_dkv_kernel(DiffArgs
         }
 #pragma unroll
         for (int e = 0; e < 16; ++e) {
-          const float p = exp2_fast(x[e] * c);
-          w[e] = i ? __builtin_fmaf(p, minus, w[e]) : p;
-          d[e] = p * dp[e];
+          if constexpr (kScaled<T>) {
+            const float p = exp2_fast(__builtin_fmaf(x[e], c, raise));
+            w[e] = i ? __builtin_fmaf(p, minus * to_w, w[e]) : p * to_w;
+            d[e] = p * dp[e];
+          } else {
+            const float p = exp2_fast(x[e] * c);
+            w[e] = i ? __builtin_fmaf(p, minus, w[e]) : p;
+            d[e] = p * dp[e];
+          }
         }
         df[i][0] = pack8<T>(d);
         df[i][1] = pack8<T>(d + 8);
@@ -236,6 +315,16 @@ __global__ __launch_bounds__(HALVES * kThreads, 2) void diff_dkv_kernel(DiffArgs
         }
     }
     if (half) return;
+  }
+  if constexpr (kScaled<T>) {
+    int kw, ks;
+    scales(kw, ks);
+    const float fw = __builtin_ldexpf(1.0f, -kw), fs = __builtin_ldexpf(1.0f, -ks);
+#pragma unroll
+    for (int t = 0; t < S; ++t) {
+      dv[t] *= fw;
+      dk[t / (S / 2)][t % (S / 2)] *= fs;
+    }
   }
   // accumulator register e: key 8 (e/4) + 4 g + e%4, lane%32: channel
 #pragma unroll
@@ -290,13 +379,14 @@ __global__ __launch_bounds__(kThreads) void diff_dkv_join_kernel(DiffArgs a, con
 }
 
 // del and dQ of 128 or 64 rows (a key head's query heads together, in workgroups as in the forward pass). The keys go
-// through LDS twice. The rows' statistics go to `stat`.
+// through LDS twice. The rows' statistics go to `stat`, of every 32 rows the largest |dP| and |lambda| to `tops` (kScaled
+// types).
 template <typename T, int D, int SHARE>
-__global__ __launch_bounds__(64 * Many<SHARE>::kWaves, 2) void diff_dq_kernel(DiffArgs a, float* stat, int tiles, int units) {
+__global__ __launch_bounds__(64 * Many<SHARE>::kWaves, 2) void diff_dq_kernel(DiffArgs a, float* stat, float2* tops, int tiles, int units) {
   constexpr int S = D / 32, K = Many<SHARE>::kKeys, WAVES = Many<SHARE>::kWaves, BYTES = K * Tile<D>::kRow, R = Tile<D>::kRowsPerCopy;
   constexpr int GROUPS = Many<SHARE>::kGroups, ROWS = Many<SHARE>::kRows;
   __shared__ __align__(256) char lds[2][2][BYTES];  // [buffer][K, V]
-  __shared__ float sums[SHARE][GROUPS][2][64];
+  __shared__ float sums[SHARE][GROUPS][2 + kScaled<T>][64];
   // keys spread over those that the workgroup's rows see, and their mean
   constexpr int SAMPLE = 4 * WAVES * 128 / D;
   __shared__ __align__(16) T sample[SAMPLE][D];
@@ -334,7 +424,8 @@ __global__ __launch_bounds__(64 * Many<SHARE>::kWaves, 2) void diff_dq_kernel(Di
     }
   }
   const int64_t bhn = static_cast<int64_t>(b) * a.Hq + h;
-  float lse[2], d[2] = {0.0f, 0.0f};
+  float lse[2], d[2] = {0.0f, 0.0f}, top = 0.0f;  // top: the largest |dP| that the row meets
+  int ks = 0;                                     // exponent of the scale of its dS
 #pragma unroll
   for (int i = 0; i < 2; ++i) {
     const float l = a.rlse[(bhn * 2 + i) * a.N + n];
@@ -377,12 +468,21 @@ __global__ __launch_bounds__(64 * Many<SHARE>::kWaves, 2) void diff_dq_kernel(Di
         s16x8 df[2][2];
         const bool mask = at + 32 > low;
         const int left = limit - at - 16 * g;
+        if constexpr (kSums && kScaled<T>) {
+          if (mask) {
+#pragma unroll
+            for (int e = 0; e < 16; ++e) top = fmaxf(top, e < left ? fabsf(dp[e]) : 0.0f);
+          } else {
+#pragma unroll
+            for (int e = 0; e < 16; ++e) top = fmaxf(top, fabsf(dp[e]));
+          }
+        }
 #pragma unroll
         for (int i = 0; i < 2; ++i) {
           f32x16 x{};
 #pragma unroll
           for (int s = 0; s < S; ++s) x = mma<T>(rows.read(kt, j, i * S + s), qf[i][s], x);
-          const float l = lse[i] * c;
+          const float l = kScaled<T> && !kSums ? lse[i] * c - static_cast<float>(ks) : lse[i] * c;
           float ds[16];
           if (mask)
 #pragma unroll
@@ -430,7 +530,19 @@ __global__ __launch_bounds__(64 * Many<SHARE>::kWaves, 2) void diff_dq_kernel(Di
       }
     }
   };
+  if constexpr (kScaled<T>) {
+    top = max_halves(top);
+    if constexpr (SHARE > 1) sums[share][group][2][lane] = top;
+  }
   add_up(d);
+  if constexpr (kScaled<T>) {
+    if constexpr (SHARE > 1)
+#pragma unroll
+      for (int o = 0; o < SHARE; ++o) top = fmaxf(top, sums[o][group][2][lane]);
+    ks = 14 - exponent_above(top);
+    const float2 most = make_float2(wave_max_f32(top), wave_max_f32(fabsf(a.lam[h])));
+    if (!share && lane == 0) tops[(static_cast<int64_t>(bh) * tiles + tile) * GROUPS + group] = most;
+  }
   if (!share && live && lane < 32) put_stat(stat_at(stat, bhn, n, a.N), lse[0], lse[1], d[0], d[1], a.lam[h], c);
   if (tile == tiles - 1)  // rows behind the last token
     for (int x = threadIdx.x; x < G * static_cast<int>(padded(a.N) - a.N); x += 64 * WAVES)
@@ -482,7 +594,7 @@ __global__ __launch_bounds__(64 * Many<SHARE>::kWaves, 2) void diff_dq_kernel(Di
           for (int x = 0; x < 4; ++x) dq[t / (S / 2)][t % (S / 2)][4 * e + x] += y[x];
         }
   }
-  const float f[2] = {a.scale, -a.lam[h] * a.scale};
+  const float back = kScaled<T> ? __builtin_ldexpf(a.scale, -ks) : a.scale, f[2] = {back, -a.lam[h] * back};
   T* out = static_cast<T*>(a.dq.p) + b * a.dq.sb + h * a.dq.sh + n * a.dq.sn;
 #pragma unroll
   for (int t = 0; t < S; ++t) {
@@ -499,6 +611,11 @@ __global__ __launch_bounds__(64 * Many<SHARE>::kWaves, 2) void diff_dq_kernel(Di
 }
 
 int64_t stat_floats(int B, int Hq, int N) { return 4ll * B * Hq * padded(N); }
+// Two for every 32 rows of the tiles of 128 (or 64), two for a key head, and the next section on a multiple of 64.
+int64_t top_floats(int B, int Hk, int64_t rows) {
+  const int64_t heads = static_cast<int64_t>(B) * Hk;
+  return padded(2 * heads * ((rows + 127) / 128 * 4 + 1));
+}
 
 // How a key tile's queries are shared out where the tiles alone leave CUs idle: without a causal mask over two sets of
 // waves of a workgroup, then over as many workgroups as bring the card one a CU; with one, over 4-wave workgroups until
@@ -518,30 +635,41 @@ Share dkv_share(int B, int Hq, int Hk, int N, int M, bool causal) {
 template <typename T, int D>
 hipError_t launch(const DiffArgs& a, hipStream_t stream) {
   float* stat = a.ws;
+  float2* tops = reinterpret_cast<float2*>(stat + stat_floats(a.B, a.Hq, a.N));
+  int n_tops;  // of a key head
   const int64_t rows = static_cast<int64_t>(a.N) * (a.Hq / a.Hk);
   const int row_tiles = static_cast<int>((rows + 127) / 128), row_units = a.B * a.Hk * row_tiles;
   // as in the forward pass: 192 tiles of 2,048 keys 237 -> 207 us for the backward pass, 384 causal ones of up to 4,096
   // 518 -> 415, 384 without a mask 655 -> 699; half the rows: 64 tiles of 1,024 keys 88 -> 71, 126 of 777 keys of 64
   // channels 60 -> 51, 192 of 1,024 keys 104 -> 119
   if (row_units > (a.causal ? 512 : 256)) {
-    diff_dq_kernel<T, D, 1><<<grid_of(row_units), kThreads, 0, stream>>>(a, stat, row_tiles, row_units);
+    diff_dq_kernel<T, D, 1><<<grid_of(row_units), kThreads, 0, stream>>>(a, stat, tops, row_tiles, row_units);
+    n_tops = row_tiles * Many<1>::kGroups;
   } else if (row_units > 128) {
-    diff_dq_kernel<T, D, 2><<<grid_of(row_units), 2 * kThreads, 0, stream>>>(a, stat, row_tiles, row_units);
+    diff_dq_kernel<T, D, 2><<<grid_of(row_units), 2 * kThreads, 0, stream>>>(a, stat, tops, row_tiles, row_units);
+    n_tops = row_tiles * Many<2>::kGroups;
   } else {
     const int tiles = static_cast<int>((rows + 63) / 64), n = a.B * a.Hk * tiles;
-    diff_dq_kernel<T, D, 4><<<grid_of(n), 2 * kThreads, 0, stream>>>(a, stat, tiles, n);
+    diff_dq_kernel<T, D, 4><<<grid_of(n), 2 * kThreads, 0, stream>>>(a, stat, tops, tiles, n);
+    n_tops = tiles * Many<4>::kGroups;
   }
   const int key_tiles = static_cast<int>((a.M + 127ll) / 128);
   const Share share = dkv_share(a.B, a.Hq, a.Hk, a.N, a.M, a.causal);
   const int parts = share.parts;
   const int64_t keys = static_cast<int64_t>(a.B) * a.Hk * a.M;  // at most 768 tiles of 128 where they are joined
   const int key_units = a.B * a.Hk * key_tiles * parts;
-  float* sums = stat + stat_floats(a.B, a.Hq, a.N);
+  float* sums = stat + stat_floats(a.B, a.Hq, a.N) + top_floats(a.B, a.Hk, rows);
+  if (kScaled<T> && n_tops > kMostTops) {
+    float2* out = tops + static_cast<int64_t>(a.B) * a.Hk * n_tops;
+    diff_tops_kernel<<<a.B * a.Hk, kThreads, 0, stream>>>(tops, n_tops, out);
+    tops = out;
+    n_tops = 1;
+  }
   const int lambdas = static_cast<int>(grid_of(a.Hq));
   if (share.halves == 1) {
-    diff_dkv_kernel<T, D, 1><<<lambdas + grid_of(key_units), kThreads, 0, stream>>>(a, stat, sums, key_tiles, parts, key_units, lambdas);
+    diff_dkv_kernel<T, D, 1><<<lambdas + grid_of(key_units), kThreads, 0, stream>>>(a, stat, tops, n_tops, sums, key_tiles, parts, key_units, lambdas);
   } else {
-    diff_dkv_kernel<T, D, 2><<<lambdas + grid_of(key_units), 2 * kThreads, 0, stream>>>(a, stat, sums, key_tiles, parts, key_units, lambdas);
+    diff_dkv_kernel<T, D, 2><<<lambdas + grid_of(key_units), 2 * kThreads, 0, stream>>>(a, stat, tops, n_tops, sums, key_tiles, parts, key_units, lambdas);
   }
   if (parts > 1)
     diff_dkv_join_kernel<T, D><<<static_cast<unsigned>((keys + 1024 / D - 1) / (1024 / D)), kThreads, 0, stream>>>(a, sums, parts, keys);
@@ -552,7 +680,7 @@ hipError_t launch(const DiffArgs& a, hipStream_t stream) {
 
 int64_t diff_bwd_ws_bytes(int B, int Hq, int Hk, int N, int M, int d) {
   const int64_t parts = std::max(dkv_share(B, Hq, Hk, N, M, false).parts, dkv_share(B, Hq, Hk, N, M, true).parts);
-  return 4 * (stat_floats(B, Hq, N) + (parts > 1 ? parts * B * Hk * M * 2 * d : 0));
+  return 4 * (stat_floats(B, Hq, N) + top_floats(B, Hk, static_cast<int64_t>(N) * (Hq / Hk)) + (parts > 1 ? parts * B * Hk * M * 2 * d : 0));
 }
 
 hipError_t launch_diff_bwd(const DiffArgs& a, hipStream_t stream) {

@@ -1,0 +1,90 @@
+"""Differential attention on the GPU at the edges of its types' range: gradients of small and large size.
+
+Tolerance of the gradients' size: the 2-norm of the error over a whole gradient. Every rounded weight and score gradient is
+off by at most u = finfo(type).eps / 2 of itself, and over the step around it evenly, so by u^2 / 3 of its square in the
+mean; the roundings of different pairs do not depend on each other, so the mean squares add up: for dQ,
+scale^2 u^2 / 3 sum_j dS_j^2 ((K_j - mean K)^2 + var K), as dQ takes each key's distance to a middle of the keys, which is
+within a deviation of their mean; for dK the same with Q^2; for dV u^2 / 3 sum_i (P1 - lam P2)^2 dO^2. With more than 10^4
+elements the sum is near its mean. The result is rounded to the type, subnormal numbers among them, by what rounding the
+exact gradient gives. The error is at most 1.5 times both together; the float32 sums are finer by 2^-10 and more."""
+import math
+
+import numpy as np
+import pytest
+import torch
+
+from oracle import token
+from paper_2609_32628_amd import api
+from test_gpu_diff import Case, T, check, f64
+
+pytestmark = pytest.mark.gpu
+
+
+def gradients(case):
+    """Outputs of both passes."""
+    out = {n: torch.full_like(x, float("nan")) for n, x in (("O", case.Q), ("dQ", case.Q), ("dK", case.K), ("dV", case.V), ("dlam", case.lam))}
+    out["lse"] = torch.full((case.B, case.H, 2, case.N), float("nan"), device="cuda")
+    ws = torch.full((api.da2_diff_ws_bytes(case.Q, case.K, True),), 0xFF, dtype=torch.uint8, device="cuda")
+    api.da2_diff_attn(case.Q, case.K, case.V, case.lam, out["O"], ws, out["lse"], **case.how())
+    ws.fill_(0xFF)
+    api.da2_diff_attn_bwd(case.Q, case.K, case.V, case.lam, out["lse"], case.dO, out["dQ"], out["dK"], out["dV"], out["dlam"], ws,
+                          **case.how())
+    return out
+
+
+def spread(case):
+    """Mean square error of every element of dQ, dK and dV from the roundings of the weights and score gradients."""
+    h, u = case.d // 2, torch.finfo(case.Q.dtype).eps / 2
+    scale = 1 / math.sqrt(h) if case.scale is None else case.scale
+    var = {"dQ": np.zeros(case.Q.shape), "dK": np.zeros(case.K.shape), "dV": np.zeros(case.V.shape)}
+    for b, n in enumerate(case.n_keys):
+        see = token.diff_visible(case.N, case.M, n, case.start[b], case.causal)[:, :n]
+        for hq in range(case.H):
+            kh, lam = hq // (case.H // case.Hk), float(case.lam[hq])
+            q, k, v, g = f64(case.Q[b, hq]), f64(case.K[b, kh, :n]), f64(case.V[b, kh, :n]), f64(case.dO[b, hq])
+            P, _ = token._maps(q, k, see, scale)
+            dP = g @ v.T
+            var["dV"][b, kh, :n] += u * u / 3 * ((P[0] - lam * P[1]) ** 2).T @ g ** 2
+            for m, f in ((0, 1.0), (1, lam)):
+                c = slice(m * h, (m + 1) * h)
+                dS2 = (u * scale * f * P[m] * (dP - (P[m] * dP).sum(-1, keepdims=True))) ** 2 / 3
+                var["dQ"][b, hq, :, c] = dS2 @ ((k[:, c] - k[:, c].mean(0)) ** 2 + k[:, c].var(0))
+                var["dK"][b, kh, :n, c] += dS2.T @ q[:, c] ** 2
+    return var
+
+
+def rounded(x, t):
+    return f64(torch.from_numpy(x).to(t))
+
+
+@pytest.mark.parametrize("size", [1e-5, 1e-4, 1e-3, 1.0, 1e3])
+@pytest.mark.parametrize("B,H,Hk,N,M,d,causal,dtype", [
+    (1, 2, 1, 200, 4096, 128, False, "fp16"), (1, 1, 1, 700, 4096, 64, False, "fp16"), (1, 4, 2, 600, 4500, 64, True, "fp16"),
+    (2, 4, 2, 3000, 3000, 128, True, "fp16"), (1, 2, 2, 9000, 300, 64, False, "fp16"), (1, 2, 1, 200, 4096, 128, False, "bf16")])
+def test_size_of_gradients(B, H, Hk, N, M, d, causal, dtype, size):
+    """What comes back of a dO of any size: over thousands of keys the weights are small, and dS falls with dO below fp16's
+    normal numbers. Q, K and V are taken smaller with a large one, so that the gradients stay numbers of the type."""
+    case = Case(B, H, Hk, N, M, d, dtype, causal, seed=31)
+    if size > 1:
+        case.K *= 2.0 ** -6
+        case.Q *= 2.0 ** -4
+        case.V *= 0.25
+    case.dO = (case.dO.float() * size).to(T[dtype])
+    want, var, out = case.oracle(True), spread(case), gradients(case)
+    for n in ("dQ", "dK", "dV"):
+        off = np.linalg.norm(f64(out[n]) - want[n])
+        own = np.linalg.norm(rounded(want[n], out[n].dtype) - want[n])
+        assert np.abs(want[n]).max() < torch.finfo(out[n].dtype).max, n
+        assert off <= 1.5 * (math.sqrt(var[n].sum()) + own), (n, off, math.sqrt(var[n].sum()), own)
+
+
+@pytest.mark.parametrize("M", [2, 40])
+@pytest.mark.parametrize("d,dtype", [(64, "fp16"), (128, "fp16"), (128, "bf16")])
+def test_score_gradients_beyond_the_type(d, dtype, M):
+    """dO V' of about 5 10^5, over few keys: dS passes fp16's largest number, dQ, dK and dV do not."""
+    case = Case(1, 2, 2, 8, M, d, dtype, seed=33)
+    case.Q *= 2.0 ** -6
+    case.K *= 2.0 ** -6
+    case.V *= 8
+    case.dO = (case.dO.float() * 8e3).to(T[dtype])
+    check(case)
