@@ -1,4 +1,5 @@
-"""Differential attention on the GPU at the edges of its types' range: gradients of small and large size.
+"""Differential attention on the GPU at the edges of its types' range: gradients of small and large size, keys of which one
+is far from the others.
 
 Tolerance of the gradients' size: the 2-norm of the error over a whole gradient. Every rounded weight and score gradient is
 off by at most u = finfo(type).eps / 2 of itself, and over the step around it evenly, so by u^2 / 3 of its square in the
@@ -32,8 +33,9 @@ def gradients(case):
     return out
 
 
-def spread(case):
-    """Mean square error of every element of dQ, dK and dV from the roundings of the weights and score gradients."""
+def spread(case, first=0):
+    """Mean square error of every element of dQ, dK and dV from the roundings of the weights and score gradients; the keys
+    before ``first`` are not counted among those whose middle dQ takes."""
     h, u = case.d // 2, torch.finfo(case.Q.dtype).eps / 2
     scale = 1 / math.sqrt(h) if case.scale is None else case.scale
     var = {"dQ": np.zeros(case.Q.shape), "dK": np.zeros(case.K.shape), "dV": np.zeros(case.V.shape)}
@@ -48,7 +50,7 @@ def spread(case):
             for m, f in ((0, 1.0), (1, lam)):
                 c = slice(m * h, (m + 1) * h)
                 dS2 = (u * scale * f * P[m] * (dP - (P[m] * dP).sum(-1, keepdims=True))) ** 2 / 3
-                var["dQ"][b, hq, :, c] = dS2 @ ((k[:, c] - k[:, c].mean(0)) ** 2 + k[:, c].var(0))
+                var["dQ"][b, hq, :, c] = dS2 @ ((k[:, c] - k[first:, c].mean(0)) ** 2 + k[first:, c].var(0))
                 var["dK"][b, kh, :n, c] += dS2.T @ q[:, c] ** 2
     return var
 
@@ -88,3 +90,18 @@ def test_score_gradients_beyond_the_type(d, dtype, M):
     case.V *= 8
     case.dO = (case.dO.float() * 8e3).to(T[dtype])
     check(case)
+
+
+@pytest.mark.parametrize("H,N,M,d,dtype", [(2, 130, 2048, 128, "bf16"), (2, 130, 2048, 64, "fp16"), (2, 9000, 400, 128, "bf16"), (40, 900, 300, 64, "bf16"),
+                                           (36, 1000, 300, 128, "fp16")])
+def test_a_large_first_key(H, N, M, d, dtype):
+    """A first key 400 times as large as the others, which no query attends to: its weight, and with it what its dS is off,
+    is zero, so dQ is as exact as without it."""
+    case = Case(1, H, H, N, M, d, dtype, seed=35)
+    case.Q += 1.5                # its distance from the other keys is along minus the queries' mean
+    case.K[:, :, 0] = -400
+    want, var, out = case.oracle(True), spread(case, 1), gradients(case)
+    for n in ("dQ", "dK", "dV"):
+        off = np.linalg.norm(f64(out[n]) - want[n])
+        own = np.linalg.norm(rounded(want[n], out[n].dtype) - want[n])
+        assert off <= 1.5 * (math.sqrt(var[n].sum()) + own), (n, off, math.sqrt(var[n].sum()), own)
