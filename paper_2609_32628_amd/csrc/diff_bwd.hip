@@ -433,7 +433,7 @@ __global__ __launch_bounds__(64 * Many<SHARE>::kWaves, 2) void diff_dq_kernel(Di
 #pragma unroll
   for (int i = 0; i < 2; ++i) {
     const float l = a.rlse[(bhn * 2 + i) * a.N + n];
-    lse[i] = l == -__builtin_inff() ? kNever : l / a.scale;
+    lse[i] = l == -__builtin_inff() ? kNever : l * kLog2e;
   }
   f32x16 dq[2][S / 2];
   float rest[2] = {0.0f, 0.0f};  // sums of the rounded dS of each map
@@ -486,7 +486,7 @@ __global__ __launch_bounds__(64 * Many<SHARE>::kWaves, 2) void diff_dq_kernel(Di
           f32x16 x{};
 #pragma unroll
           for (int s = 0; s < S; ++s) x = mma<T>(rows.read(kt, j, i * S + s), qf[i][s], x);
-          const float l = kScaled<T> && !kSums ? lse[i] * c - static_cast<float>(ks) : lse[i] * c;
+          const float l = kScaled<T> && !kSums ? lse[i] - static_cast<float>(ks) : lse[i];
           float ds[16];
           if (mask)
 #pragma unroll
@@ -547,7 +547,7 @@ __global__ __launch_bounds__(64 * Many<SHARE>::kWaves, 2) void diff_dq_kernel(Di
     const float2 most = make_float2(wave_max_f32(top), wave_max_f32(fabsf(a.lam[h])));
     if (!share && lane == 0) tops[(static_cast<int64_t>(bh) * tiles + tile) * GROUPS + group] = most;
   }
-  if (!share && live && lane < 32) put_stat(stat_at(stat, bhn, n, a.N), lse[0], lse[1], d[0], d[1], a.lam[h], c);
+  if (!share && live && lane < 32) put_stat(stat_at(stat, bhn, n, a.N), lse[0] / c, lse[1] / c, d[0], d[1], a.lam[h], c);
   if (tile == tiles - 1)  // rows behind the last token
     for (int x = threadIdx.x; x < G * static_cast<int>(padded(a.N) - a.N); x += 64 * WAVES)
       put_stat(stat_at(stat, static_cast<int64_t>(b) * a.Hq + hk * G + x % G, a.N + x / G, a.N), kNever, kNever, 0.0f, 0.0f, 1.0f, 1.0f);
