@@ -487,7 +487,7 @@ __global__ __launch_bounds__(64 * Many<SHARE>::kWaves, 2) void diff_dq_kernel(Di
 #pragma unroll
           for (int s = 0; s < S; ++s) x = mma<T>(rows.read(kt, j, i * S + s), qf[i][s], x);
           const float l = kScaled<T> && !kSums ? lse[i] - static_cast<float>(ks) : lse[i];
-          float ds[16];
+          float ds[16], sum = 0.0f;  // of P dP over 16 keys
           if (mask)
 #pragma unroll
             for (int e = 0; e < 16; ++e) x[e] = e < left ? x[e] : -__builtin_inff();
@@ -495,12 +495,14 @@ __global__ __launch_bounds__(64 * Many<SHARE>::kWaves, 2) void diff_dq_kernel(Di
           for (int e = 0; e < 16; ++e) {
             const float p = exp2_fast(__builtin_fmaf(x[e], c, -l));
             if constexpr (kSums) {
-              d[i] = __builtin_fmaf(p, dp[e], d[i]);
+              sum = __builtin_fmaf(p, dp[e], sum);
             } else {
               ds[e] = p * (dp[e] - d[i]);
             }
           }
-          if constexpr (!kSums) {
+          if constexpr (kSums) {
+            d[i] += sum;
+          } else {
             df[i][0] = pack8<T>(ds);
             df[i][1] = pack8<T>(ds + 8);
             rest[i] = add8<T>(df[i][1], add8<T>(df[i][0], rest[i]));

@@ -127,10 +127,8 @@ struct Rows32 {
     for (int i = 0; i < 2; ++i) {
       float w[16];
 #pragma unroll
-      for (int e = 0; e < 16; ++e) {
-        w[e] = exp2_fast(__builtin_fmaf(x[i][e], c, -m[i]));
-        l[i] += w[e];
-      }
+      for (int e = 0; e < 16; ++e) w[e] = exp2_fast(__builtin_fmaf(x[i][e], c, -m[i]));
+      l[i] += sum16(w);
       p[i][0] = pack8<T>(w);
       p[i][1] = pack8<T>(w + 8);
     }

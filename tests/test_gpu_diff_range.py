@@ -1,5 +1,5 @@
 """Differential attention on the GPU at the edges of its types' range: gradients of small and large size, keys of which one
-is far from the others.
+is far from the others, rows of very many small weights.
 
 Tolerance of the gradients' size: the 2-norm of the error over a whole gradient. Every rounded weight and score gradient is
 off by at most u = finfo(type).eps / 2 of itself, and over the step around it evenly, so by u^2 / 3 of its square in the
@@ -105,3 +105,27 @@ def test_a_large_first_key(H, N, M, d, dtype):
         off = np.linalg.norm(f64(out[n]) - want[n])
         own = np.linalg.norm(rounded(want[n], out[n].dtype) - want[n])
         assert off <= 1.5 * (math.sqrt(var[n].sum()) + own), (n, off, math.sqrt(var[n].sum()), own)
+
+
+def many_keys(N, dtype, bits):
+    """O and lse of one key with a value of zero before 2^17 others with one, each of 2^-bits of its weight. There are heads
+    enough that none of them is split; they share the keys' memory."""
+    M, d = 2 ** 17, 64
+    Q = torch.zeros(1, 256, N, d, dtype=T[dtype], device="cuda")
+    K, V = (torch.zeros(1, 1, M, d, dtype=T[dtype], device="cuda") for _ in range(2))
+    Q[..., 0], K[:, :, 0, 0], V[:, :, 1:] = 1, 1, 1
+    out, lse = torch.full_like(Q, float("nan")), torch.full((1, 256, 2, N), float("nan"), device="cuda")
+    K, V = K.expand(1, 256, M, d), V.expand(1, 256, M, d)
+    ws = torch.empty(max(api.da2_diff_ws_bytes(Q, K), 1), dtype=torch.uint8, device="cuda")
+    api.da2_diff_attn(Q, K, V, torch.zeros(256, device="cuda"), out, ws, lse, scale=bits * math.log(2))
+    return out.double(), lse[0, :, 0].double(), M
+
+
+@pytest.mark.parametrize("N", [1, 128, 600])
+@pytest.mark.parametrize("bits,dtype", [(8.5, "fp16"), (20.5, "fp16"), (20.5, "bf16"), (25.5, "bf16")])
+def test_a_sum_of_many_small_weights(bits, dtype, N):
+    """A sum of M weights has M/16 + 40 additions in a chain, each off by 2^-24 of the sum; the logarithm adds the weights'
+    own errors and a few steps of its size."""
+    _, lse, M = many_keys(N, dtype, bits)
+    want = bits * math.log(2) + math.log1p((M - 1) * 2.0 ** -bits)
+    assert (lse - want).abs().max() <= (M / 16 + 40) * 2.0 ** -24 + 2.0 ** -20 + 4 * 2.0 ** -24 * want
