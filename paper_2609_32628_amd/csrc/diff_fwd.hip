@@ -66,6 +66,10 @@ template <typename T, int D>
 struct Rows32 {
   static constexpr int S = D / 32;  // 16-channel steps of a map
   static constexpr int C = D / 32;  // 32-channel tiles of V
+  // A key's weight is 2^(score - m); a new maximum's is 2^kTop, and the largest 2^kMost. Weights are rounded to T: fp16 has
+  // numbers up to 2^15 but few below 2^-14, which a long row's many small weights are (2^17 keys 2^-25 each of the first
+  // one's weight, 0.3% of the row together, came out as zeros).
+  static constexpr float kTop = __is_same(T, fp16_t) ? 11.0f : 0.0f, kMost = __is_same(T, fp16_t) ? 15.0f : 8.0f;
   s16x8 q[2][S];
   f32x16 u[2][C];
   float m[2], l[2];
@@ -105,16 +109,16 @@ struct Rows32 {
         for (int e = 0; e < 16; ++e) x[i][e] = e < left ? x[i][e] : -__builtin_inff();
     }
   }
-  // The maximum is a reference for the exponentials only: it follows when a score passes it by 2^8, which the weights'
-  // float32 sums and 16-bit values hold, so that the accumulators are rarely rescaled.
+  // The maximum is a reference for the exponentials only: it follows when a weight would pass 2^kMost, up to which the
+  // weights' float32 sums and 16-bit values hold them, so that the accumulators are rarely rescaled.
   __device__ void follow(const f32x16 (&x)[2], float c) {
     float top[2];
 #pragma unroll
     for (int i = 0; i < 2; ++i) top[i] = max_halves(max16(x[i])) * c;
-    if (__any(top[0] > m[0] + 8.0f || top[1] > m[1] + 8.0f)) {
+    if (__any(top[0] > m[0] + kMost || top[1] > m[1] + kMost)) {
 #pragma unroll
       for (int i = 0; i < 2; ++i) {
-        const float to = fmaxf(m[i], top[i]), f = exp2_fast(m[i] - to);
+        const float to = fmaxf(m[i], top[i] - kTop), f = exp2_fast(m[i] - to);
         m[i] = to;
         l[i] *= f;
 #pragma unroll

@@ -129,3 +129,17 @@ def test_a_sum_of_many_small_weights(bits, dtype, N):
     _, lse, M = many_keys(N, dtype, bits)
     want = bits * math.log(2) + math.log1p((M - 1) * 2.0 ** -bits)
     assert (lse - want).abs().max() <= (M / 16 + 40) * 2.0 ** -24 + 2.0 ** -20 + 4 * 2.0 ** -24 * want
+
+
+@pytest.mark.parametrize("N", [1, 128, 600])
+@pytest.mark.parametrize("bits,dtype", [(8.5, "fp16"), (20.5, "fp16"), (25.5, "fp16"), (30.5, "fp16"), (25.5, "bf16")])
+def test_many_small_weights(bits, dtype, N):
+    """The output is what the small weights come to together. Float32 sums of M weights are off by (M/16 + 40) 2^-24 of
+    themselves, twice (weights and values), weights and outputs by u each, and fp16's smallest weights by 2^-25 of 2^-11 of
+    the first key's each."""
+    out, _, M = many_keys(N, dtype, bits)
+    u = torch.finfo(T[dtype]).eps / 2
+    rest = (M - 1) * 2.0 ** -bits
+    want = rest / (1 + rest)
+    tol = (2 * u + 2 * (M / 16 + 40) * 2.0 ** -24) * want + (M * 2.0 ** -36 if dtype == "fp16" else 0)
+    assert (out - want).abs().max() <= tol
