@@ -162,9 +162,10 @@ __device__ inline T* row_ptr(const OutView& o, int b, int h, int n) {
   return static_cast<T*>(o.p) + b * o.sb + h * o.sh + n * o.sn;
 }
 
+// Only a sum without a key is the zero of all bits; by its bits, so that a NaN of the caller's stays one.
 __device__ inline void store_lse(const DiffArgs& a, int b, int h, int n, int i, float m, float l) {
   a.lse[((static_cast<int64_t>(b) * a.Hq + h) * 2 + i) * a.N + n] =
-      l > 0.0f ? kLn2 * (m + __builtin_amdgcn_logf(l)) : -__builtin_inff();
+      __float_as_uint(l) ? kLn2 * (m + __builtin_amdgcn_logf(l)) : -__builtin_inff();
 }
 
 // Output of one row from its accumulators as columns (see store_columns) and its whole sums l.

@@ -1,0 +1,65 @@
+"""Differential attention on the GPU: what a NaN of the caller's reaches, in every shape of workgroup."""
+import pytest
+import torch
+
+from paper_2609_32628_amd import api
+from test_gpu_diff import Case
+
+pytestmark = pytest.mark.gpu
+
+
+def forward(case):
+    out = torch.full_like(case.Q, 7.0)
+    lse = torch.full((case.B, case.H, 2, case.N), 7.0, device="cuda")
+    ws = torch.empty(max(api.da2_diff_ws_bytes(case.Q, case.K), 1), dtype=torch.uint8, device="cuda")
+    api.da2_diff_attn(case.Q, case.K, case.V, case.lam, out, ws, lse, **case.how())
+    return out, lse
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "fp16"])
+@pytest.mark.parametrize("B,H,Hk,N,M,d", [(2, 4, 2, 3, 90, 64), (1, 4, 2, 3, 3000, 128), (1, 2, 2, 100, 130, 128), (1, 2, 2, 100, 4096, 64),
+                                          (1, 130, 130, 150, 70, 64), (1, 260, 260, 150, 70, 128)])
+def test_a_nan_reaches_its_rows_and_no_others(B, H, Hk, N, M, d, dtype):
+    """Of a query: its row's output and the log sum of the map whose half holds it. Of a key: every row of its heads, and
+    the log sums of its half's map. Of a value: one channel. Everything else stays as it was, up to the roundings: the rows
+    of a wave follow their maxima together, so one row's weights are rounded elsewhere for another's NaN. An output is off
+    by u of sum (P1 + lam P2) |V| <= 1.8 max |V|, and by u of itself, which is no larger, in either call; a log sum by a few
+    2^-24 of its size."""
+    case = Case(B, H, Hk, N, M, d, dtype, seed=41)
+    u, top = torch.finfo(case.Q.dtype).eps / 2, float(case.V.abs().max())
+
+    def same(got, want):
+        tol = 2 * 2 * 1.8 * u * top if got.dtype != torch.float32 else 2.0 ** -19 + 2.0 ** -21 * want.abs()
+        assert ((got.float() - want.float()).abs() <= tol).all()
+
+    clean, clean_lse = forward(case)
+    G = H // Hk
+    case.Q[0, 1, N - 1, 5] = float("nan")
+    out, lse = forward(case)
+    row = torch.zeros(B, H, N, dtype=torch.bool, device="cuda")
+    row[0, 1, N - 1] = True
+    assert out[row].isnan().all()
+    same(out[~row], clean[~row])
+    hit = torch.zeros_like(lse, dtype=torch.bool)
+    hit[0, 1, 0, N - 1] = True
+    assert lse[hit].isnan().all()
+    same(lse[~hit], clean_lse[~hit])
+    case.Q[0, 1, N - 1, 5] = 0.5
+    clean, clean_lse = forward(case)
+    for key in (0, M // 2, M - 1):
+        was = case.K[0, 1, key, d - 3].clone()
+        case.K[0, 1, key, d - 3] = float("nan")
+        out, lse = forward(case)
+        case.K[0, 1, key, d - 3] = was
+        row = torch.zeros(B, H, N, dtype=torch.bool, device="cuda")
+        row[0, G:2 * G] = True
+        assert out[row].isnan().all()
+        same(out[~row], clean[~row])
+        assert lse[0, G:2 * G, 1].isnan().all()
+        lse[0, G:2 * G, 1] = clean_lse[0, G:2 * G, 1]
+        same(lse, clean_lse)
+    case.V[0, 1, M // 3, 9] = float("nan")
+    out, lse = forward(case)
+    assert out[0, G:2 * G, :, 9].isnan().all() and torch.equal(lse, clean_lse)
+    out[0, G:2 * G, :, 9] = clean[0, G:2 * G, :, 9]
+    assert torch.equal(out, clean)
