@@ -1,9 +1,11 @@
-"""Differential attention on the GPU: what a NaN of the caller's reaches, in every shape of workgroup."""
+"""Differential attention on the GPU: what a NaN of the caller's reaches, in every shape of workgroup; lambdas of any sign
+and size; and every way in which the backward pass shares a key tile's queries out."""
 import pytest
 import torch
 
+from oracle import token
 from paper_2609_32628_amd import api
-from test_gpu_diff import Case
+from test_gpu_diff import Case, check, f64
 
 pytestmark = pytest.mark.gpu
 
@@ -63,3 +65,45 @@ def test_a_nan_reaches_its_rows_and_no_others(B, H, Hk, N, M, d, dtype):
     assert out[0, G:2 * G, :, 9].isnan().all() and torch.equal(lse, clean_lse)
     out[0, G:2 * G, :, 9] = clean[0, G:2 * G, :, 9]
     assert torch.equal(out, clean)
+
+
+class Signed(Case):
+    """Lambdas given; the bounds are those of their sizes, and dV's weights |P1 - lam P2| of a negative one are larger than
+    the bounds of its size count by 2 |lam| P2."""
+
+    def __init__(self, lam, *args, **kw):
+        super().__init__(*args, **kw)
+        self.lam = torch.tensor([lam[h % len(lam)] for h in range(self.H)], device="cuda")
+
+    def bounds(self, want, grads):
+        lam, self.lam = self.lam, self.lam.abs()
+        out = super().bounds(want, grads)
+        self.lam = lam
+        u, scale = torch.finfo(self.Q.dtype).eps / 2, (self.d // 2) ** -0.5 if self.scale is None else self.scale
+        for b, n in enumerate(self.n_keys):
+            if not grads or not n:
+                continue
+            see = token.diff_visible(self.N, self.M, n, self.start[b], self.causal)[:, :n]
+            for h in range(self.H):
+                kh = h // (self.H // self.Hk)
+                P, _ = token._maps(f64(self.Q[b, h]), f64(self.K[b, kh, :n]), see, scale)
+                out["dV"][b, kh, :n] += 2 * u * max(0.0, -float(lam[h])) * P[1].T @ abs(f64(self.dO[b, h]))
+        return out
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "fp16"])
+@pytest.mark.parametrize("d", [64, 128])
+@pytest.mark.parametrize("lam", [[-0.6, 0.0, 1.3, -2.5], [0.0], [-1.0, -1e-30, 40.0, -3000.0]])
+def test_lambdas_of_any_sign_and_size(lam, d, dtype):
+    """With shared heads, rows that see no key, a padded batch, few rows and many, and both masks."""
+    for causal in (True, False):
+        check(Signed(lam, 2, 4, 2, 75, 140, d, dtype, causal, [140, 90], [-3, 40], seed=51))
+        check(Signed(lam, 2, 8, 2, 3, 140, d, dtype, causal, [140, 0], [100, 0], seed=52))
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "fp16"])
+@pytest.mark.parametrize("H,Hk,N,M,d,causal", [(2, 2, 600, 300, 64, False), (6, 2, 333, 200, 128, False), (1, 1, 1030, 500, 128, False), (2, 1, 600, 600, 64, True),
+                                               (6, 2, 333, 333, 128, True), (260, 260, 40, 70, 64, False)])
+def test_shared_out_queries(H, Hk, N, M, d, causal, dtype):
+    """Parts of the queries over workgroups, with two sets of waves each (no mask) and one; and two sets and one without parts."""
+    check(Signed([0.5, -0.4, 0.0], 1, H, Hk, N, M, d, dtype, causal, seed=53))
