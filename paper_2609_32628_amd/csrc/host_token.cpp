@@ -44,6 +44,8 @@ int32_t check_view(const da2_tensor* t, const Ext& e, int32_t dtype, bool out) {
   for (const auto& s : d) {
     if (s.second == 1) continue;
     if (s.first < span) return DA2_ERR_INVALID_ARG;
+    // no memory holds more elements than that, and no later stride could be as large
+    if (s.first > ((1ll << 60) - span) / (s.second - 1)) return DA2_ERR_INVALID_ARG;
     span += s.first * (s.second - 1);
   }
   return DA2_OK;
