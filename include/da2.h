@@ -387,6 +387,7 @@ typedef struct {
 /* Row norm: y = (x - mean) rstd f + b over the C channels of each row, with
  * rstd = 1 / sqrt(var + eps), var the mean of (x - mean)^2, and f = w or 1 + w;
  * DA2_NORM_RMS takes mean = 0.
+ * B*H*N is at most 2^31 - 1 and C at most 2^24.
  *   X      device, rows *r per *x; Y device out per *y, of X's dtype (may be X)
  *   w, b   device, per *n, or NULL: factor 1, no bias
  *   stats  device out, float32 [B*H*N][2]: mean and rstd of each row (row
@@ -470,7 +471,8 @@ typedef struct {
  *           per *qo and *ko, of that dtype (may be Q and K). K, Ko, k, ko are
  *           not looked at when Hk = 0.
  * Errors: INVALID_ARG for d not a multiple of block, rot > block, a d above
- * 65,536, or a grid that does not fit the axes. */
+ * 65,536, Hq + Hk above 65,535, B*N*block above 2^32 - 256, or a grid that does
+ * not fit the axes. */
 int32_t da2_rope(const da2_rope_desc* r, const double* turns, double scale, const int32_t* pos,
                  int64_t pos_stride_b, const da2_rope_rows* s, const void* Q, const da2_tensor* q,
                  void* Qo, const da2_tensor* qo, const void* K, const da2_tensor* k, void* Ko,
@@ -480,7 +482,9 @@ int32_t da2_rope(const da2_rope_desc* r, const double* turns, double scale, cons
  * of d/2 (its halves) that share the head's values:
  *   O = (softmax(scale Q1 K1^T) - lambda_h softmax(scale Q2 K2^T)) V.
  * Hq query heads share Hk key and value heads (Hq a multiple of Hk: query head h
- * reads key head h / (Hq/Hk)), N queries see M keys. */
+ * reads key head h / (Hq/Hk)), N queries see M keys. N and M are at most 2^30, and
+ * R = N Hq/Hk is below 2^31; B*Hk ceil(R / 32), and B*Hk ceil(M / 128) + 2 Hq + 1024,
+ * are at most 2^24 - 8; else INVALID_ARG. */
 typedef struct {
   int32_t B, Hq, Hk, N, M, d; /* d = 64 or 128, else DA2_ERR_UNSUPPORTED */
   int32_t causal;             /* 0 or 1, see q_start */
@@ -493,8 +497,8 @@ typedef struct {
 int32_t da2_diff_ws_bytes(const da2_diff_problem* p, int32_t train, int64_t* bytes);
 
 /* Forward pass. Tensors are bf16 or fp16, all of one dtype, with 16-byte
- * aligned bases and every stride a multiple of 8 elements; the stride_n of K
- * and V (and of Q, dO) is at most 2^24.
+ * aligned bases and every stride a multiple of 8 elements; the stride_n of the
+ * inputs (Q, K, V and dO) is at most 2^24.
  *   Q       device [B,Hq,N,d]; K, V device [B,Hk,M,d]
  *   lambda  device float32 [Hq]
  *   kv_lens device int32 [B] or NULL: sample b has its first kv_lens[b] keys

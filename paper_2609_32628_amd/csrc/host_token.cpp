@@ -121,19 +121,19 @@ int32_t check_diff(const da2_diff_problem* p, DiffExt* e) {
   if (p->Hq % p->Hk || (p->causal != 0 && p->causal != 1)) return DA2_ERR_INVALID_ARG;
   if (!(p->scale >= 0x1p-64 && p->scale <= 0x1p64)) return DA2_ERR_INVALID_ARG;
   if (p->d != 64 && p->d != 128) return DA2_ERR_UNSUPPORTED;
-  // positions in 32 bits; the launch grids end at 2^32 threads
+  // Positions in 32 bits. The launch grids end at 2^32 threads: row tiles of 256 threads; key tiles and the query heads'
+  // dlambda beside them, the latter with 512 threads where key tiles are few.
   const int64_t rows = (int64_t)p->N * (p->Hq / p->Hk);
   if (p->N > (1 << 30) || p->M > (1 << 30) || rows > (1ll << 31) - 1) return DA2_ERR_INVALID_ARG;
   const int64_t heads = (int64_t)p->B * p->Hk, most = (1 << 24) - 8;
-  if (heads * ((rows + 31) / 32) > most || heads * (((int64_t)p->M + 127) / 128) > most) return DA2_ERR_INVALID_ARG;
-  if ((int64_t)p->B * p->Hq * (((int64_t)p->N + 63) / 64 * 64) * (p->d / 8) > (1ll << 32) - 256)
+  if (heads * ((rows + 31) / 32) > most || heads * (((int64_t)p->M + 127) / 128) + 2ll * p->Hq + 1024 > most)
     return DA2_ERR_INVALID_ARG;
   return DA2_OK;
 }
 
 bool aligned16(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 15u) == 0; }
 
-// A tensor of the attention: 16-byte vectors, 64 rows within 32 bits of byte offset.
+// A tensor of the attention: 16-byte vectors; 128 rows of an input, as a tile has, within 32 bits of byte offset.
 int32_t check_attn(const void* p, const da2_tensor* t, const Ext& e, int32_t dtype, bool out) {
   if (!p || !aligned16(p)) return DA2_ERR_INVALID_ARG;
   const int32_t st = check_view(t, e, dtype, out);
@@ -141,7 +141,7 @@ int32_t check_attn(const void* p, const da2_tensor* t, const Ext& e, int32_t dty
   if (dtype == DA2_FP32) return DA2_ERR_UNSUPPORTED;
   if ((e.B > 1 && t->stride_b % 8) || (e.H > 1 && t->stride_h % 8) || (e.N > 1 && t->stride_n % 8))
     return DA2_ERR_INVALID_ARG;
-  return e.N > 1 && t->stride_n > (1 << 24) ? DA2_ERR_INVALID_ARG : DA2_OK;
+  return !out && e.N > 1 && t->stride_n > (1 << 24) ? DA2_ERR_INVALID_ARG : DA2_OK;
 }
 
 da2::DiffArgs diff_args(const da2_diff_problem* p, int32_t dtype) {
@@ -163,7 +163,7 @@ int64_t diff_ws(const da2_diff_problem* p, bool train) {
   return train ? std::max(f, da2::diff_bwd_ws_bytes(p->B, p->Hq, p->Hk, p->N, p->M, p->d)) : f;
 }
 
-// A stride of an extent of 1 is never multiplied by more than zero, but 64-row copies form row * stride in 32 bits.
+// A stride of an extent of 1 is never multiplied by more than zero, but the copies of tiles form row * stride in 32 bits.
 View attn_view(const void* p, const da2_tensor* t, const Ext& e) {
   return View{p, t->stride_b, t->stride_h, e.N > 1 ? t->stride_n : 0};
 }

@@ -107,3 +107,25 @@ def test_lambdas_of_any_sign_and_size(lam, d, dtype):
 def test_shared_out_queries(H, Hk, N, M, d, causal, dtype):
     """Parts of the queries over workgroups, with two sets of waves each (no mask) and one; and two sets and one without parts."""
     check(Signed([0.5, -0.4, 0.0], 1, H, Hk, N, M, d, dtype, causal, seed=53))
+
+
+@pytest.mark.parametrize("N", [3, 70])
+def test_outputs_that_lie_apart(N):
+    """Rows of O and of the gradients more than 2^24 elements from one another: the same bits as packed ones."""
+    case = Case(1, 2, 1, N, N, 64, "bf16", True, seed=55)
+    far = (1 << 24) + 8
+    room = torch.empty(N * far, dtype=torch.bfloat16, device="cuda")
+
+    def apart(like, at):
+        return room.as_strided(like.shape, (0, 64, far, 1), at)
+
+    def both(O, dQ, dK, dV):
+        lse, dlam = torch.empty(1, 2, 2, N, device="cuda"), torch.empty(2, device="cuda")
+        ws = torch.empty(api.da2_diff_ws_bytes(case.Q, case.K, True), dtype=torch.uint8, device="cuda")
+        api.da2_diff_attn(case.Q, case.K, case.V, case.lam, O, ws, lse, **case.how())
+        api.da2_diff_attn_bwd(case.Q, case.K, case.V, case.lam, lse, case.dO, dQ, dK, dV, dlam, ws, **case.how())
+        return O, dQ, dK, dV
+
+    want = both(*(torch.empty_like(x) for x in (case.Q, case.Q, case.K, case.K)))
+    got = both(apart(case.Q, 0), apart(case.Q, 128), apart(case.K, 256), apart(case.K, 320))
+    assert all(torch.equal(a, b) for a, b in zip(got, want))

@@ -20,3 +20,31 @@ def test_outputs_whose_spans_pass_64_bits_are_refused():
             x = _lib.Tensor(0, 0, 0, _lib.DA2_BF16, 0)
             n = _lib.NormDesc(0, _lib.DA2_FP32, 0, 0, 0, 1e-6)
             assert L.da2_norm(FAKE, x, _lib.Rows(2, 1, N, 64), n, None, None, 2 * FAKE, out, None, None) == E, (N, stride)
+
+
+def test_long_prompts_have_no_limit_but_the_launches():
+    L, b = _lib.lib(), ctypes.c_int64()
+    size = lambda **kw: L.da2_diff_ws_bytes(_lib.DiffProblem(*{**dict(B=1, Hq=1, Hk=1, N=1, M=1, d=128, causal=0, reserved=0, scale=0.1),  # noqa: E731
+                                                               **kw}.values()), 1, b)
+    for ok in (dict(N=(1 << 28) - 64), dict(N=(1 << 28) + 64), dict(N=(1 << 29) - 256, d=64), dict(Hq=1 << 22, N=100), dict(M=1 << 30),
+               dict(Hq=(1 << 23) - 600)):
+        assert size(**ok) == 0 and b.value >= 4 * 4 * ok.get("N", 1) * ok.get("Hq", 1), ok
+    for bad in (dict(N=1 << 29), dict(N=1 << 30), dict(N=(1 << 30) + 1), dict(M=(1 << 30) + 1), dict(Hq=1 << 23), dict(Hq=1 << 23, N=256), dict(Hq=2, N=1 << 30),
+                dict(Hq=2048, Hk=2048, M=1 << 30)):
+        assert size(**bad) == E, bad
+
+
+def test_outputs_may_lie_apart():
+    """Rows more than 2^24 elements apart are refused where a tile is copied from them, not where results are stored. (A CPU
+    has no device to launch on: what passes the checks is UNSUPPORTED.)"""
+    if torch.cuda.is_available():
+        pytest.skip("would launch")
+    L = _lib.lib()
+    p = _lib.DiffProblem(1, 1, 1, 5, 7, 64, 0, 0, 0.1)
+    q, k, far = (_lib.Tensor(0, 0, s, _lib.DA2_BF16, 0) for s in (64, 64, (1 << 24) + 8))
+    A = [FAKE * (i + 1) for i in range(8)]
+    call = lambda q, k, o: L.da2_diff_attn(p, A[0], q, A[1], k, A[2], k, FAKE, None, None, A[3], o, None, FAKE, 1 << 30, None)  # noqa: E731
+    assert call(q, k, far) == U and call(far, k, q) == E and call(q, far, q) == E
+    back = lambda q, do, dq, dk: L.da2_diff_attn_bwd(p, A[0], q, A[1], k, A[2], k, FAKE, None, None, FAKE, A[3], do, A[4], dq, A[5], dk, A[6],  # noqa: E731
+                                                     dk, FAKE, FAKE, 1 << 30, None)
+    assert back(q, q, far, far) == U and back(far, q, q, k) == E and back(q, far, q, k) == E
