@@ -220,7 +220,12 @@ def _addr(x):
 
 
 def _bytes(ws):
-    return 0 if ws is None else ws.numel() * ws.element_size()
+    """Bytes of a workspace; one that has gaps or repeats itself does not hold as many as its elements count."""
+    if ws is None:
+        return 0
+    if not ws.is_contiguous():
+        raise ValueError("ws: expected a contiguous tensor")
+    return ws.numel() * ws.element_size()
 
 
 def _run(call, stream, tensors, *args):

@@ -48,3 +48,16 @@ def test_outputs_may_lie_apart():
     back = lambda q, do, dq, dk: L.da2_diff_attn_bwd(p, A[0], q, A[1], k, A[2], k, FAKE, None, None, FAKE, A[3], do, A[4], dq, A[5], dk, A[6],  # noqa: E731
                                                      dk, FAKE, FAKE, 1 << 30, None)
     assert back(q, q, far, far) == U and back(far, q, q, k) == E and back(q, far, q, k) == E
+
+
+def test_workspaces_hold_what_their_elements_count():
+    """A byte repeated, or every second one, counts more elements than it has memory behind its address."""
+    Q = torch.zeros(1, 2, 1, 64, dtype=torch.bfloat16)
+    K = torch.zeros(1, 2, 4000, 64, dtype=torch.bfloat16)
+    X, w, stats = torch.zeros(1, 1, 5, 8), torch.ones(8), torch.zeros(1, 1, 5, 2)
+    for ws in (torch.zeros(1, dtype=torch.uint8).expand(1 << 22), torch.zeros(1 << 23, dtype=torch.uint8)[::2]):
+        for call in (lambda: api.da2_diff_attn(Q, K, K, torch.zeros(2), torch.zeros_like(Q), ws),
+                     lambda: api.da2_diff_attn_bwd(Q, K, K, torch.zeros(2), torch.zeros(1, 2, 2, 1), Q, Q, K, K, torch.zeros(2), ws),
+                     lambda: api.da2_norm_bwd(X, X, stats, X, w, w, ws=ws)):
+            with pytest.raises(ValueError, match="contiguous"):
+                call()
