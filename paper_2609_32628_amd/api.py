@@ -257,16 +257,16 @@ def _norm_desc(X, given, kind, eps, plus_one):
     for name, t in given:
         if t is None:
             continue
+        st = t.stride()
+        if t.dtype not in DTYPES or t.shape not in ((C,), (B, C)) or (C > 1 and st[-1] != 1):
+            raise ValueError(f"{name}: expected [C] or [B, C] weights with C contiguous")
+        # one sample's weights serve all its rows whatever their stride
+        per = st[0] if len(st) == 2 and B > 1 else 0
         if first is None:
-            st, first, wdtype = t.stride(), t, t.dtype
-            if wdtype not in DTYPES or t.shape not in ((C,), (B, C)) or (C > 1 and st[-1] != 1):
-                raise ValueError(f"{name}: expected [C] or [B, C] weights with C contiguous")
-            # one sample's weights serve all its rows whatever their stride
-            if len(st) == 2 and B > 1:
-                stride = st[0]
-                if stride < C:
-                    raise ValueError(f"{name}: the samples' weights overlap")
-        elif t.shape != first.shape or t.dtype != wdtype or t.stride() != st:
+            first, wdtype, stride = t, t.dtype, per
+            if len(st) == 2 and B > 1 and per < C:
+                raise ValueError(f"{name}: the samples' weights overlap")
+        elif t.shape != first.shape or t.dtype != wdtype or per != stride:
             raise ValueError("weights and bias (and their gradients) must share shape, strides and dtype")
     return Rows(B, H, N, C), NormDesc(NORM_KINDS[kind], DTYPES[wdtype], int(plus_one), 0, stride, float(eps))
 

@@ -61,3 +61,20 @@ def test_workspaces_hold_what_their_elements_count():
                      lambda: api.da2_norm_bwd(X, X, stats, X, w, w, ws=ws)):
             with pytest.raises(ValueError, match="contiguous"):
                 call()
+
+
+def test_strides_of_one_sample_are_not_looked_at():
+    """A slice of one sample's modulation beside a packed tensor for its gradient: the distance to a next sample is nobody's.
+    (The call gets as far as to see that nothing is on a GPU.)"""
+    X, stats = torch.zeros(1, 1, 5, 8), torch.zeros(1, 1, 5, 2)
+    w, b = torch.ones(1, 48).chunk(6, 1)[:2]
+    packed = torch.empty(1, 8)
+    one, narrow = torch.ones(4)[::4], torch.ones(1, 1, 5, 1)
+    for call in (lambda: api.da2_norm(X, X, w, packed), lambda: api.da2_norm_bwd(X, X, stats, X, w, packed, torch.empty(1, 8), ws=torch.empty(64)),
+                 lambda: api.da2_norm(narrow, narrow, one, torch.ones(1))):
+        with pytest.raises(ValueError, match="GPU"):
+            call()
+    X, w = torch.zeros(2, 1, 5, 8), torch.ones(2, 48).chunk(6, 1)[0]
+    for bad in (torch.empty(2, 8), torch.ones(2, 96).chunk(6, 1)[0][:, :8]):
+        with pytest.raises(ValueError, match="strides"):
+            api.da2_norm(X, X, w, bad)
