@@ -11,13 +11,14 @@ on one GPU, and raise ValueError before the call otherwise. They run on the
 tensors' GPU, whichever device is current.
 """
 import ctypes
+import math
 from dataclasses import dataclass
 
 import numpy as np
 import torch
 
 from . import _lib
-from ._lib import (DA2_BF16, DA2_FMT4_MXFP4, DA2_FMT4_NVFP4, DA2_FP16, DA2_FP32, DA2_NORM_LAYER, DA2_NORM_RMS,
+from ._lib import (DA2_BF16, DA2_ERR_WORKSPACE, DA2_FMT4_MXFP4, DA2_FMT4_NVFP4, DA2_FP16, DA2_FP32, DA2_NORM_LAYER, DA2_NORM_RMS,
                    DA2_PART_RAGGED, DA2_PART_TILES8, DA2_ROPE_HALF, DA2_ROPE_INTERLEAVED, DA2_ROPE_LINEAR,
                    DA2_ROPE_NTK, DA2_ROPE_PLAIN, DA2_ROPE_YARN, DA2_SCOPE_HEAD, DA2_SCOPE_ROW, DiffProblem, NormDesc, Problem,
                    RopeDesc, RopeFreq, RopeRows, Rows, Tensor, check, lib)
@@ -164,7 +165,10 @@ def attention(Q, K, V, buf, lam, budgets, O, stream=None, num16=0, fmt4=None, qk
     of the 4-bit path. qk_norm = (w_q, w_k), weights [d] or None each: the heads
     of Q and K are RMS-normalised first; rope, a Rope over one axis (the token
     numbers) or three (the problem's grid): they are rotated next. Both work in
-    place, on Q and K themselves."""
+    place, on Q and K themselves: a second call with them would do so again, and
+    who needs them as they were calls da2_norm and da2_rope into tensors of
+    their own and then this without. All arguments of all calls are checked
+    before Q and K are touched."""
     p = buf.p
     fmt4 = buf.fmt4 if fmt4 is None else fmt4
     if fmt4 != buf.fmt4 or (num16 > 0 and not buf.with16):
@@ -174,16 +178,71 @@ def attention(Q, K, V, buf, lam, budgets, O, stream=None, num16=0, fmt4=None, qk
         raise ValueError(f"rope: expected 1 or 3 axes, got {len(rope.rot_axis)}")
     if (qk_norm is not None or rope is not None) and Q.data_ptr() == K.data_ptr():
         raise ValueError("Q and K are one tensor: the norm and rotation in place would meet it twice")
+    if qk_norm is not None or rope is not None:
+        turn = _check_in_place(Q, K, V, buf, lam, budgets, O, num16, qk_norm, rope)
     if qk_norm is not None:
         da2_norm(Q, Q, qk_norm[0], kind="rms", stream=stream)
         da2_norm(K, K, qk_norm[1], kind="rms", stream=stream)
     if rope is not None:
-        da2_rope(rope, Q, Q, K, K, grid=None if len(rope.rot_axis) == 1 else (p.Hg, p.Wg), inverse=False, stream=stream)
+        _run("da2_rope", stream, *turn)
     da2_draft_map(Q, K, buf.layout, p, lam, buf.A, buf.stats, buf.ws_draft, stream)
     da2_rank_assign(buf.A, p, num16, *budgets, buf.scope, buf.cls, buf.lists, buf.ws_rank, stream)
     da2_prep_operands(Q, K, V, buf.layout, p, int(num16 > 0), fmt4, buf.stats, buf.ops, None, stream)
     da2_mixed_attn(buf.ops, buf.lists, buf.layout, p, O, stream, fmt4)
     return O
+
+
+def _in_order(call, *args):
+    """Raises what the call says of its arguments, which it is given without a workspace: it looks at that last, and so
+    launches nothing."""
+    status = getattr(lib(), call)(*args)
+    if status != DA2_ERR_WORKSPACE:
+        check(call, status)
+        raise AssertionError(f"{call} ran without a workspace")
+
+
+def _check_in_place(Q, K, V, buf, lam, budgets, O, num16, qk_norm, rope):
+    """Everything that attention's calls refuse, before the first of them writes to Q and K. Returns what da2_rope takes."""
+    p = buf.p
+    size = da2_sizes(p, buf.scope, buf.fmt4, buf.with16)
+    shape = (p.B, p.H, p.T * p.Hg * p.Wg, p.d)
+    for name, t in (("Q", Q), ("K", K), ("V", V), ("O", O)):
+        _tensor_desc(t)
+        if t.shape != shape:
+            raise ValueError(f"{name}: expected shape {shape}, got {tuple(t.shape)}")
+    if not (Q.stride() == K.stride() == V.stride() and Q.dtype == K.dtype == V.dtype):
+        raise ValueError("Q, K and V must share shape, strides and dtype")
+    if V.data_ptr() in (Q.data_ptr(), K.data_ptr()):
+        raise ValueError("V is Q's or K's memory: the norm and rotation in place would meet it too")
+    if min(O.stride()) <= 0 or O.stride(2) < p.d:
+        raise ValueError("O: rows overlap")
+    for name in ("layout", "A", "cls", "stats", "lists", "ops", "ws_draft", "ws_rank"):
+        t = getattr(buf, name)
+        if not t.is_contiguous() or t.numel() * t.element_size() < size[name + "_bytes"]:
+            raise ValueError(f"buf.{name}: expected {size[name + '_bytes']} contiguous bytes")
+    desc = ctypes.byref(_tensor_desc(Q))
+    P = ctypes.byref(p)
+    _in_order("da2_draft_map", _ptr(Q), _ptr(K), desc, _ptr(buf.layout), P, float(lam), _ptr(buf.A), _ptr(buf.stats),
+              _ptr(buf.ws_draft), 0, None)
+    _in_order("da2_rank_assign", _ptr(buf.A), P, num16, *budgets, SCOPES[buf.scope], _ptr(buf.cls), _ptr(buf.lists), _ptr(buf.ws_rank), 0,
+              None)
+    _in_order("da2_prep_operands", _ptr(Q), _ptr(K), _ptr(V), desc, _ptr(buf.layout), P, int(num16 > 0), FMT4[buf.fmt4],
+              _ptr(buf.stats), _ptr(buf.ops), 0, None, -1, None)
+    tensors, turn = [Q, K, V, O, buf.layout, buf.A, buf.cls, buf.stats, buf.lists, buf.ops, buf.ws_draft, buf.ws_rank], None
+    if qk_norm is not None:
+        w_q, w_k = qk_norm
+        _norm_desc(Q, (("w_q", w_q),), "rms", 0.0, False)
+        _norm_desc(K, (("w_k", w_k),), "rms", 0.0, False)
+        tensors += [w_q, w_k]
+    if rope is not None:
+        turn = _rope_args(rope, Q, Q, K, K, None, None if len(rope.rot_axis) == 1 else (p.Hg, p.Wg), False)
+        # what da2_rope itself asks
+        if (any(D < 2 or D % 2 for D in rope.rot_axis) or sum(rope.rot_axis) > rope.block or p.d % rope.block
+                or not math.isfinite(rope.scale) or p.B * shape[2] * rope.block > (1 << 32) - 256):
+            raise ValueError(f"rope: {rope.rot_axis} of {rope.block} channels, scale {rope.scale}, for heads of {p.d}")
+        tensors.append(rope.turns)
+    _one_gpu(tensors)
+    return turn
 
 
 # ---- token operators ---------------------------------------------------------------
@@ -228,14 +287,19 @@ def _bytes(ws):
     return ws.numel() * ws.element_size()
 
 
-def _run(call, stream, tensors, *args):
-    """Makes the call on the GPU that holds all the tensors and on its current stream (or the given one)."""
+def _one_gpu(tensors):
     dev = tensors[0].get_device()
     for t in tensors:
         if t is not None and t.get_device() != dev:
             raise ValueError("expected all tensors on one GPU")
     if dev < 0:
         raise ValueError("expected tensors on a GPU")
+    return dev
+
+
+def _run(call, stream, tensors, *args):
+    """Makes the call on the GPU that holds all the tensors and on its current stream (or the given one)."""
+    dev = _one_gpu(tensors)
     if stream is None:
         s = torch._C._cuda_getCurrentRawStream(dev)
     elif stream.device.index == dev:
@@ -337,9 +401,8 @@ def da2_rope_plan(block, rot_axis, layout="interleaved", base=10000.0, scaling="
     return rope
 
 
-def da2_rope(rope, Q, Qo, K=None, Ko=None, pos=None, grid=None, inverse=False, stream=None):
-    """Rotates Q (and K) into Qo (and Ko), which may be the inputs. pos: int32 [B or 1, N, axes] positions; without it
-    the tokens are numbered, on 2 and 3 axes over a ``grid`` of (height, width) per frame. inverse: the gradient."""
+def _rope_args(rope, Q, Qo, K, Ko, pos, grid, inverse):
+    """The tensors of a da2_rope call and its arguments."""
     q = _rows("Q", Q)
     qo = _rows("Qo", Qo, Q.shape, Q.dtype)
     B, Hq, N, d = Q.shape
@@ -359,8 +422,14 @@ def da2_rope(rope, Q, Qo, K=None, Ko=None, pos=None, grid=None, inverse=False, s
         stride = pos.stride(0) if pos.shape[0] > 1 else 0
     t = _plain("turns", rope.turns, (sum(rope.rot_axis) // 2,), torch.float64)
     gh, gw = grid if grid is not None else (0, 0)
-    _run("da2_rope", stream, (Q, Qo, K, Ko, pos, rope.turns), rope.desc(), t, rope.scale, _addr(pos), stride,
-         RopeRows(B, Hq, Hk, N, d, gh, gw, int(inverse)), Q.data_ptr(), q, Qo.data_ptr(), qo, _addr(K), k, _addr(Ko), ko)
+    return ((Q, Qo, K, Ko, pos, rope.turns), rope.desc(), t, rope.scale, _addr(pos), stride,
+            RopeRows(B, Hq, Hk, N, d, gh, gw, int(inverse)), Q.data_ptr(), q, Qo.data_ptr(), qo, _addr(K), k, _addr(Ko), ko)
+
+
+def da2_rope(rope, Q, Qo, K=None, Ko=None, pos=None, grid=None, inverse=False, stream=None):
+    """Rotates Q (and K) into Qo (and Ko), which may be the inputs. pos: int32 [B or 1, N, axes] positions; without it
+    the tokens are numbered, on 2 and 3 axes over a ``grid`` of (height, width) per frame. inverse: the gradient."""
+    _run("da2_rope", stream, *_rope_args(rope, Q, Qo, K, Ko, pos, grid, inverse))
 
 
 def _diff_problem(Q, K, causal=False, scale=None):
