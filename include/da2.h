@@ -460,8 +460,9 @@ typedef struct {
 } da2_rope_rows;
 
 /* Rotates every row of Q and of K: (a, b) -> scale (a cos - b sin, a sin + b cos)
- * with the angle 2 pi turns[p] pos, computed in float64 and reduced by whole
- * turns, so that far positions lose nothing; inverse = 1 turns back (same scale).
+ * with the angle 2 pi turns[p] pos; the product is taken without rounding and
+ * reduced by whole turns, so that far positions and fast pairs lose nothing
+ * (pi 2^-25); inverse = 1 turns back (same scale).
  *   turns   device, float64 [rot/2]; scale finite
  *   pos     device, int32 [B][N][axes] with pos_stride_b elements between the
  *           samples (0: shared, else >= N*axes), any values; or NULL: the token

@@ -2,8 +2,9 @@
 //
 // Pair (a, b) of a token at position pos becomes scale (a cos t - b sin t,
 // a sin t + b cos t) with t = 2 pi turns[p] pos. turns pos is a float64 product
-// from which the nearest whole number is taken before it is rounded to float32,
-// so the angle is off by at most pi 2^-25 wherever the token is.
+// and what its rounding left out; whole turns are taken out of both before their
+// sum is rounded to float32, so the angle is off by at most pi 2^-25 (and 2^-50)
+// wherever the token is and however fast the pair turns.
 //
 // Bound by memory: Q and K in and out. The angles do not depend on the head, so
 // a thread computes the cosines and sines of its pairs of one token once and
@@ -67,9 +68,10 @@ __device__ inline void angles(const RopeArgs& a, int b, int n, int p, float* c, 
   for (int i = 0; i < P; ++i) {
     if (2 * (p + i) >= a.rot) break;
     const int where = p + i < a.pair0 ? at[0] : p + i < a.pair1 ? at[1] : at[2];
-    const double t = a.turns[p + i] * where;
+    const double t = a.turns[p + i] * where, rest = __builtin_fma(a.turns[p + i], static_cast<double>(where), -t);
+    const double f = (t - __builtin_rint(t)) + (rest - __builtin_rint(rest));
     float sn, cs;
-    sincospif(2.0f * static_cast<float>(t - __builtin_rint(t)), &sn, &cs);
+    sincospif(2.0f * static_cast<float>(f - __builtin_rint(f)), &sn, &cs);
     c[i] = cs * a.scale;
     s[i] = sn * (a.scale * a.sign);
   }
