@@ -578,6 +578,13 @@ Shape shape_of(int C, int vec, int max_k) {
   return {kLong, 0};
 }
 
+// Whether shape_of gives TPR threads with K chunks for any row: those of 256 and 512 threads have more than max_k chunks
+// for each of the 64 or 256 threads before them.
+template <int TPR, int K>
+constexpr bool reached(int max_k) {
+  return K <= max_k && (TPR <= 64 || K * TPR > max_k * (TPR == 256 ? 64 : 256));
+}
+
 // Calls f<TPR, K, TAIL>() for the shape; tail: the row's last chunk is not whole.
 template <bool TAIL, typename F>
 hipError_t with_shape(Shape s, F&& f) {
@@ -638,10 +645,14 @@ hipError_t launch_norm(const NormArgs& a, hipStream_t stream) {
       return hipGetLastError();
     }
     return with_shape(s, a.C % kVec<T> != 0, [&]<int TPR, int K, bool TAIL>() {
-      constexpr int RPB = block_of<TPR>() / TPR;
-      const int64_t units = (rows + RPB - 1) / RPB, fill = (resident(fwd_waves(K * kVec<T>, TPR), block_of<TPR>()) + groups - 1) / groups;
-      norm_kernel<T, TPR, K, TAIL><<<dim3(static_cast<unsigned>(units < fill ? units : fill), groups), block_of<TPR>(), 0, stream>>>(a, rows, grouped);
-      return hipGetLastError();
+      if constexpr (!reached<TPR, K>(kFwdK)) {
+        return hipErrorInvalidValue;
+      } else {
+        constexpr int RPB = block_of<TPR>() / TPR;
+        const int64_t units = (rows + RPB - 1) / RPB, fill = (resident(fwd_waves(K * kVec<T>, TPR), block_of<TPR>()) + groups - 1) / groups;
+        norm_kernel<T, TPR, K, TAIL><<<dim3(static_cast<unsigned>(units < fill ? units : fill), groups), block_of<TPR>(), 0, stream>>>(a, rows, grouped);
+        return hipGetLastError();
+      }
     });
   });
 }
@@ -662,8 +673,8 @@ hipError_t launch_norm_bwd(const NormArgs& a, hipStream_t stream) {
     }
     return with_shape(s, a.C % kVec<T> != 0, [&]<int TPR, int K, bool TAIL>() {
       constexpr int RPB = block_of<TPR>() / TPR;
-      if constexpr (K > kBwdK) {
-        return hipErrorInvalidValue;  // no shape of the backward pass
+      if constexpr (!reached<TPR, K>(kBwdK)) {
+        return hipErrorInvalidValue;
       } else if (sums) {
         norm_bwd_kernel<T, TPR, K, TAIL, true><<<dim3(parts, groups), block_of<TPR>(), 0, stream>>>(a, rows, grouped);
       } else {
