@@ -143,3 +143,25 @@ def test_many_small_weights(bits, dtype, N):
     want = rest / (1 + rest)
     tol = (2 * u + 2 * (M / 16 + 40) * 2.0 ** -24) * want + (M * 2.0 ** -36 if dtype == "fp16" else 0)
     assert (out - want).abs().max() <= tol
+
+
+@pytest.mark.parametrize("H,N,M,d,causal", [(2, 9000, 300, 64, False), (4, 333, 333, 128, True), (2, 40, 40, 64, False)])
+def test_scales_in_a_captured_pass(H, N, M, d, causal):
+    """The powers of two are taken from the data at every replay: gradients of other sizes through one graph, bit for bit as
+    outside of it."""
+    case = Case(1, H, H, N, M, d, "fp16", causal, seed=37)
+    gradients(case)
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        out = gradients(case)
+    for i, size in enumerate((1e-4, 30.0, 1e-2, 1.0)):
+        g = torch.Generator(device="cuda")
+        g.manual_seed(i)
+        case.dO.copy_(torch.randn(case.dO.shape, generator=g, device="cuda") * size)
+        case.lam.copy_(torch.randn(H, generator=g, device="cuda") * 3)
+        for x in out.values():
+            x.fill_(float("nan"))
+        graph.replay()
+        want = gradients(case)
+        torch.cuda.synchronize()
+        assert all(torch.equal(out[n], want[n]) for n in out)
