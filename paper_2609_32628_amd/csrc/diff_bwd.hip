@@ -386,7 +386,7 @@ __global__ __launch_bounds__(64 * Many<SHARE>::kWaves, 2) void diff_dq_kernel(Di
   constexpr int S = D / 32, K = Many<SHARE>::kKeys, WAVES = Many<SHARE>::kWaves, BYTES = K * Tile<D>::kRow, R = Tile<D>::kRowsPerCopy;
   constexpr int GROUPS = Many<SHARE>::kGroups, ROWS = Many<SHARE>::kRows;
   __shared__ __align__(256) char lds[2][2][BYTES];  // [buffer][K, V]
-  __shared__ float sums[SHARE][GROUPS][2 + kScaled<T>][64];
+  __shared__ float sums[SHARE][GROUPS][3 + kScaled<T>][64];
   // keys spread over those that the workgroup's rows see, and the middle of them
   constexpr int SAMPLE = 8 * WAVES * 128 / D;
   __shared__ __align__(16) T sample[SAMPLE][D];
@@ -428,7 +428,7 @@ __global__ __launch_bounds__(64 * Many<SHARE>::kWaves, 2) void diff_dq_kernel(Di
     }
   }
   const int64_t bhn = static_cast<int64_t>(b) * a.Hq + h;
-  float lse[2], d[2] = {0.0f, 0.0f}, top = 0.0f;  // top: the largest |dP| that the row meets
+  float lse[2], d[3] = {0.0f, 0.0f, 0.0f}, top = 0.0f;  // del1, del2, the sum of P2; the largest |dP| that the row meets
   int ks = 0;                                     // exponent of the scale of its dS
 #pragma unroll
   for (int i = 0; i < 2; ++i) {
@@ -487,7 +487,7 @@ __global__ __launch_bounds__(64 * Many<SHARE>::kWaves, 2) void diff_dq_kernel(Di
 #pragma unroll
           for (int s = 0; s < S; ++s) x = mma<T>(rows.read(kt, j, i * S + s), qf[i][s], x);
           const float l = kScaled<T> && !kSums ? lse[i] - static_cast<float>(ks) : lse[i];
-          float ds[16], sum = 0.0f;  // of P dP over 16 keys
+          float ds[16], sum = 0.0f, whole = 0.0f;  // of P dP over 16 keys, and of P
           if (mask)
 #pragma unroll
             for (int e = 0; e < 16; ++e) x[e] = e < left ? x[e] : -__builtin_inff();
@@ -496,12 +496,14 @@ __global__ __launch_bounds__(64 * Many<SHARE>::kWaves, 2) void diff_dq_kernel(Di
             const float p = exp2_fast(__builtin_fmaf(x[e], c, -l));
             if constexpr (kSums) {
               sum = __builtin_fmaf(p, dp[e], sum);
+              if (i) whole += p;
             } else {
               ds[e] = p * (dp[e] - d[i]);
             }
           }
           if constexpr (kSums) {
             d[i] += sum;
+            if (i) d[2] += whole;
           } else {
             df[i][0] = pack8<T>(ds);
             df[i][1] = pack8<T>(ds + 8);
@@ -522,14 +524,14 @@ __global__ __launch_bounds__(64 * Many<SHARE>::kWaves, 2) void diff_dq_kernel(Di
   };
   walk(std::integral_constant<int, 0>{});
 #pragma unroll
-  for (int i = 0; i < 2; ++i) d[i] = sum_halves(d[i]);
-  const auto add_up = [&](float (&v)[2]) {  // over the waves of a row, in order; each gets the sum
+  for (int i = 0; i < 3; ++i) d[i] = sum_halves(d[i]);
+  const auto add_up = [&]<int N>(float (&v)[N]) {  // over the waves of a row, in order; each gets the sum
     if constexpr (SHARE > 1) {
 #pragma unroll
-      for (int i = 0; i < 2; ++i) sums[share][group][i][lane] = v[i];
+      for (int i = 0; i < N; ++i) sums[share][group][i][lane] = v[i];
       __syncthreads();
 #pragma unroll
-      for (int i = 0; i < 2; ++i) {
+      for (int i = 0; i < N; ++i) {
         v[i] = sums[0][group][i][lane];
 #pragma unroll
         for (int o = 1; o < SHARE; ++o) v[i] += sums[o][group][i][lane];
@@ -538,13 +540,17 @@ __global__ __launch_bounds__(64 * Many<SHARE>::kWaves, 2) void diff_dq_kernel(Di
   };
   if constexpr (kScaled<T>) {
     top = max_halves(top);
-    if constexpr (SHARE > 1) sums[share][group][2][lane] = top;
+    if constexpr (SHARE > 1) sums[share][group][3][lane] = top;
   }
   add_up(d);
+  // del2 by what the weights sum to: the float32 log sum moves all of a row's weights by up to 2^-24 of its size, and dlambda
+  // is a sum in which most of del2 may cancel (60 training cases: its error was 2.3 times that of float32 softmax maps, and
+  // is 0.8 times; 0.6% of the backward pass, at d = 64 and thousands of keys up to 3.5%).
+  if (d[2] > 0.0f) d[1] /= d[2];
   if constexpr (kScaled<T>) {
     if constexpr (SHARE > 1)
 #pragma unroll
-      for (int o = 0; o < SHARE; ++o) top = fmaxf(top, sums[o][group][2][lane]);
+      for (int o = 0; o < SHARE; ++o) top = fmaxf(top, sums[o][group][3][lane]);
     ks = 14 - exponent_above(top);
     const float2 most = make_float2(wave_max_f32(top), wave_max_f32(fabsf(a.lam[h])));
     if (!share && lane == 0) tops[(static_cast<int64_t>(bh) * tiles + tile) * GROUPS + group] = most;

@@ -165,3 +165,22 @@ def test_scales_in_a_captured_pass(H, N, M, d, causal):
         want = gradients(case)
         torch.cuda.synchronize()
         assert all(torch.equal(out[n], want[n]) for n in out)
+
+
+@pytest.mark.parametrize("d,dtype", [(64, "bf16"), (128, "fp16")])
+def test_lambda_gradient_of_values_far_from_zero(d, dtype):
+    """dlam = -sum over the rows of del2, where values of one sign leave del2 much larger than what it changes by. A weight's
+    own errors (2^-21, exponent and score) do not depend on another's and count with dP - del2; what a row's weights are off
+    together, as by the float32 log sum, does not count at all. Roundings of del2's size: two sums of at most 12 terms in a
+    chain (each addition off by 2^-24 of the sum so far, evenly: sqrt(12 / 3) 2^-24 / sqrt 3) and four more: 2^-23 of del2
+    in the mean square. Over 64 heads the mean square is near its mean: the error is at most 1.5 times that."""
+    case = Case(1, 64, 64, 100, 700, d, dtype, seed=39, q_scale=2.5)
+    case.V += 16
+    got, want = f64(gradients(case)["dlam"]), case.oracle(True)["dlam"]
+    square = np.zeros(case.H)
+    for h in range(case.H):
+        P, _ = token._maps(f64(case.Q[0, h]), f64(case.K[0, h]), np.ones((case.N, case.M), bool), 1 / math.sqrt(d // 2))
+        dP = f64(case.dO[0, h]) @ f64(case.V[0, h]).T
+        delta = (P[1] * dP).sum(-1, keepdims=True)
+        square[h] = (2.0 ** -46 * delta ** 2).sum() + (2.0 ** -42 * P[1] ** 2 * (dP - delta) ** 2).sum()
+    assert math.sqrt(((got - want) ** 2 / square).mean()) <= 1.5
