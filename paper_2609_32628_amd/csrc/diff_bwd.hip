@@ -8,10 +8,11 @@
 //
 // del_i equals dO . (output of map i), but outputs stored in 16 bits are too
 // coarse for it: their rounding moves every dS_i of a row the same way, which
-// the mean of K does not cancel (2.5 times the error of the gradients' own
+// the middle of K does not cancel (2.5 times the error of the gradients' own
 // rounding, measured), and dlambda is a sum in which most of del2 cancels. So
 // the rows are walked twice: once for del_i, in float32 from unrounded weights,
-// then for dQ.
+// then for dQ. (Not tried: one walk with a del from such outputs, and what it was
+// off by, summed on the way, taken out of dQ with the weights' own sum of K.)
 //
 // Two kernels: dQ, where a wave keeps 32 queries and walks over the keys; dK and
 // dV, where a wave keeps 32 keys and walks over the queries. Each recomputes the
@@ -19,7 +20,7 @@
 // the order of workgroups and nothing has to be cleared. In multiply-adds of d
 // per pair: 2 for del, 3 for dQ, 4 for dK and dV, where one pass over both sides
 // (which would need sums in memory) takes 5 beside del. (bf16, 2 x 2,048 causal
-// tokens, 12 heads on 4 key heads, d = 128: dQ 111 us, dK and dV 84, joined in 16.)
+// tokens, 12 heads on 4 key heads, d = 128: dQ 114 us, dK and dV 85, joined in 17.)
 //
 // The weights and score gradients are rounded to 16 bits for their products. In
 // fp16 that would lose them: a weight is about one over the number of keys, and dS

@@ -17,9 +17,10 @@
 //   - few rows (up to 64): 4 waves with the same 32 rows walk the 32-key quarters
 //     of 128-key tiles, each its own, and are joined at the end.
 // Where that leaves CUs idle the keys are split over workgroups; a second kernel
-// joins the parts. (bf16, 16,380 tokens of 12 heads, d = 128: 2.3 ms, 1.08 PFLOP/s,
-// bound by products and exponentials, which share the issue slots; one token over
-// 16 caches of up to 16,384 keys, 8 key heads: 161 us, 5.1 TB/s.)
+// joins the parts. (bf16, 16,380 tokens of 12 heads, d = 128: 2.31 to 2.43 ms from
+// one card to another, 1.02 to 1.07 PFLOP/s, bound by products and exponentials,
+// which share the issue slots; one token over 16 caches of up to 16,384 keys, 8 key
+// heads: 161 us, 5.1 TB/s.)
 #include "diff.hpp"
 
 namespace da2 {
@@ -47,7 +48,8 @@ Cut cut_of(int B, int Hq, int Hk, int N, int M) {
   // 8,192, 12 heads: 113, 74 and 80): 256 keys. Many rows: 128 keys take a workgroup of 128 rows 2.5 us, and a launch and
   // the parts' way through memory 5 us and more, so parts have 512 keys (from 1,536 on) where the tiles leave most CUs idle
   // and 2,048 else (32 tiles against 1,024 keys: 24 us whole and 26 in two parts; 64 against 2,048: 42 whole, 40 in two, 36
-  // in four; 128 against 2,048: 44 whole and 49 in two).
+  // in four; 128 against 2,048: 44 whole and 49 in two; near the borders it loses: 8 against 1,535 30.9 whole and
+  // 28.4 in two parts, 96 against 3,000 59.0 and 56.7).
   int64_t s = 256 / units, most = c.few ? (M + 255) / 256 : units <= 64 && M >= 1536 ? M / 512 : M / 2048;
   s = s < most ? s : most;
   c.splits = static_cast<int>(s < 1 ? 1 : s);
