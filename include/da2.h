@@ -541,6 +541,117 @@ int32_t da2_diff_attn_bwd(const da2_diff_problem* p, const void* Q, const da2_te
                           const da2_tensor* dv, float* dlambda, void* ws, int64_t ws_bytes,
                           void* stream);
 
+/* ---- The rest of a layer: norm and rotation of Q and K, projections, gated blocks ----
+ *
+ * Conventions of the token operators above.
+ *
+ * Norm of the heads of Q and K (da2_norm over their d channels, no bias), then da2_rope,
+ * in one pass with one rounding:  y = R(pos) (f xh), xh = (x - mean) rstd.
+ *   r .. s    as in da2_rope, s->inverse = 0; d at most 512, else UNSUPPORTED, and
+ *             B*N at most 2^26 - 4
+ *   n         kind, plus_one, eps as in da2_norm; wdtype the type of w_q, w_k, dw_q,
+ *             dw_k; stride_b 0
+ *   w_q, w_k  device [d] or NULL: factor 1
+ * Q and K in and out as in da2_rope, which may be the same memory. */
+int32_t da2_qk_norm_rope(const da2_rope_desc* r, const double* turns, double scale, const int32_t* pos,
+                         int64_t pos_stride_b, const da2_rope_rows* s, const da2_norm_desc* n, const void* w_q,
+                         const void* w_k, const void* Q, const da2_tensor* q, void* Qo, const da2_tensor* qo,
+                         const void* K, const da2_tensor* k, void* Ko, const da2_tensor* ko, void* stream);
+
+/* Host only: workspace bytes of da2_qk_norm_rope_bwd for dw_q or dw_k. */
+int32_t da2_qk_norm_rope_ws_bytes(const da2_rope_rows* s, int64_t* bytes);
+
+/* Gradients of da2_qk_norm_rope from its inputs: with g = R(pos)' dy and h = g f,
+ *   dx = rstd (h - mean(h) - xh mean(h xh)) (RMS: without mean(h)), dw = sum of g xh over all rows
+ * (mean and rstd are computed again).
+ *   dQo, dKo    device, gradients of the results; Q, K the inputs of the forward pass
+ *   dQ, dK      device out (may be dQo and dKo, or Q and K); Hk = 0: Q alone
+ *   dw_q, dw_k  device out [d] of n->wdtype, or NULL
+ *   ws          device scratch of da2_qk_norm_rope_ws_bytes, needed for dw_q or dw_k */
+int32_t da2_qk_norm_rope_bwd(const da2_rope_desc* r, const double* turns, double scale, const int32_t* pos,
+                             int64_t pos_stride_b, const da2_rope_rows* s, const da2_norm_desc* n, const void* w_q,
+                             const void* w_k, const void* dQo, const da2_tensor* dqo, const void* Q,
+                             const da2_tensor* q, void* dQ, const da2_tensor* dq, const void* dKo,
+                             const da2_tensor* dko, const void* K, const da2_tensor* k, void* dK,
+                             const da2_tensor* dk, void* dw_q, void* dw_k, void* ws, int64_t ws_bytes,
+                             void* stream);
+
+/* Activations: z; max(z, 0); z Phi(z) with the normal distribution function Phi; its approximation
+ * z / (1 + exp(-2 sqrt(2/pi) (z + 0.044715 z^3))); z / (1 + exp(-z)); 1 / (1 + exp(-z)). */
+typedef enum {
+  DA2_ACT_NONE = 0,
+  DA2_ACT_RELU = 1,
+  DA2_ACT_GELU = 2,
+  DA2_ACT_GELU_TANH = 3,
+  DA2_ACT_SILU = 4,
+  DA2_ACT_SIGMOID = 5
+} da2_act;
+
+/* A projection of token rows: B samples of N tokens, each a row of K = Hx Cx input features and F = Hy Cy
+ * output features. Hidden rows are one block (Hx or Hy = 1); the heads of an attention's tensors are
+ * features as they lie in [B, H, N, C], feature h C + c. Blocks of more than one have Cx a multiple of 64, Cy of 8.
+ * Tensors are bf16 or fp16 (fp32: UNSUPPORTED), all of the one dtype, and read and written in 16-byte
+ * vectors: bases 16-byte aligned (bias and gate: of an element), every stride of X, Y, R, W and their gradients a multiple
+ * of 8 elements, the stride_n of inputs and the row stride of W at most 2^22. Any K and F: what lies between a row's end and
+ * its stride is neither used nor written.
+ * K and F at most 2^20; B*N at most 2^31 - 1 (backward with dW: 2^22 - 8*B), and
+ * ceil(B*N / 128) ceil(K or F / 128) at most 2^24 - 8 (da2_glu: 2 F; and (F + 256) times W's row stride below 2^31). */
+typedef struct {
+  int32_t B, N, Hx, Cx, Hy, Cy;
+  int32_t act;   /* da2_act   */
+  int32_t dtype; /* da2_dtype */
+} da2_proj;
+
+/* Host only: workspace bytes of da2_linear (train = 1: and of da2_linear_bwd). */
+int32_t da2_linear_ws_bytes(const da2_proj* p, int32_t train, int64_t* bytes);
+
+/* Y = R + gate act(Z), Z = X W' + bias.
+ *   X     device [B,Hx,N,Cx] per *x
+ *   W     device [F][K], w_stride elements between the rows (at least K)
+ *   bias  device [F], or NULL
+ *   gate  device [F] (gate_stride_b = 0), or [B][F] with gate_stride_b >= F elements between the
+ *         samples, or NULL: 1
+ *   R     device [B,Hy,N,Cy] per *r (residual; may be Y, with its strides), or NULL: 0
+ *   Y     device out [B,Hy,N,Cy] per *y
+ *   Z     device out float32 [B*N][F8], F8 = F rounded up to a multiple of 8, or NULL: Z for the
+ *         backward pass, unrounded (columns from F on are not written)
+ *   ws    device scratch of da2_linear_ws_bytes(p, 0); may be NULL when that is 0
+ * Sums are float32, and the activation, gate and residual are applied to them before one rounding. */
+int32_t da2_linear(const da2_proj* p, const void* X, const da2_tensor* x, const void* W, int64_t w_stride,
+                   const void* bias, const void* gate, int64_t gate_stride_b, const void* R, const da2_tensor* r,
+                   void* Y, const da2_tensor* y, float* Z, void* ws, int64_t ws_bytes, void* stream);
+
+/* Gradients of da2_linear (that of R is dY): with dZ = dY gate act'(Z),
+ *   dX = dZ W, dW = dZ' X, dbias = column sums of dZ, dgate = those of dY act(Z) (per sample when gate_stride_b > 0).
+ * dZ is rounded to the tensors' type for the products with W and X (with neither activation nor gate it
+ * is dY itself); the column sums are taken in float32 before.
+ *   Z      what da2_linear wrote; needed with an activation or for dgate
+ *   dX     device out per *dx, like X, or NULL; dW device out [F][K], dw_stride elements between the rows, or NULL
+ *   dbias  device out [F], or NULL; dgate device out like gate (same gate_stride_b), or NULL
+ *   ws     device scratch of da2_linear_ws_bytes(p, 1)
+ * Outputs are not the memory of an input. INVALID_ARG when all four outputs are NULL. */
+int32_t da2_linear_bwd(const da2_proj* p, const void* dY, const da2_tensor* dy, const void* X, const da2_tensor* x,
+                       const void* W, int64_t w_stride, const void* gate, int64_t gate_stride_b, const float* Z,
+                       void* dX, const da2_tensor* dx, void* dW, int64_t dw_stride, void* dbias, void* dgate,
+                       void* ws, int64_t ws_bytes, void* stream);
+
+/* Host only: workspace bytes of da2_glu (train = 1: and of da2_glu_bwd). */
+int32_t da2_glu_ws_bytes(const da2_proj* p, int32_t train, int64_t* bytes);
+
+/* The gated half of a feed-forward block: Y = act(G) U with G = X Wg' + bg and U = X Wu' + bu.
+ *   W     device [2F][K]: the F rows of Wg, then those of Wu; bias device [2F] alike, or NULL
+ *   Z     device out float32 [B*N][2][F8]: G and U, or NULL
+ * The rest as in da2_linear. */
+int32_t da2_glu(const da2_proj* p, const void* X, const da2_tensor* x, const void* W, int64_t w_stride,
+                const void* bias, void* Y, const da2_tensor* y, float* Z, void* ws, int64_t ws_bytes, void* stream);
+
+/* Gradients of da2_glu: with dG = dY U act'(G) and dU = dY act(G), rounded to the tensors' type for the products,
+ *   dX = dG Wg + dU Wu, dW = [dG' X; dU' X], dbias = their column sums.
+ * Z is what da2_glu wrote. The rest as in da2_linear_bwd. */
+int32_t da2_glu_bwd(const da2_proj* p, const void* dY, const da2_tensor* dy, const void* X, const da2_tensor* x,
+                    const void* W, int64_t w_stride, const float* Z, void* dX, const da2_tensor* dx, void* dW,
+                    int64_t dw_stride, void* dbias, void* ws, int64_t ws_bytes, void* stream);
+
 #ifdef __cplusplus
 }
 #endif

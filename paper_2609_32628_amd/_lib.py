@@ -20,13 +20,16 @@ DA2_NORM_LAYER, DA2_NORM_RMS = 0, 1
 DA2_ROPE_INTERLEAVED, DA2_ROPE_HALF = 0, 1
 DA2_ROPE_PLAIN, DA2_ROPE_LINEAR, DA2_ROPE_NTK, DA2_ROPE_YARN = 0, 1, 2, 3
 DA2_ATTN_ERR_LAYOUT, DA2_ATTN_ERR_FMT4, DA2_ATTN_ERR_NO16 = 1, 2, 4
+DA2_ACT_NONE, DA2_ACT_RELU, DA2_ACT_GELU, DA2_ACT_GELU_TANH, DA2_ACT_SILU, DA2_ACT_SIGMOID = 0, 1, 2, 3, 4, 5
 TAG_MARKER = 0xDA200000   # encoding tag in word 3 of each head's g entry
 
 # Every symbol include/da2.h declares.
 EXPORTS = ("da2_status_string", "da2_sizes", "da2_ops_layout_version", "da2_layout_build", "da2_draft_map", "da2_ws_draft_offsets",
            "da2_rank_assign", "da2_rank_assign_noalloc", "da2_lists_offsets", "da2_prep_operands", "da2_ops_offsets", "da2_mixed_attn",
            "da2_norm", "da2_norm_ws_bytes", "da2_norm_bwd", "da2_rope_plan", "da2_rope",
-           "da2_diff_ws_bytes", "da2_diff_attn", "da2_diff_attn_bwd")
+           "da2_diff_ws_bytes", "da2_diff_attn", "da2_diff_attn_bwd",
+           "da2_qk_norm_rope", "da2_qk_norm_rope_ws_bytes", "da2_qk_norm_rope_bwd", "da2_linear_ws_bytes", "da2_linear",
+           "da2_linear_bwd", "da2_glu_ws_bytes", "da2_glu", "da2_glu_bwd")
 
 
 class Problem(ctypes.Structure):
@@ -79,6 +82,11 @@ class DiffProblem(ctypes.Structure):
                 ("scale", ctypes.c_double)]
 
 
+class Proj(ctypes.Structure):
+    _fields_ = [("B", ctypes.c_int32), ("N", ctypes.c_int32), ("Hx", ctypes.c_int32), ("Cx", ctypes.c_int32),
+                ("Hy", ctypes.c_int32), ("Cy", ctypes.c_int32), ("act", ctypes.c_int32), ("dtype", ctypes.c_int32)]
+
+
 class Da2Error(RuntimeError):
     def __init__(self, call, status, lib):
         msg = lib.da2_status_string(status).decode()
@@ -100,7 +108,7 @@ def lib():
         P, T, S = ctypes.POINTER(Problem), ctypes.POINTER(Tensor), ctypes.POINTER(Sizes)
         R, ND = ctypes.POINTER(Rows), ctypes.POINTER(NormDesc)
         RD, RF, RR = ctypes.POINTER(RopeDesc), ctypes.POINTER(RopeFreq), ctypes.POINTER(RopeRows)
-        DP = ctypes.POINTER(DiffProblem)
+        DP, PJ = ctypes.POINTER(DiffProblem), ctypes.POINTER(Proj)
         pdbl = ctypes.POINTER(ctypes.c_double)
         pi64, pi32 = ctypes.POINTER(ctypes.c_int64), ctypes.POINTER(ctypes.c_int32)
         sig = {
@@ -125,6 +133,16 @@ def lib():
             "da2_diff_attn": (i32, [DP, vp, T, vp, T, vp, T, vp, vp, vp, vp, T, vp, vp, i64, vp]),
             "da2_diff_attn_bwd": (i32, [DP, vp, T, vp, T, vp, T, vp, vp, vp, vp, vp, T, vp, T, vp, T, vp, T, vp, vp,
                                         i64, vp]),
+            "da2_qk_norm_rope": (i32, [RD, vp, dbl, vp, i64, RR, ND, vp, vp, vp, T, vp, T, vp, T, vp, T, vp]),
+            "da2_qk_norm_rope_ws_bytes": (i32, [RR, pi64]),
+            "da2_qk_norm_rope_bwd": (i32, [RD, vp, dbl, vp, i64, RR, ND, vp, vp, vp, T, vp, T, vp, T, vp, T, vp, T, vp, T, vp, vp,
+                                           vp, i64, vp]),
+            "da2_linear_ws_bytes": (i32, [PJ, i32, pi64]),
+            "da2_linear": (i32, [PJ, vp, T, vp, i64, vp, vp, i64, vp, T, vp, T, vp, vp, i64, vp]),
+            "da2_linear_bwd": (i32, [PJ, vp, T, vp, T, vp, i64, vp, i64, vp, vp, T, vp, i64, vp, vp, vp, i64, vp]),
+            "da2_glu_ws_bytes": (i32, [PJ, i32, pi64]),
+            "da2_glu": (i32, [PJ, vp, T, vp, i64, vp, vp, T, vp, vp, i64, vp]),
+            "da2_glu_bwd": (i32, [PJ, vp, T, vp, T, vp, i64, vp, vp, T, vp, i64, vp, vp, i64, vp]),
         }
         for name, (res, args) in sig.items():
             f = getattr(L, name)

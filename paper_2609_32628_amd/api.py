@@ -18,7 +18,7 @@ import numpy as np
 import torch
 
 from . import _lib
-from ._lib import (DA2_BF16, DA2_ERR_WORKSPACE, DA2_FMT4_MXFP4, DA2_FMT4_NVFP4, DA2_FP16, DA2_FP32, DA2_NORM_LAYER, DA2_NORM_RMS,
+from ._lib import (DA2_ACT_GELU, DA2_ACT_GELU_TANH, DA2_ACT_NONE, DA2_ACT_RELU, DA2_ACT_SIGMOID, DA2_ACT_SILU, DA2_BF16, DA2_ERR_WORKSPACE, DA2_FMT4_MXFP4, DA2_FMT4_NVFP4, DA2_FP16, DA2_FP32, DA2_NORM_LAYER, DA2_NORM_RMS,
                    DA2_PART_RAGGED, DA2_PART_TILES8, DA2_ROPE_HALF, DA2_ROPE_INTERLEAVED, DA2_ROPE_LINEAR,
                    DA2_ROPE_NTK, DA2_ROPE_PLAIN, DA2_ROPE_YARN, DA2_SCOPE_HEAD, DA2_SCOPE_ROW, DiffProblem, NormDesc, Problem,
                    RopeDesc, RopeFreq, RopeRows, Rows, Tensor, check, lib)
@@ -484,3 +484,175 @@ def da2_diff_attn_bwd(Q, K, V, lam, lse, dO, dQ, dK, dV, dlam, ws, kv_lens=None,
     _run("da2_diff_attn_bwd", stream, (Q, K, V, lam, lse, dO, dQ, dK, dV, dlam, ws, kv_lens, q_start), p, Q.data_ptr(), q,
          K.data_ptr(), k, V.data_ptr(), v, l, kl, qs, ls, dO.data_ptr(), do, dQ.data_ptr(), dq, dK.data_ptr(), dk,
          dV.data_ptr(), dv, dl, _addr(ws), _bytes(ws))
+
+
+# ---- the rest of a layer: norm and rotation of Q and K, projections, gated blocks -------
+ACTS = {"none": DA2_ACT_NONE, "relu": DA2_ACT_RELU, "gelu": DA2_ACT_GELU, "gelu_tanh": DA2_ACT_GELU_TANH, "silu": DA2_ACT_SILU,
+        "sigmoid": DA2_ACT_SIGMOID}
+
+
+def _head_weights(d, given, kind, eps, plus_one, dtype):
+    """NormDesc of a norm over heads of d channels with weights [d] (``given``: by name)."""
+    wdtype = None
+    for name, t in given:
+        if t is None:
+            continue
+        if t.dtype not in DTYPES or t.shape != (d,) or not t.is_contiguous():
+            raise ValueError(f"{name}: expected contiguous weights [{d}]")
+        if wdtype is not None and t.dtype != wdtype:
+            raise ValueError("the weights (and their gradients) must share a dtype")
+        wdtype = t.dtype
+    return NormDesc(NORM_KINDS[kind], DTYPES[wdtype or dtype], int(plus_one), 0, 0, float(eps))
+
+
+def da2_qk_norm_rope(rope, Q, Qo, K=None, Ko=None, w_q=None, w_k=None, kind="rms", eps=1e-6, plus_one=False, pos=None, grid=None,
+                     stream=None):
+    """Qo (and Ko) = rotation of the normalised heads of Q (and K) times w_q (w_k), or 1 + w: da2_norm over the heads and da2_rope
+    in one pass. w_q, w_k: [d]. pos and grid as in da2_rope. Qo and Ko may be Q and K."""
+    tensors, desc, turns, scale, p, stride, rows, *io = _rope_args(rope, Q, Qo, K, Ko, pos, grid, False)
+    n = _head_weights(Q.shape[3], (("w_q", w_q), ("w_k", w_k)), kind, eps, plus_one, Q.dtype)
+    _run("da2_qk_norm_rope", stream, tensors + (w_q, w_k), desc, turns, scale, p, stride, rows, n, _addr(w_q), _addr(w_k), *io)
+
+
+def da2_qk_norm_rope_ws_bytes(Q, K=None):
+    """Workspace bytes of da2_qk_norm_rope_bwd for the gradients of the weights."""
+    _rows("Q", Q)
+    B, Hq, N, d = Q.shape
+    out = ctypes.c_int64()
+    check("da2_qk_norm_rope_ws_bytes", lib().da2_qk_norm_rope_ws_bytes(
+        RopeRows(B, Hq, 0 if K is None else K.shape[1], N, d, 0, 0, 0), out))
+    return out.value
+
+
+def da2_qk_norm_rope_bwd(rope, dQo, Q, dQ, dKo=None, K=None, dK=None, w_q=None, w_k=None, dw_q=None, dw_k=None, kind="rms", eps=1e-6,
+                         plus_one=False, pos=None, grid=None, ws=None, stream=None):
+    """Gradients of da2_qk_norm_rope from its inputs Q and K; dw_q and dw_k are written where given. dQ and dK may be dQo and dKo, or
+    Q and K. ws: da2_qk_norm_rope_ws_bytes(Q, K), for dw_q and dw_k."""
+    if (K is None) != (dK is None):
+        raise ValueError("K, dKo and dK are given together")
+    tensors, desc, turns, scale, p, stride, rows, dqo, dqo_t, dq, dq_t, dko, dko_t, dk, dk_t = _rope_args(rope, dQo, dQ, dKo, dK, pos, grid, False)
+    q = _rows("Q", Q, dQo.shape, dQo.dtype)
+    k = None if K is None else _rows("K", K, dKo.shape if dKo is not None else None, dQo.dtype)
+    n = _head_weights(Q.shape[3], (("w_q", w_q), ("w_k", w_k), ("dw_q", dw_q), ("dw_k", dw_k)), kind, eps, plus_one, Q.dtype)
+    _run("da2_qk_norm_rope_bwd", stream, tensors + (Q, K, w_q, w_k, dw_q, dw_k, ws), desc, turns, scale, p, stride, rows, n, _addr(w_q),
+         _addr(w_k), dqo, dqo_t, Q.data_ptr(), q, dq, dq_t, dko, dko_t, _addr(K), k, dk, dk_t, _addr(dw_q), _addr(dw_k), _addr(ws), _bytes(ws))
+
+
+def _proj(X, Y, act="none"):
+    """Proj of rows X -> Y, and the input and output features."""
+    _rows("X", X)
+    _rows("Y", Y, dtype=X.dtype)
+    B, Hx, N, Cx = X.shape
+    if Y.shape[0] != B or Y.shape[2] != N:
+        raise ValueError(f"X {tuple(X.shape)} and Y {tuple(Y.shape)} do not belong together")
+    return _lib.Proj(B, N, Hx, Cx, Y.shape[1], Y.shape[3], ACTS[act], DTYPES[X.dtype]), Hx * Cx, Y.shape[1] * Y.shape[3]
+
+
+def _matrix(name, W, shape, dtype):
+    """Address and row stride of a matrix of the given shape and type whose rows are contiguous."""
+    if W.shape != shape or W.dtype != dtype or (shape[1] > 1 and W.stride(1) != 1):
+        raise ValueError(f"{name}: expected {dtype} [{shape[0]}, {shape[1]}] with contiguous rows")
+    return W.data_ptr(), W.stride(0) if shape[0] > 1 else -(-shape[1] // 8) * 8
+
+
+def _gate(gate, like, B, F, dtype):
+    """Distance between the samples' gates; ``like``: a gradient, laid out alike."""
+    for name, t in (("gate", gate), ("dgate", like)):
+        if t is not None and (t.dtype != dtype or t.shape not in ((F,), (B, F)) or (F > 1 and t.stride(-1) != 1)):
+            raise ValueError(f"{name}: expected {dtype} [{F}] or [{B}, {F}] with contiguous rows")
+    if gate is None:
+        return 0
+    per = gate.stride(0) if gate.dim() == 2 and B > 1 else 0
+    if gate.dim() == 2 and B > 1 and per < F:
+        raise ValueError("gate: the samples' gates overlap")
+    if like is not None and (like.shape != gate.shape or (per and like.stride(0) != per)):
+        raise ValueError("gate and dgate must share shape and strides")
+    return per
+
+
+def _z(X, Y, parts):
+    p, _, F = _proj(X, Y)
+    wide = -(-F // 8) * 8
+    return (p.B, p.N, wide) if parts == 1 else (p.B, p.N, 2, wide)
+
+
+def da2_linear_z(X, Y):
+    """An empty Z (float32) for da2_linear and da2_linear_bwd."""
+    return torch.empty(_z(X, Y, 1), device=X.device)
+
+
+def da2_glu_z(X, Y):
+    """An empty Z (float32) for da2_glu and da2_glu_bwd."""
+    return torch.empty(_z(X, Y, 2), device=X.device)
+
+
+def _ws_bytes(call, X, W, Y, train):
+    p, _, _ = _proj(X, Y)
+    out = ctypes.c_int64()
+    check(call, getattr(lib(), call)(p, int(train), out))
+    return out.value
+
+
+def da2_linear_ws_bytes(X, W, Y, train=False):
+    """Workspace bytes of da2_linear (train: and of da2_linear_bwd) for tensors of these shapes."""
+    return _ws_bytes("da2_linear_ws_bytes", X, W, Y, train)
+
+
+def da2_glu_ws_bytes(X, W, Y, train=False):
+    """Workspace bytes of da2_glu (train: and of da2_glu_bwd) for tensors of these shapes."""
+    return _ws_bytes("da2_glu_ws_bytes", X, W, Y, train)
+
+
+def da2_linear(X, W, Y, bias=None, act="none", gate=None, residual=None, Z=None, ws=None, stream=None):
+    """Y = residual + gate * act(X W' + bias). X [B, Hx, N, Cx] and Y [B, Hy, N, Cy]: rows of Hx Cx and Hy Cy features (hidden rows are
+    one block; heads as the attention has them). W: [Hy Cy, Hx Cx]; bias [Hy Cy]; gate [Hy Cy] or [B, Hy Cy]; residual like Y, or Y
+    itself. act: "none", "relu", "gelu", "gelu_tanh", "silu" or "sigmoid". Z: da2_linear_z(X, Y), for da2_linear_bwd. ws:
+    da2_linear_ws_bytes(X, W, Y)."""
+    p, K, F = _proj(X, Y, act)
+    x, y = _rows("X", X), _rows("Y", Y)
+    w, stride = _matrix("W", W, (F, K), X.dtype)
+    r = None if residual is None else _rows("residual", residual, Y.shape, X.dtype)
+    b = _plain("bias", bias, (F,), X.dtype)
+    z = _plain("Z", Z, _z(X, Y, 1), torch.float32)
+    _run("da2_linear", stream, (X, W, Y, bias, gate, residual, Z, ws), p, X.data_ptr(), x, w, stride, b, _addr(gate),
+         _gate(gate, None, p.B, F, X.dtype), _addr(residual), r, Y.data_ptr(), y, z, _addr(ws), _bytes(ws))
+    return Y
+
+
+def da2_linear_bwd(dY, X, W, Z=None, dX=None, dW=None, dbias=None, act="none", gate=None, dgate=None, ws=None, stream=None):
+    """Gradients of da2_linear (that of the residual is dY), written where given. Z: what da2_linear wrote, needed with an activation or
+    for dgate. ws: da2_linear_ws_bytes(X, W, Y, True)."""
+    p, K, F = _proj(X, dY, act)
+    x, dy = _rows("X", X), _rows("dY", dY)
+    w, stride = _matrix("W", W, (F, K), X.dtype)
+    dx = None if dX is None else _rows("dX", dX, X.shape, X.dtype)
+    dw, dstride = (None, 0) if dW is None else _matrix("dW", dW, (F, K), X.dtype)
+    db = _plain("dbias", dbias, (F,), X.dtype)
+    z = _plain("Z", Z, _z(X, dY, 1), torch.float32)
+    _run("da2_linear_bwd", stream, (X, W, dY, gate, Z, dX, dW, dbias, dgate, ws), p, dY.data_ptr(), dy, X.data_ptr(), x, w, stride,
+         _addr(gate), _gate(gate, dgate, p.B, F, X.dtype), z, _addr(dX), dx, dw, dstride, db, _addr(dgate), _addr(ws), _bytes(ws))
+
+
+def da2_glu(X, W, Y, bias=None, act="silu", Z=None, ws=None, stream=None):
+    """Y = act(X Wg' + bg) * (X Wu' + bu): W [2 F, K] holds the rows of Wg, then those of Wu, and bias [2 F] alike. Z: da2_glu_z(X, Y), for
+    da2_glu_bwd. ws: da2_glu_ws_bytes(X, W, Y). The rest as in da2_linear."""
+    p, K, F = _proj(X, Y, act)
+    x, y = _rows("X", X), _rows("Y", Y)
+    w, stride = _matrix("W", W, (2 * F, K), X.dtype)
+    b = _plain("bias", bias, (2 * F,), X.dtype)
+    z = _plain("Z", Z, _z(X, Y, 2), torch.float32)
+    _run("da2_glu", stream, (X, W, Y, bias, Z, ws), p, X.data_ptr(), x, w, stride, b, Y.data_ptr(), y, z, _addr(ws), _bytes(ws))
+    return Y
+
+
+def da2_glu_bwd(dY, X, W, Z, dX=None, dW=None, dbias=None, act="silu", ws=None, stream=None):
+    """Gradients of da2_glu, written where given. Z: what da2_glu wrote. ws: da2_glu_ws_bytes(X, W, Y, True)."""
+    p, K, F = _proj(X, dY, act)
+    x, dy = _rows("X", X), _rows("dY", dY)
+    w, stride = _matrix("W", W, (2 * F, K), X.dtype)
+    dx = None if dX is None else _rows("dX", dX, X.shape, X.dtype)
+    dw, dstride = (None, 0) if dW is None else _matrix("dW", dW, (2 * F, K), X.dtype)
+    db = _plain("dbias", dbias, (2 * F,), X.dtype)
+    z = _plain("Z", Z, _z(X, dY, 2), torch.float32)
+    _run("da2_glu_bwd", stream, (X, W, dY, Z, dX, dW, dbias, ws), p, dY.data_ptr(), dy, X.data_ptr(), x, w, stride, z, _addr(dX), dx, dw,
+         dstride, db, _addr(ws), _bytes(ws))

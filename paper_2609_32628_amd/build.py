@@ -13,7 +13,7 @@ CSRC = os.path.join(HERE, "csrc")
 OUT = os.path.join(HERE, "libda2.so")
 BUILD = os.path.join(HERE, "_build")
 SOURCES = ["host.cpp", "draft.hip", "rank.hip", "prep.hip", "attn.hip", "host_token.cpp", "norm.hip", "rope.hip",
-           "diff_fwd.hip", "diff_bwd.hip"]
+           "diff_fwd.hip", "diff_bwd.hip", "host_layer.cpp", "qk.hip", "product.hip", "product_bwd.hip"]
 HIPCC = os.environ.get("HIPCC", "/opt/rocm/bin/hipcc")
 FLAGS = [
     "--offload-arch=gfx950", "-O3", "-fPIC", "-std=c++20",

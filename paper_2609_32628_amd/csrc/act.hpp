@@ -1,0 +1,146 @@
+// Activations of the projections and their derivatives, in float32, and eight values
+// at a time of rows that may end inside them. Results are rounded to 16 bits after, so
+// exponentials come from v_exp_f32 (relative error of e^x below |x| 2^-23) and quotients
+// from v_rcp_f32.
+#pragma once
+
+#include "layer.hpp"
+#include "tile.hpp"
+
+namespace da2 {
+
+__device__ inline float exp_fast(float x) { return __builtin_amdgcn_exp2f(x * 1.4426950408889634f); }
+__device__ inline float rcp_fast(float x) { return __builtin_amdgcn_rcpf(x); }
+
+// Standard normal distribution function of z and exp(-z^2 / 2). The tail is
+// erfc(x) / 2 with erfc(x) = exp(-x^2) q(1 / (1 + x / 2)), x = |z| / sqrt 2: q is a polynomial
+// fitted to exp(x^2) erfc(x) over x in [0, 12], relative error 2.3e-6 in float32, so the small
+// values of the negative side keep their digits.
+__device__ inline float normal_cdf(float z, float& e) {
+  e = __builtin_amdgcn_exp2f(z * z * -0.72134752044448170f);
+  const float t = rcp_fast(__builtin_fmaf(__builtin_fabsf(z), 0.35355339059327376f, 1.0f));
+  float q = 0.08493691682815552f;
+  q = __builtin_fmaf(q, t, -0.34534457325935364f);
+  q = __builtin_fmaf(q, t, 0.3734673857688904f);
+  q = __builtin_fmaf(q, t, 0.048874229192733765f);
+  q = __builtin_fmaf(q, t, 0.2774653434753418f);
+  q = __builtin_fmaf(q, t, 0.27831903100013733f);
+  q = __builtin_fmaf(q, t, 0.2822796106338501f);
+  const float tail = 0.5f * e * (q * t);
+  return z < 0.0f ? tail : 1.0f - tail;
+}
+
+// f(z) and, where asked for, f'(z).
+template <int ACT, bool D>
+__device__ inline float act_one(float z, float& d) {
+  if constexpr (ACT == DA2_ACT_RELU) {
+    if (D) d = z > 0.0f ? 1.0f : 0.0f;
+    return z > 0.0f ? z : z * 0.0f;  // a NaN stays one
+  } else if constexpr (ACT == DA2_ACT_GELU) {
+    float e;
+    const float p = normal_cdf(z, e);
+    if (D) d = __builtin_fmaf(z, e * 0.39894228040143268f, p);
+    return z * p;
+  } else if constexpr (ACT == DA2_ACT_GELU_TANH) {  // z (1 + tanh u) / 2 = z / (1 + exp(-2 u))
+    constexpr float a = 2 * 0.79788456080286536f, b = a * 0.044715f;
+    const float zz = z * z, p = rcp_fast(1.0f + exp_fast(-z * __builtin_fmaf(zz, b, a)));
+    if (D) d = __builtin_fmaf(z * (p - p * p), __builtin_fmaf(zz, 3 * b, a), p);
+    return z * p;
+  } else if constexpr (ACT == DA2_ACT_SILU) {
+    const float p = rcp_fast(1.0f + exp_fast(-z));
+    if (D) d = __builtin_fmaf(z, p - p * p, p);
+    return z * p;
+  } else if constexpr (ACT == DA2_ACT_SIGMOID) {
+    const float p = rcp_fast(1.0f + exp_fast(-z));
+    if (D) d = p - p * p;
+    return p;
+  } else {
+    if (D) d = 1.0f;
+    return z;
+  }
+}
+// Calls f<ACT>() (one branch for the whole wave).
+template <typename F>
+__device__ inline void with_act(int act, F&& f) {
+  switch (act) {
+    case DA2_ACT_RELU: return f.template operator()<DA2_ACT_RELU>();
+    case DA2_ACT_GELU: return f.template operator()<DA2_ACT_GELU>();
+    case DA2_ACT_GELU_TANH: return f.template operator()<DA2_ACT_GELU_TANH>();
+    case DA2_ACT_SILU: return f.template operator()<DA2_ACT_SILU>();
+    case DA2_ACT_SIGMOID: return f.template operator()<DA2_ACT_SIGMOID>();
+    default: return f.template operator()<DA2_ACT_NONE>();
+  }
+}
+__device__ inline void act8(int act, float* z) {
+  with_act(act, [&]<int ACT>() {
+    float d;
+#pragma unroll
+    for (int i = 0; i < 8; ++i) z[i] = act_one<ACT, false>(z[i], d);
+  });
+}
+
+// Eight elements at p (n of them are the row's) as floats, and back.
+template <typename T>
+__device__ inline void load8(const void* p, int64_t at, int n, float* x) {
+  load_part(static_cast<const T*>(p) + at, n, x);
+}
+template <typename T>
+__device__ inline void store8(void* p, int64_t at, int n, const float* x) {
+  store_part(static_cast<T*>(p) + at, n, x);
+}
+
+// Eight floats at p, of which n are the row's.
+__device__ inline void load_eight(const float* p, int n, float* x) {
+  load_part(p, n, x);
+  load_part(p + 4, n - 4, x + 4);
+}
+__device__ inline void store_eight(float* p, int n, const float* x) {
+  store_part(p, n, x);
+  store_part(p + 4, n - 4, x + 4);
+}
+
+// Element offset of feature f of rows whose features are blocks of C, sh apart.
+__device__ inline int64_t feature_at(int f, int H, int C, int64_t sh) {
+  if (H == 1) return f;
+  const int h = f / C;
+  return h * sh + (f - h * C);
+}
+
+// Features [f8, f8 + 8) of row m (token n of sample b) from their sums v (gated block: v and u).
+template <typename T, bool GLU>
+__device__ inline void finish8(const Finish& e, float* v, float* u, int64_t m, int b, int n, int f8) {
+  const int left = e.F - f8;
+  float x[8];
+  if (e.bias) {
+    load8<T>(e.bias, f8, left, x);
+#pragma unroll
+    for (int i = 0; i < 8; ++i) v[i] += x[i];
+    if constexpr (GLU) {
+      load8<T>(e.bias, static_cast<int64_t>(e.F) + f8, left, x);
+#pragma unroll
+      for (int i = 0; i < 8; ++i) u[i] += x[i];
+    }
+  }
+  if (e.z) {
+    float* at = e.z + m * (GLU ? 2 : 1) * e.z_ld + f8;
+    store_eight(at, left, v);
+    if constexpr (GLU) store_eight(at + e.z_ld, left, u);
+  }
+  act8(e.act, v);
+  if constexpr (GLU) {
+#pragma unroll
+    for (int i = 0; i < 8; ++i) v[i] *= u[i];
+  } else if (e.gate) {
+    load8<T>(e.gate, b * e.gate_sb + f8, left, x);
+#pragma unroll
+    for (int i = 0; i < 8; ++i) v[i] *= x[i];
+  }
+  if (!GLU && e.r.p) {
+    load8<T>(e.r.p, b * e.r.sb + n * e.r.sn + feature_at(f8, e.Hy, e.Cy, e.r.sh), left, x);
+#pragma unroll
+    for (int i = 0; i < 8; ++i) v[i] += x[i];
+  }
+  store8<T>(e.y.p, b * e.y.sb + n * e.y.sn + feature_at(f8, e.Hy, e.Cy, e.y.sh), left, v);
+}
+
+}  // namespace da2

@@ -12,15 +12,10 @@
 // product as they are, whose 16-row step s takes rows 16 g + 8 s + e.
 #pragma once
 
-#include "common.hpp"
-#include "token.hpp"
+#include "tile.hpp"
 
 namespace da2 {
 namespace diff {
-
-typedef short s16x4 __attribute__((ext_vector_type(4)));
-typedef short s16x8 __attribute__((ext_vector_type(8)));
-typedef bf16_t bf16x8 __attribute__((ext_vector_type(8)));
 
 constexpr float kLog2e = 1.4426950408889634f;
 constexpr float kLn2 = 0.6931471805599453f;
@@ -29,25 +24,6 @@ constexpr float kLn2 = 0.6931471805599453f;
 constexpr float kNoMax = -3.0e38f;
 
 __device__ inline float exp2_fast(float x) { return __builtin_amdgcn_exp2f(x); }
-
-// ---- MFMA on fragments of 8 16-bit values --------------------------------------------
-template <typename T>
-__device__ inline f32x16 mma(const s16x8& a, const s16x8& b, const f32x16& c) {
-  if constexpr (__is_same(T, bf16_t)) {
-    return __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, a), __builtin_bit_cast(bf16x8, b), c, 0, 0, 0);
-  } else {
-    return __builtin_amdgcn_mfma_f32_32x32x16_f16(__builtin_bit_cast(f16x8, a), __builtin_bit_cast(f16x8, b), c, 0, 0, 0);
-  }
-}
-// Eight floats rounded to T (nearest even).
-template <typename T>
-__device__ inline s16x8 pack8(const float* x) {
-  typedef T Tx8 __attribute__((ext_vector_type(8)));
-  Tx8 v;
-#pragma unroll
-  for (int i = 0; i < 8; ++i) v[i] = static_cast<T>(x[i]);
-  return __builtin_bit_cast(s16x8, v);
-}
 
 // The sum of eight values of T and s.
 template <typename T>
@@ -78,17 +54,6 @@ struct Tile {
     return hi | ((r >> 2) & 1) | ((((r >> 3) ^ (r >> 4)) & 1) << 1);
   }
 };
-
-typedef __attribute__((address_space(3))) const s16x8* lds_s16x8;
-typedef __attribute__((address_space(3))) s16x4* lds_s16x4;
-
-__device__ inline uint32_t lds_offset(const void* p) {
-  return static_cast<uint32_t>(reinterpret_cast<uintptr_t>((__attribute__((address_space(3))) const void*)p));
-}
-__device__ inline s16x8 read_b128(uint32_t at) { return *reinterpret_cast<lds_s16x8>(at); }
-__device__ inline s16x4 read_tr(uint32_t at) {
-  return __builtin_amdgcn_ds_read_tr16_b64_v4i16(reinterpret_cast<lds_s16x4>(at));
-}
 
 __device__ inline int kappa(int l) { return 16 * ((l / 4) % 2) + 4 * (l / 8) + l % 4; }
 
@@ -128,12 +93,6 @@ struct ColReader {
 // wave. The wave's rows start at LDS byte `lds` (a row of the tile that is a
 // multiple of kRowsPerCopy); rows behind `last` repeat it, so nothing beyond the
 // tensor's valid rows is read and the tile holds no stray values.
-// Issued as assembly, since the compiler would wait for it before every LDS read
-// that follows; the kernels wait for their copies themselves.
-__device__ inline void copy_1k(const void* base, uint32_t voff, uint32_t lds) {
-  asm volatile("s_mov_b32 m0, %2\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %0, %1" ::"v"(voff), "s"(base), "s"(lds)
-               : "memory", "m0");
-}
 template <int D>
 __device__ inline void copy_rows(const void* base, int64_t row_bytes, int row, int last, int lane, uint32_t lds) {
   constexpr int C = Tile<D>::kChunks;
@@ -142,10 +101,6 @@ __device__ inline void copy_rows(const void* base, int64_t row_bytes, int row, i
   const uint32_t voff = static_cast<uint32_t>(min(r, last)) * static_cast<uint32_t>(row_bytes) + chunk * 16;
   copy_1k(base, voff, __builtin_amdgcn_readfirstlane(lds));
 }
-// The wave's copies have arrived, and its reads of LDS have been answered (so that
-// after a barrier no read is left that the next copy could overtake).
-__device__ inline void wait_copies() { asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)" ::: "memory"); }
-__device__ inline void barrier() { asm volatile("s_barrier" ::: "memory"); }
 
 // A workgroup's shape by how many waves share a row's keys, every SHARE-th 32 of a tile each: 4 waves with 128 rows and
 // 64-key tiles (1), 8 waves with 128 rows (2) or 64 rows (4) and 128-key tiles.
@@ -174,16 +129,6 @@ __device__ inline int key_limit(const DiffArgs& a, const Visible& s, int n) {
   const int64_t e = s.start + n + 1;
   return static_cast<int>(e < 0 ? 0 : e < s.len ? e : s.len);
 }
-
-// Workgroup id -> unit of work, such that each XCD (ids go around the eight of
-// them) has consecutive units, which share a head's keys in its L2; -1: none.
-// Units, rows of a key head and workgroups are 32-bit numbers (the host checks):
-// a 64-bit division costs a short call as much as a key tile.
-__device__ inline int unit_of(uint32_t id, int total) {
-  const int per = (total + 7) / 8, u = static_cast<int>(id % 8) * per + static_cast<int>(id / 8);
-  return u < total ? u : -1;
-}
-inline unsigned grid_of(int total) { return static_cast<unsigned>((total + 7) / 8 * 8); }
 
 __device__ inline float max16(const f32x16& v) {
   const float a = fmaxf(fmaxf(v[0], v[1]), v[2]), b = fmaxf(fmaxf(v[3], v[4]), v[5]);
