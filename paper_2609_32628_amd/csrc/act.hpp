@@ -106,9 +106,26 @@ __device__ inline int64_t feature_at(int f, int H, int C, int64_t sh) {
   return h * sh + (f - h * C);
 }
 
-// Features [f8, f8 + 8) of row m (token n of sample b) from their sums v (gated block: v and u).
+// Where a row's outputs, residual, gate and sums lie.
 template <typename T, bool GLU>
-__device__ inline void finish8(const Finish& e, float* v, float* u, int64_t m, int b, int n, int f8) {
+struct RowPlace {
+  T* y;
+  const T *r, *gate;
+  float* z;
+  __device__ RowPlace(const Finish& e, int64_t m) {
+    const int b = static_cast<int>(static_cast<uint32_t>(m) / static_cast<uint32_t>(e.N));
+    const int n = static_cast<int>(m - static_cast<int64_t>(b) * e.N);
+    y = static_cast<T*>(e.y.p) + b * e.y.sb + n * e.y.sn;
+    r = e.r.p ? static_cast<const T*>(e.r.p) + b * e.r.sb + n * e.r.sn : nullptr;
+    gate = e.gate ? static_cast<const T*>(e.gate) + b * e.gate_sb : nullptr;
+    z = e.z ? e.z + m * (GLU ? 2 : 1) * e.z_ld : nullptr;
+  }
+};
+
+// Features [f8, f8 + 8) of a row from their sums v (gated block: v and u); they lie in 32 features from fb on, a number that
+// is the same for the whole wave, or fb = f8.
+template <typename T, bool GLU>
+__device__ inline void finish8(const Finish& e, const RowPlace<T, GLU>& row, float* v, float* u, int f8, int fb) {
   const int left = e.F - f8;
   float x[8];
   if (e.bias) {
@@ -122,25 +139,26 @@ __device__ inline void finish8(const Finish& e, float* v, float* u, int64_t m, i
     }
   }
   if (e.z) {
-    float* at = e.z + m * (GLU ? 2 : 1) * e.z_ld + f8;
-    store_eight(at, left, v);
-    if constexpr (GLU) store_eight(at + e.z_ld, left, u);
+    store_eight(row.z + f8, left, v);
+    if constexpr (GLU) store_eight(row.z + e.z_ld + f8, left, u);
   }
   act8(e.act, v);
   if constexpr (GLU) {
 #pragma unroll
     for (int i = 0; i < 8; ++i) v[i] *= u[i];
   } else if (e.gate) {
-    load8<T>(e.gate, b * e.gate_sb + f8, left, x);
+    load8<T>(row.gate, f8, left, x);
 #pragma unroll
     for (int i = 0; i < 8; ++i) v[i] *= x[i];
   }
+  // features are blocks of Cy; 32 of them lie in one where blocks are whole 32s
+  const int h = e.Hy == 1 ? 0 : e.Cy % 32 == 0 ? fb / e.Cy : f8 / e.Cy, c = f8 - h * e.Cy;
   if (!GLU && e.r.p) {
-    load8<T>(e.r.p, b * e.r.sb + n * e.r.sn + feature_at(f8, e.Hy, e.Cy, e.r.sh), left, x);
+    load8<T>(row.r, h * e.r.sh + c, left, x);
 #pragma unroll
     for (int i = 0; i < 8; ++i) v[i] += x[i];
   }
-  store8<T>(e.y.p, b * e.y.sb + n * e.y.sn + feature_at(f8, e.Hy, e.Cy, e.y.sh), left, v);
+  store8<T>(row.y, h * e.y.sh + c, left, v);
 }
 
 }  // namespace da2

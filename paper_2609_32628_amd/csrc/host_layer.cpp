@@ -123,7 +123,7 @@ int32_t check_side(const void* p, const da2_tensor* t, const Ext& e, int32_t dty
 }
 int32_t check_weights(const void* W, int64_t stride, const Proj& e) {
   if (!W || !aligned16(W) || stride < e.K || stride % 8 || stride > (1 << 22)) return DA2_ERR_INVALID_ARG;
-  return e.parts > 1 && (e.F + 256) * stride >= (1ll << 31) ? DA2_ERR_INVALID_ARG : DA2_OK;
+  return e.parts > 1 && (e.F + 256) * stride >= (1ll << 31) - (1 << 16) ? DA2_ERR_INVALID_ARG : DA2_OK;
 }
 bool gate_ok(const void* gate, int64_t stride, const Proj& e) {
   return !gate || stride == 0 || (stride >= e.F && stride <= (1ll << 40));

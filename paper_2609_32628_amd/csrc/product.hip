@@ -10,6 +10,7 @@
 // lies at position c ^ (r / 2 % 8), so that the 16 rows of a read meet all banks.
 // In a gated block a wave's feature rows are half gate, half up, of the same features.
 #include <algorithm>
+#include <utility>
 
 #include "act.hpp"
 
@@ -17,9 +18,13 @@ namespace da2 {
 
 namespace {
 
-constexpr int kStep = 64;               // elements of K a step
-constexpr int kRowBytes = 2 * kStep;    // of a tile's row in LDS
+enum Mode { kLinear, kGated, kPartial };
 
+constexpr int kStep = 64;            // elements of K a step
+constexpr int kRowBytes = 2 * kStep;  // of a tile's row in LDS
+constexpr int kStage = 2048;          // LDS bytes of a wave's epilogue
+
+// Chunk c of row r lies at position c ^ swz(r), so that the 16 rows of a read meet all banks.
 __device__ inline int swz(int r) { return (r >> 1) & 7; }
 
 // Element offset of row r.
@@ -39,7 +44,7 @@ struct Walk {
   const char* at;
   int64_t jump;  // bytes from a block's last step to the next block's first
   int in, C;
-  __device__ Walk(const Side& s, int64_t row, int k) {
+  __device__ void start(const Side& s, int64_t row, int k) {
     const int h = k / s.C;
     in = k - h * s.C;
     C = s.C;
@@ -53,13 +58,38 @@ struct Walk {
   }
 };
 
-enum Mode { kLinear, kGated, kPartial };
+// Four copies of 1 KB to LDS from byte `to` on, by the lanes of a mask that is all or none of them (a branch would cut the
+// products' schedule). The immediate offset counts for both addresses: offsets v are 1 KB less from one to the next.
+__device__ inline void copy_4k(const void* base, const uint32_t* v, uint32_t to) {
+  asm volatile(
+      "s_mov_b32 m0, %5\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %0, %4\n\tglobal_load_lds_dwordx4 %1, %4 offset:1024\n\t"
+      "global_load_lds_dwordx4 %2, %4 offset:2048\n\tglobal_load_lds_dwordx4 %3, %4 offset:3072" ::"v"(v[0]),
+      "v"(v[1]), "v"(v[2]), "v"(v[3]), "s"(base), "s"(to)
+      : "memory", "m0");
+}
+__device__ inline void copy_4k_if(const void* base, const uint32_t* v, uint32_t to, int lanes) {
+  asm volatile(
+      "s_mov_b32 m0, %5\n\ts_mov_b32 exec_lo, %6\n\ts_mov_b32 exec_hi, %6\n\tglobal_load_lds_dwordx4 %0, %4\n\t"
+      "global_load_lds_dwordx4 %1, %4 offset:1024\n\tglobal_load_lds_dwordx4 %2, %4 offset:2048\n\t"
+      "global_load_lds_dwordx4 %3, %4 offset:3072\n\ts_mov_b64 exec, -1" ::"v"(v[0]),
+      "v"(v[1]), "v"(v[2]), "v"(v[3]), "s"(base), "s"(to), "s"(lanes)
+      : "memory", "m0");
+}
 
-template <int TW, int TT, int WW, int WT>
+__device__ inline void in_order() { asm volatile("" ::: "memory"); }
+
+
+// A workgroup's tile of TW feature rows and TT tokens, and its WW x WT waves. END: K is no whole number of steps.
+template <int MODE_, bool END, int TW_, int TT_, int WW_, int WT_>
 struct Shape {
-  static constexpr int kWaves = WW * WT, kW = TW / WW / 32, kT = TT / WT / 32;  // 32x32 blocks of a wave
-  static constexpr int kTile = (TW + TT) * kRowBytes;                           // LDS bytes of a step
-  static constexpr int kCopyW = TW / 8 / kWaves, kCopyT = TT / 8 / kWaves;      // 1 KB copies a wave makes
+  static constexpr int MODE = MODE_, TW = TW_, TT = TT_, WW = WW_, WT = WT_;
+  static constexpr bool kEnd = END;
+  static constexpr int kWaves = WW * WT, kW = TW / WW / 32, kT = TT / WT / 32;   // 32x32 blocks of a wave
+  static constexpr int kBlocks = MODE == kGated ? kW / 2 : kW;                   // blocks of features
+  static constexpr int kCopyW = TW / 8 / kWaves, kCopyT = TT / 8 / kWaves;       // 1 KB copies a wave makes of a step
+  static constexpr int kTile = (TW + TT) * kRowBytes;                            // LDS bytes of a step
+  static constexpr int kLds = 2 * kTile + kStage * kWaves;
+  static constexpr int kPerCu = 160 * 1024 / kLds;                               // workgroups of a CU
 };
 
 // Feature row of a tile's row q of the weights' side (gated: a wave's first half are part 0's).
@@ -75,143 +105,258 @@ __device__ inline int64_t weight_row(int tile, int q, int64_t R, int F) {
   }
 }
 
-template <typename T, int MODE, int TW, int TT, int WW, int WT>
-__global__ __launch_bounds__(64 * WW * WT, 2) void product_kernel(ProductArgs a, int tiles_w, int tiles_t, int splits) {
-  using S = Shape<TW, TT, WW, WT>;
-  __shared__ __attribute__((aligned(1024))) char lds[2 * S::kTile];
-  const uint32_t lds0 = lds_offset(lds);
-  const int tid = threadIdx.x, lane = tid % 64, wave = __builtin_amdgcn_readfirstlane(tid / 64);
-  const int wave_w = wave % WW, wave_t = wave / WW;
-  const int tiles = tiles_w * tiles_t, unit = unit_of(blockIdx.x, tiles * splits);
-  if (unit < 0) return;
-  const int split = unit / tiles, tile = unit - split * tiles;
-  // tiles in groups of 8 token tiles, token tiles first: those that run at once share rows in their XCD's L2
-  const int group = tile / (8 * tiles_w), in_group = tile - group * 8 * tiles_w, wide = min(8, tiles_t - group * 8);
-  const int tile_w = in_group / wide, tile_t = group * 8 + in_group - tile_w * wide;
-  const int64_t R = static_cast<int64_t>(a.parts) * a.f.F, m0 = static_cast<int64_t>(tile_t) * TT;
-
-  const int steps_all = (a.K + kStep - 1) / kStep, per = (steps_all + splits - 1) / splits;
-  const int step0 = split * per, steps = min(per, steps_all - step0);
-
-  // byte offsets of the chunks that this lane copies, from the tile's lowest row; rows behind the last repeat it
-  const int64_t w_first = MODE == kGated ? row_at(a.w, weight_row<MODE, TW, WW>(tile_w, 0, R, a.f.F))
-                                         : first_at(a.w, weight_row<MODE, TW, WW>(tile_w, 0, R, a.f.F),
-                                                    weight_row<MODE, TW, WW>(tile_w, TW - 1, R, a.f.F));
-  const int64_t t_first = first_at(a.t, m0, min(m0 + TT, a.M) - 1);
-  uint32_t off_w[S::kCopyW], off_t[S::kCopyT];
-#pragma unroll
-  for (int i = 0; i < S::kCopyW; ++i) {
-    const int q = (i * S::kWaves + wave) * 8 + lane / 8, chunk = (lane % 8) ^ swz(q);
-    off_w[i] = static_cast<uint32_t>(2 * (row_at(a.w, weight_row<MODE, TW, WW>(tile_w, q, R, a.f.F)) - w_first)) + chunk * 16;
+// A workgroup's units of work: tiles, or parts of K of a tile. Ids go around the eight XCDs; each XCD has consecutive
+// units, which its workgroups take in turn, and tiles come in groups of 8 token tiles, token tiles first: those that run
+// at once share rows in their XCD's L2.
+struct Units {
+  int unit, end, stride;
+  __device__ Units(int total) {
+    const int per = (total + 7) / 8, xcd = blockIdx.x % 8;
+    unit = xcd * per + blockIdx.x / 8;
+    end = min((xcd + 1) * per, total);
+    stride = gridDim.x / 8;
   }
-#pragma unroll
-  for (int i = 0; i < S::kCopyT; ++i) {
-    const int q = (i * S::kWaves + wave) * 8 + lane / 8, chunk = (lane % 8) ^ swz(q);
-    off_t[i] = static_cast<uint32_t>(2 * (row_at(a.t, min(m0 + q, a.M - 1)) - t_first)) + chunk * 16;
+};
+struct Unit {
+  int split, tile_w, tile_t, step0, steps;
+  __device__ Unit(int unit, int tiles_w, int tiles_t, int splits, int K) {
+    const int tiles = tiles_w * tiles_t;
+    split = unit / tiles;
+    const int tile = unit - split * tiles, group = tile / (8 * tiles_w), in_group = tile - group * 8 * tiles_w;
+    const int wide = min(8, tiles_t - group * 8);
+    tile_w = in_group / wide;
+    tile_t = group * 8 + in_group - tile_w * wide;
+    const int all = (K + kStep - 1) / kStep, per = (all + splits - 1) / splits;
+    step0 = split * per;
+    steps = min(per, all - step0);
   }
-  Walk walk_w(a.w, w_first, step0 * kStep), walk_t(a.t, t_first, step0 * kStep);
+};
 
-  // brings step s into buffer s % 2
-  const auto fetch = [&](int s) {
-    const uint32_t to = lds0 + (s & 1) * S::kTile;
-    const int k = (step0 + s) * kStep;
-    if (k + kStep <= a.K) {
+// The copies of a workgroup's steps into LDS, in order: step i goes to buffer i % 2.
+template <typename S>
+struct Copies {
+  static constexpr int TW = S::TW, TT = S::TT;
+  const ProductArgs& a;
+  const int tiles_w, tiles_t, splits;
+  Units units;
+  int k, left, lane, wave;  // element of the next step, steps left of the unit
+  uint32_t lds0, to;
+  Walk walk_w, walk_t;
+  uint32_t off_w[S::kCopyW], off_t[S::kCopyT];  // of the chunks that this lane copies, from the tile's lowest row
+
+  __device__ Copies(const ProductArgs& a_, int tiles_w_, int tiles_t_, int splits_, uint32_t lds, int lane_, int wave_)
+      : a(a_), tiles_w(tiles_w_), tiles_t(tiles_t_), splits(splits_), units(tiles_w_ * tiles_t_ * splits_), lane(lane_), wave(wave_), lds0(lds), to(lds) {
+    left = 0;
+    if (more()) start();
+  }
+  __device__ bool more() const { return units.unit < units.end; }
+  template <bool W>
+  __device__ int row(int i) const { return (wave * (W ? S::kCopyW : S::kCopyT) + i) * 8 + lane / 8; }  // of copy i
+  __device__ void start() {
+    const Unit u(units.unit, tiles_w, tiles_t, splits, a.K);
+    const int64_t R = static_cast<int64_t>(a.parts) * a.f.F, m0 = static_cast<int64_t>(u.tile_t) * TT;
+    const auto weight = [&](int q) { return weight_row<S::MODE, TW, S::WW>(u.tile_w, q, R, a.f.F); };
+    const int64_t w_first = S::MODE == kGated ? row_at(a.w, weight(0)) : first_at(a.w, weight(0), weight(TW - 1));
+    const int64_t t_first = first_at(a.t, m0, min(m0 + TT, a.M) - 1);
+    // rows behind the last repeat it
 #pragma unroll
-      for (int i = 0; i < S::kCopyW; ++i) copy_1k(walk_w.at, off_w[i], to + (i * S::kWaves + wave) * 1024);
+    for (int i = 0; i < S::kCopyW; ++i)
+      off_w[i] = static_cast<uint32_t>(2 * (row_at(a.w, weight(row<true>(i))) - w_first)) + ((lane % 8) ^ swz(row<true>(i))) * 16 + 1024 * (3 - i);
 #pragma unroll
-      for (int i = 0; i < S::kCopyT; ++i) copy_1k(walk_t.at, off_t[i], to + TW * kRowBytes + (i * S::kWaves + wave) * 1024);
-    } else {  // the end of K inside a step: through registers, zeros behind it
-      const auto part = [&](const char* at, uint32_t off, uint32_t dst, int q) {
-        const int left = a.K - k - ((lane % 8) ^ swz(q)) * 8;
-        uint4 v = make_uint4(0, 0, 0, 0);
-        const char* p = at + off;
-        if (left >= 8) {
-          v = *reinterpret_cast<const uint4*>(p);
-        } else if (left > 0) {
-          uint32_t e[4] = {};
+    for (int i = 0; i < S::kCopyT; ++i)
+      off_t[i] = static_cast<uint32_t>(2 * (row_at(a.t, min(m0 + row<false>(i), a.M - 1)) - t_first)) + ((lane % 8) ^ swz(row<false>(i))) * 16 + 1024 * (3 - i);
+    walk_w.start(a.w, w_first, u.step0 * kStep);
+    walk_t.start(a.t, t_first, u.step0 * kStep);
+    k = u.step0 * kStep;
+    left = u.steps;
+  }
+  // Whether there is a next step and it is whole.
+  __device__ bool whole() const { return more() && (!S::kEnd || k + kStep <= a.K); }
+  // The copies of one side of the step.
+  template <bool W>
+  __device__ void side(int lanes) {
+    const uint32_t at = to + (W ? wave * (S::kCopyW * 1024) : TW * kRowBytes + wave * (S::kCopyT * 1024));
+    if constexpr (S::kEnd) copy_4k_if((W ? walk_w.at : walk_t.at) - 3072, W ? off_w : off_t, at, lanes);
+    else copy_4k((W ? walk_w.at : walk_t.at) - 3072, W ? off_w : off_t, at);
+  }
+  // The end of K inside a step: through registers, zeros behind it.
+  __device__ void copy_end(char* lds) {
 #pragma unroll
-          for (int i = 0; i < 8; ++i)
-            if (i < left) e[i / 2] |= static_cast<uint32_t>(reinterpret_cast<const uint16_t*>(p)[i]) << (16 * (i % 2));
-          v = make_uint4(e[0], e[1], e[2], e[3]);
-        }
-        *reinterpret_cast<uint4*>(lds + (dst - lds0) + lane * 16) = v;
-      };
+    for (int i = 0; i < S::kCopyW + S::kCopyT; ++i) {
+      const bool w = i < S::kCopyW;
+      const int c = w ? i : i - S::kCopyW, rest = a.K - k - ((lane % 8) ^ swz(w ? row<true>(c) : row<false>(c))) * 8;
+      const char* p = (w ? walk_w.at + off_w[w ? c : 0] : walk_t.at + off_t[w ? 0 : c]) - 1024 * (3 - c);
+      uint4 v = make_uint4(0, 0, 0, 0);
+      if (rest >= 8) {
+        v = *reinterpret_cast<const uint4*>(p);
+      } else if (rest > 0) {
+        uint32_t e[4] = {};
 #pragma unroll
-      for (int i = 0; i < S::kCopyW; ++i)
-        part(walk_w.at, off_w[i], to + (i * S::kWaves + wave) * 1024, (i * S::kWaves + wave) * 8 + lane / 8);
-#pragma unroll
-      for (int i = 0; i < S::kCopyT; ++i)
-        part(walk_t.at, off_t[i], to + TW * kRowBytes + (i * S::kWaves + wave) * 1024, (i * S::kWaves + wave) * 8 + lane / 8);
+        for (int j = 0; j < 8; ++j)
+          if (j < rest) e[j / 2] |= static_cast<uint32_t>(reinterpret_cast<const uint16_t*>(p)[j]) << (16 * (j % 2));
+        v = make_uint4(e[0], e[1], e[2], e[3]);
+      }
+      *reinterpret_cast<uint4*>(lds + (to - lds0) + (w ? wave * S::kCopyW : TW / 8 + wave * S::kCopyT) * 1024 + c * 1024 + lane * 16) = v;
+    }
+  }
+  __device__ void next() {
+    to = lds0 + (to == lds0 ? S::kTile : 0);
+    if (!more()) return;
+    if (--left == 0) {
+      units.unit += units.stride;
+      if (more()) start();  // else the last step is copied again, to where it is not read
+      return;
     }
     walk_w.next();
     walk_t.next();
-  };
+    k += kStep;
+  }
+  __device__ void step(char* lds) {
+    if (whole()) {
+      side<true>(-1);
+      side<false>(-1);
+    } else if (more()) {
+      copy_end(lds);
+    }
+    next();
+  }
+};
+
+template <typename T, typename S>
+__global__ __launch_bounds__(64 * S::kWaves, 2) void product_kernel(ProductArgs a, int tiles_w, int tiles_t, int splits) {
+  constexpr int MODE = S::MODE, TW = S::TW, TT = S::TT, WW = S::WW;
+  __shared__ __attribute__((aligned(1024))) char lds[S::kLds];
+  const int lane = threadIdx.x % 64, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64);
+  const int wave_w = wave % WW, wave_t = wave / WW;
+  char* const stage = lds + 2 * S::kTile + wave * kStage;
+  const uint32_t lds0 = lds_offset(lds);
+  const int64_t R = static_cast<int64_t>(a.parts) * a.f.F;
+  Units mine(tiles_w * tiles_t * splits);
+  if (mine.unit >= mine.end) return;
+  Copies<S> copies(a, tiles_w, tiles_t, splits, lds0, lane, wave);
+  copies.step(lds);
 
   f32x16 acc[S::kW][S::kT];
+  const auto clear = [&] {
 #pragma unroll
-  for (int i = 0; i < S::kW; ++i)
+    for (int i = 0; i < S::kW; ++i)
 #pragma unroll
-    for (int j = 0; j < S::kT; ++j) acc[i][j] = f32x16{};
-
-  // chunk 2 s + lane / 32 of a wave's rows: the positions differ in the address bits of a row's chunks only
+      for (int j = 0; j < S::kT; ++j) acc[i][j] = f32x16{};
+  };
+  clear();
+  // chunk 2 c + lane / 32 of a wave's rows: the positions differ in the address bits of a row's chunks only
   const uint32_t read = (lane % 32) * kRowBytes + (((lane / 32) ^ swz(lane % 32)) << 4);
   const uint32_t read_w = wave_w * S::kW * 32 * kRowBytes + read, read_t = TW * kRowBytes + wave_t * S::kT * 32 * kRowBytes + read;
-  if (steps > 0) fetch(0);
-  for (int s = 0; s < steps; ++s) {
-    wait_copies();
-    barrier();
-    if (s + 1 < steps) fetch(s + 1);
-    const uint32_t at = lds0 + (s & 1) * S::kTile;
+  s16x8 frag[2][S::kW + S::kT];
+  const auto fetch = [&](uint32_t at, int c, int i) {
+    return i < S::kW ? read_b128(((at + read_w) ^ (c << 5)) + i * 32 * kRowBytes)
+                     : read_b128(((at + read_t) ^ (c << 5)) + (i - S::kW) * 32 * kRowBytes);
+  };
+  constexpr int kProducts = S::kW * S::kT, kReads = S::kW + S::kT;
+  static_assert(S::kCopyW == 4 && S::kCopyT == 4);
+  static_assert(kReads <= 2 * kProducts);
+  // The products of 16 elements of K, with the reads of the next 16's operands and a step's copies of one side (1: weights, 2:
+  // tokens) among them.
+  const auto products = [&]<int SIDE>(uint32_t from, int c, const s16x8* f, s16x8* into, int lanes) {
+    const auto product = [&]<int P>() {
+      // two reads a product: those that the next 16's first products take come first
 #pragma unroll
-    for (int c = 0; c < 4; ++c) {
-      s16x8 w[S::kW], t[S::kT];
+      for (int q = 2 * P; q < 2 * P + 2 && q < kReads; ++q) {
+        const int i = q == 0 ? 0 : q <= S::kT ? S::kW + q - 1 : q - S::kT;
+        into[i] = fetch(from, c, i);
+      }
+      if constexpr (SIDE && P == kProducts / 2 - 1) copies.template side<SIDE == 1>(lanes);
+      acc[P / S::kT][P % S::kT] = mma<T>(f[P / S::kT], f[S::kW + P % S::kT], acc[P / S::kT][P % S::kT]);
+      __builtin_amdgcn_sched_barrier(0);
+    };
+    [&]<int... P>(std::integer_sequence<int, P...>) { (product.template operator()<P>(), ...); }(std::make_integer_sequence<int, kProducts>{});
+  };
+  const auto mask = [&](bool whole) { return __builtin_amdgcn_readfirstlane(whole ? -1 : 0); };
+  bool whole = copies.whole();
+  if (whole) copies.template side<true>(-1);
+  uint32_t at = lds0;
+  wait_copies();
+  barrier();
 #pragma unroll
-      for (int i = 0; i < S::kW; ++i) w[i] = read_b128(((at + read_w) ^ (c << 5)) + i * 32 * kRowBytes);
-#pragma unroll
-      for (int j = 0; j < S::kT; ++j) t[j] = read_b128(((at + read_t) ^ (c << 5)) + j * 32 * kRowBytes);
-#pragma unroll
-      for (int i = 0; i < S::kW; ++i)
-#pragma unroll
-        for (int j = 0; j < S::kT; ++j) acc[i][j] = mma<T>(w[i], t[j], acc[i][j]);
-    }
-  }
+  for (int i = 0; i < kReads; ++i) frag[0][i] = fetch(at, 0, i);
 
-  const int g = lane / 32;
+  for (; mine.unit < mine.end; mine.unit += mine.stride) {
+    const Unit u(mine.unit, tiles_w, tiles_t, splits, a.K);
+    for (int s = 0; s < u.steps; ++s) {
+      products.template operator()<2>(at, 1, frag[0], frag[1], mask(whole));
+      products.template operator()<0>(at, 2, frag[1], frag[0], 0);
+      if (S::kEnd && copies.more() && !whole) copies.copy_end(lds);
+      copies.next();
+      whole = copies.whole();
+      products.template operator()<0>(at, 3, frag[0], frag[1], 0);
+      // the next step has arrived, and every wave's reads of this one have been answered: its buffer takes the one after
+      wait_copies();
+      barrier();
+      at = lds0 + (at == lds0 ? S::kTile : 0);
+      products.template operator()<1>(at, 0, frag[1], frag[0], mask(whole));
+    }
+
+    // The epilogue, 16 tokens and 32 features at a time: the sums go through the wave's 2 KB of LDS, so that one piece of
+    // code with 8 features of a token a lane serves all blocks (unrolled over the blocks' registers it was 170 KB of
+    // instructions, whose fetches took 18 us a tile).
+    const int64_t m0 = static_cast<int64_t>(u.tile_t) * TT + wave_t * S::kT * 32;
+    const int f0 = (u.tile_w * WW + wave_w) * (32 * S::kBlocks), chunk = lane % 4;
+    const auto put = [&](const f32x16& x) {
 #pragma unroll
-  for (int j = 0; j < S::kT; ++j) {
-    const int64_t m = m0 + (wave_t * S::kT + j) * 32 + lane % 32;
-    const bool live = m < a.M;
-    const int b = static_cast<int>(static_cast<uint32_t>(live ? m : 0) / static_cast<uint32_t>(a.f.N));
-    const int n = static_cast<int>((live ? m : 0) - static_cast<int64_t>(b) * a.f.N);
-    // eight features in a row of the lane's token: quads k and k + 1 of the lane halves
-    const auto eight = [&](const f32x16& x, int k, float* v) {
+      for (int q = 0; q < 4; ++q)
+        *reinterpret_cast<f32x4*>(stage + lane % 16 * 128 + (((2 * q + lane / 32) ^ (lane % 8)) << 4)) = f32x4{x[4 * q], x[4 * q + 1], x[4 * q + 2], x[4 * q + 3]};
+    };
+    const auto take = [&](float* v) {
+      const int row = lane / 4;
 #pragma unroll
-      for (int e = 0; e < 4; ++e) {
-        const auto p = __builtin_amdgcn_permlane32_swap(__float_as_uint(x[4 * k + e]), __float_as_uint(x[4 * k + 4 + e]), false, false);
-        v[e] = __uint_as_float(p[0]);
-        v[4 + e] = __uint_as_float(p[1]);
+      for (int h = 0; h < 2; ++h) {
+        const f32x4 x = *reinterpret_cast<const f32x4*>(stage + row * 128 + (((2 * chunk + h) ^ (row % 8)) << 4));
+#pragma unroll
+        for (int e = 0; e < 4; ++e) v[4 * h + e] = x[e];
       }
     };
-    constexpr int blocks = MODE == kGated ? S::kW / 2 : S::kW;
-#pragma unroll
-    for (int i = 0; i < blocks; ++i)
-#pragma unroll
-      for (int k = 0; k < 4; k += 2) {
-        float v[8], u[8];
-        eight(acc[i][j], k, v);
-        if constexpr (MODE == kGated) eight(acc[i + blocks][j], k, u);
-        const int64_t f8 = (static_cast<int64_t>(tile_w) * WW + wave_w) * (32 * blocks) + i * 32 + 8 * (k + g);
+#pragma unroll 1
+    for (int t16 = 0; t16 < 2 * S::kT; ++t16) {
+      const int64_t m = m0 + t16 * 16 + lane / 4;
+      const bool live = m < a.M;
+      const RowPlace<T, MODE == kGated> row(a.f, live ? m : a.M - 1);
+      const bool writes = lane % 32 / 16 == t16 % 2;
+#pragma unroll 1
+      for (int i = 0; i < S::kBlocks; ++i) {
+        const auto put_block = [&]<int SECOND>() {
+          if (!writes) return;
+          const auto one = [&]<int B>() {
+            if (i + t16 / 2 * S::kBlocks == B) put(acc[B % S::kBlocks + SECOND * S::kBlocks][B / S::kBlocks]);
+          };
+          [&]<int... B>(std::integer_sequence<int, B...>) { (one.template operator()<B>(), ...); }(std::make_integer_sequence<int, S::kBlocks * S::kT>{});
+        };
+        // the wave's lanes read what others wrote: LDS takes its accesses in order, and the compiler has to leave them so
+        float v[8], w[8];
+        put_block.template operator()<0>();
+        in_order();
+        take(v);
+        in_order();
+        if constexpr (MODE == kGated) {
+          put_block.template operator()<1>();
+          in_order();
+          take(w);
+          in_order();
+        }
+        const int fb = f0 + i * 32, f8 = fb + 8 * chunk;
         if constexpr (MODE == kPartial) {
           if (live && f8 < R) {
-            float* to = a.ws + (static_cast<int64_t>(split) * a.M + m) * ((R + 7) / 8 * 8) + f8;
+            float* to = a.ws + (static_cast<int64_t>(u.split) * a.M + m) * ((R + 7) / 8 * 8) + f8;
             store_vec(to, v);
             store_vec(to + 4, v + 4);
           }
         } else if (live && f8 < a.f.F) {
-          finish8<T, MODE == kGated>(a.f, v, u, m, b, n, static_cast<int>(f8));
+          finish8<T, MODE == kGated>(a.f, row, v, w, f8, fb);
         }
       }
+    }
+    clear();
   }
+  wait_copies();  // LDS may become another workgroup's
 }
 
 // The partial sums of a split product added up in order, and the epilogue: a thread for eight features of a row.
@@ -237,8 +382,7 @@ __global__ __launch_bounds__(256) void product_join_kernel(ProductArgs a, int sp
       for (int i = 0; i < 8; ++i) u[i] += x[i];
     }
   }
-  const int b = static_cast<int>(m / a.f.N);
-  finish8<T, GLU>(a.f, v, u, m, b, static_cast<int>(m - static_cast<int64_t>(b) * a.f.N), f8);
+  finish8<T, GLU>(a.f, RowPlace<T, GLU>(a.f, m), v, u, f8, f8);
 }
 
 // How a product is cut: big tiles or small ones, and parts of K.
@@ -248,7 +392,7 @@ struct Plan {
 };
 Plan plan_of(int64_t M, int64_t R, int64_t K) {
   const int64_t big = ((M + 255) / 256) * ((R + 255) / 256), small = ((M + 127) / 128) * ((R + 127) / 128);
-  const int64_t steps = (K + kStep - 1) / kStep;
+  const int64_t steps = (K + 63) / 64;
   if (big >= 256) return {true, 1};
   int64_t splits = 1;
   while (small * splits * 2 <= 512 && steps / (splits * 2) >= 8) splits *= 2;
@@ -256,21 +400,25 @@ Plan plan_of(int64_t M, int64_t R, int64_t K) {
   return {false, static_cast<int>((steps + per - 1) / per)};
 }
 
-template <typename T, int MODE, int TW, int TT, int WW, int WT>
-hipError_t launch_tiles(const ProductArgs& a, int64_t features, int splits, hipStream_t stream) {
-  using S = Shape<TW, TT, WW, WT>;
-  const int64_t tw = (features + TW - 1) / TW, tt = (a.M + TT - 1) / TT;
-  const auto kernel = product_kernel<T, MODE, TW, TT, WW, WT>;
-  kernel<<<grid_of(static_cast<int>(tw * tt * splits)), 64 * S::kWaves, 0, stream>>>(a, static_cast<int>(tw), static_cast<int>(tt), splits);
+template <typename T, typename S>
+hipError_t launch_tiles(const ProductArgs& a, int splits, hipStream_t stream) {
+  // a gated tile's rows are two for each feature
+  const int64_t features = static_cast<int64_t>(a.parts) * a.f.F;
+  const int64_t tw = (features + S::TW - 1) / S::TW, tt = (a.M + S::TT - 1) / S::TT;
+  // as many workgroups as run at once, in eights
+  const int64_t units = (tw * tt * splits + 7) / 8 * 8, most = 256 * S::kPerCu;
+  product_kernel<T, S><<<static_cast<unsigned>(units < most ? units : most), 64 * S::kWaves, 0, stream>>>(a, static_cast<int>(tw), static_cast<int>(tt), splits);
   return hipGetLastError();
 }
 
+template <typename T, int MODE, bool END>
+hipError_t launch_plan(const ProductArgs& a, const Plan& p, hipStream_t stream) {
+  return p.big ? launch_tiles<T, Shape<MODE, END, 256, 256, 2, 4>>(a, p.splits, stream)
+               : launch_tiles<T, Shape<MODE, END, 128, 128, 2, 2>>(a, p.splits, stream);
+}
 template <typename T, int MODE>
 hipError_t launch_plan(const ProductArgs& a, const Plan& p, hipStream_t stream) {
-  // a gated tile's rows are two for each feature
-  const int64_t features = MODE == kGated ? 2 * static_cast<int64_t>(a.f.F) : static_cast<int64_t>(a.parts) * a.f.F;
-  return p.big ? launch_tiles<T, MODE, 256, 256, 2, 4>(a, features, p.splits, stream)
-               : launch_tiles<T, MODE, 128, 128, 2, 2>(a, features, p.splits, stream);
+  return a.K % kStep ? launch_plan<T, MODE, true>(a, p, stream) : launch_plan<T, MODE, false>(a, p, stream);
 }
 
 }  // namespace
@@ -286,7 +434,7 @@ int64_t product_ws_bytes(int64_t M, int64_t N, int64_t F, int64_t K, int parts) 
 hipError_t launch_product(const ProductArgs& a, hipStream_t stream) {
   // A tile addresses its token rows by 32 bits from the lowest. Samples further apart than that go one by one.
   const int64_t samples = a.M / a.t.N;
-  if (samples > 1 && (std::min<int64_t>(samples, 256 / a.t.N + 2) * a.t.sb + a.t.N * a.t.sn) >> 31) {
+  if (samples > 1 && (std::min<int64_t>(samples, 256 / a.t.N + 2) * a.t.sb + a.t.N * a.t.sn + (1 << 16)) >> 31) {
     for (int64_t b = 0; b < samples; ++b) {
       ProductArgs one = a;
       const auto skip = [&](const void* p, int64_t n) { return p ? static_cast<const char*>(p) + 2 * b * n : nullptr; };
