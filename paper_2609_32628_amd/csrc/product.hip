@@ -6,8 +6,7 @@
 // then features of one token, four in a row, and lanes l and l ^ 32 trade quads so that
 // the epilogue works on eight features in a row of one token with 16-byte accesses.
 // A tile takes K in steps of 64: 128 bytes of each row, brought into LDS by
-// asynchronous copies while the step before is multiplied. Chunk c (16 bytes) of row r
-// lies at position c ^ (r / 2 % 8), so that the 16 rows of a read meet all banks.
+// asynchronous copies while the step before is multiplied.
 // In a gated block a wave's feature rows are half gate, half up, of the same features.
 #include <algorithm>
 #include <utility>
@@ -21,11 +20,17 @@ namespace {
 enum Mode { kLinear, kGated, kPartial };
 
 constexpr int kStep = 64;            // elements of K a step
-constexpr int kRowBytes = 2 * kStep;  // of a tile's row in LDS
+constexpr int kRowBytes = 2 * kStep;  // of a tile's row
 constexpr int kStage = 2048;          // LDS bytes of a wave's epilogue
 
-// Chunk c of row r lies at position c ^ swz(r), so that the 16 rows of a read meet all banks.
-__device__ inline int swz(int r) { return (r >> 1) & 7; }
+// A step's rows lie in LDS in blocks of eight, as one copy of 1 KB brings them: 128 bytes of a row after the other, in the order
+// of the lanes. (Chunks that trade places within their 128 bytes make the copies slow: XXX TFLOP/s on 8,192^3.) Row
+// 64 q + 16 j + 2 b + p is line 2 j + p of block 8 q + b, and a block begins 16 bytes behind the one before, so that the 16 rows of
+// a read meet all banks.
+constexpr int kBlock = 1024 + 16;
+__device__ inline int row_of(int block, int line) { return block / 8 * 64 + line / 2 * 16 + block % 8 * 2 + line % 2; }
+// LDS byte of row r's first chunk, for r below 64.
+__device__ inline int line_at(int r) { return r % 16 / 2 * kBlock + (r / 16 * 2 + r % 2) * kRowBytes; }
 
 // Element offset of row r.
 __device__ inline int64_t row_at(const Side& s, int64_t r) {
@@ -58,21 +63,28 @@ struct Walk {
   }
 };
 
-// Four copies of 1 KB to LDS from byte `to` on, by the lanes of a mask that is all or none of them (a branch would cut the
-// products' schedule). The immediate offset counts for both addresses: offsets v are 1 KB less from one to the next.
-__device__ inline void copy_4k(const void* base, const uint32_t* v, uint32_t to) {
+// Four copies of 1 KB to the LDS blocks from byte `to` on, by the lanes of a mask that is all or none of them (a branch would
+// cut the products' schedule). The immediate offset counts for both addresses: offsets v are a block less from one to the next.
+// Buffer loads: global loads into LDS take the path of flat accesses, which holds up LDS reads and the products behind them
+// (XXX TFLOP/s on 8,192^3 instead of XXX).
+__device__ inline i32x4 buffer_at(const char* base) {
+  const uint64_t p = reinterpret_cast<uint64_t>(base);
+  // raw buffer: 48 bits of address, no stride, 2^32 - 1 bytes, 32-bit data format
+  return i32x4{__builtin_amdgcn_readfirstlane(static_cast<int>(p)), __builtin_amdgcn_readfirstlane(static_cast<int>(p >> 32 & 0xFFFF)), -1, 0x00020000};
+}
+__device__ inline void copy_4k(const i32x4& base, const uint32_t* v, uint32_t to) {
   asm volatile(
-      "s_mov_b32 m0, %5\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %0, %4\n\tglobal_load_lds_dwordx4 %1, %4 offset:1024\n\t"
-      "global_load_lds_dwordx4 %2, %4 offset:2048\n\tglobal_load_lds_dwordx4 %3, %4 offset:3072" ::"v"(v[0]),
-      "v"(v[1]), "v"(v[2]), "v"(v[3]), "s"(base), "s"(to)
+      "s_mov_b32 m0, %5\n\ts_nop 0\n\tbuffer_load_dwordx4 %0, %4, 0 offen lds\n\tbuffer_load_dwordx4 %1, %4, 0 offen offset:1040 lds\n\t"
+      "buffer_load_dwordx4 %2, %4, 0 offen offset:2080 lds\n\tbuffer_load_dwordx4 %3, %4, 0 offen offset:3120 lds" ::"v"(v[0]),
+      "v"(v[1]), "v"(v[2]), "v"(v[3]), "s"(base), "s"(__builtin_amdgcn_readfirstlane(to))
       : "memory", "m0");
 }
-__device__ inline void copy_4k_if(const void* base, const uint32_t* v, uint32_t to, int lanes) {
+__device__ inline void copy_4k_if(const i32x4& base, const uint32_t* v, uint32_t to, int lanes) {
   asm volatile(
-      "s_mov_b32 m0, %5\n\ts_mov_b32 exec_lo, %6\n\ts_mov_b32 exec_hi, %6\n\tglobal_load_lds_dwordx4 %0, %4\n\t"
-      "global_load_lds_dwordx4 %1, %4 offset:1024\n\tglobal_load_lds_dwordx4 %2, %4 offset:2048\n\t"
-      "global_load_lds_dwordx4 %3, %4 offset:3072\n\ts_mov_b64 exec, -1" ::"v"(v[0]),
-      "v"(v[1]), "v"(v[2]), "v"(v[3]), "s"(base), "s"(to), "s"(lanes)
+      "s_mov_b32 m0, %5\n\ts_mov_b32 exec_lo, %6\n\ts_mov_b32 exec_hi, %6\n\tbuffer_load_dwordx4 %0, %4, 0 offen lds\n\t"
+      "buffer_load_dwordx4 %1, %4, 0 offen offset:1040 lds\n\tbuffer_load_dwordx4 %2, %4, 0 offen offset:2080 lds\n\t"
+      "buffer_load_dwordx4 %3, %4, 0 offen offset:3120 lds\n\ts_mov_b64 exec, -1" ::"v"(v[0]),
+      "v"(v[1]), "v"(v[2]), "v"(v[3]), "s"(base), "s"(__builtin_amdgcn_readfirstlane(to)), "s"(__builtin_amdgcn_readfirstlane(lanes))
       : "memory", "m0");
 }
 
@@ -87,7 +99,8 @@ struct Shape {
   static constexpr int kWaves = WW * WT, kW = TW / WW / 32, kT = TT / WT / 32;   // 32x32 blocks of a wave
   static constexpr int kBlocks = MODE == kGated ? kW / 2 : kW;                   // blocks of features
   static constexpr int kCopyW = TW / 8 / kWaves, kCopyT = TT / 8 / kWaves;       // 1 KB copies a wave makes of a step
-  static constexpr int kTile = (TW + TT) * kRowBytes;                            // LDS bytes of a step
+  static constexpr int kSideW = TW / 8 * kBlock;                                  // LDS bytes of a step's feature rows
+  static constexpr int kTile = kSideW + TT / 8 * kBlock;                         // of a step
   static constexpr int kLds = 2 * kTile + kStage * kWaves;
   static constexpr int kPerCu = 160 * 1024 / kLds;                               // workgroups of a CU
 };
@@ -151,7 +164,7 @@ struct Copies {
   }
   __device__ bool more() const { return units.unit < units.end; }
   template <bool W>
-  __device__ int row(int i) const { return (wave * (W ? S::kCopyW : S::kCopyT) + i) * 8 + lane / 8; }  // of copy i
+  __device__ int row(int i) const { return row_of(wave * (W ? S::kCopyW : S::kCopyT) + i, lane / 8); }  // of copy i
   __device__ void start() {
     const Unit u(units.unit, tiles_w, tiles_t, splits, a.K);
     const int64_t R = static_cast<int64_t>(a.parts) * a.f.F, m0 = static_cast<int64_t>(u.tile_t) * TT;
@@ -161,10 +174,10 @@ struct Copies {
     // rows behind the last repeat it
 #pragma unroll
     for (int i = 0; i < S::kCopyW; ++i)
-      off_w[i] = static_cast<uint32_t>(2 * (row_at(a.w, weight(row<true>(i))) - w_first)) + ((lane % 8) ^ swz(row<true>(i))) * 16 + 1024 * (3 - i);
+      off_w[i] = static_cast<uint32_t>(2 * (row_at(a.w, weight(row<true>(i))) - w_first)) + lane % 8 * 16 + kBlock * (3 - i);
 #pragma unroll
     for (int i = 0; i < S::kCopyT; ++i)
-      off_t[i] = static_cast<uint32_t>(2 * (row_at(a.t, min(m0 + row<false>(i), a.M - 1)) - t_first)) + ((lane % 8) ^ swz(row<false>(i))) * 16 + 1024 * (3 - i);
+      off_t[i] = static_cast<uint32_t>(2 * (row_at(a.t, min(m0 + row<false>(i), a.M - 1)) - t_first)) + lane % 8 * 16 + kBlock * (3 - i);
     walk_w.start(a.w, w_first, u.step0 * kStep);
     walk_t.start(a.t, t_first, u.step0 * kStep);
     k = u.step0 * kStep;
@@ -175,17 +188,17 @@ struct Copies {
   // The copies of one side of the step.
   template <bool W>
   __device__ void side(int lanes) {
-    const uint32_t at = to + (W ? wave * (S::kCopyW * 1024) : TW * kRowBytes + wave * (S::kCopyT * 1024));
-    if constexpr (S::kEnd) copy_4k_if((W ? walk_w.at : walk_t.at) - 3072, W ? off_w : off_t, at, lanes);
-    else copy_4k((W ? walk_w.at : walk_t.at) - 3072, W ? off_w : off_t, at);
+    const uint32_t at = to + (W ? wave * (S::kCopyW * kBlock) : S::kSideW + wave * (S::kCopyT * kBlock));
+    if constexpr (S::kEnd) copy_4k_if(buffer_at((W ? walk_w.at : walk_t.at) - 3 * kBlock), W ? off_w : off_t, at, lanes);
+    else copy_4k(buffer_at((W ? walk_w.at : walk_t.at) - 3 * kBlock), W ? off_w : off_t, at);
   }
   // The end of K inside a step: through registers, zeros behind it.
   __device__ void copy_end(char* lds) {
 #pragma unroll
     for (int i = 0; i < S::kCopyW + S::kCopyT; ++i) {
       const bool w = i < S::kCopyW;
-      const int c = w ? i : i - S::kCopyW, rest = a.K - k - ((lane % 8) ^ swz(w ? row<true>(c) : row<false>(c))) * 8;
-      const char* p = (w ? walk_w.at + off_w[w ? c : 0] : walk_t.at + off_t[w ? 0 : c]) - 1024 * (3 - c);
+      const int c = w ? i : i - S::kCopyW, rest = a.K - k - lane % 8 * 8;
+      const char* p = (w ? walk_w.at + off_w[w ? c : 0] : walk_t.at + off_t[w ? 0 : c]) - kBlock * (3 - c);
       uint4 v = make_uint4(0, 0, 0, 0);
       if (rest >= 8) {
         v = *reinterpret_cast<const uint4*>(p);
@@ -196,7 +209,7 @@ struct Copies {
           if (j < rest) e[j / 2] |= static_cast<uint32_t>(reinterpret_cast<const uint16_t*>(p)[j]) << (16 * (j % 2));
         v = make_uint4(e[0], e[1], e[2], e[3]);
       }
-      *reinterpret_cast<uint4*>(lds + (to - lds0) + (w ? wave * S::kCopyW : TW / 8 + wave * S::kCopyT) * 1024 + c * 1024 + lane * 16) = v;
+      *reinterpret_cast<uint4*>(lds + (to - lds0) + ((w ? wave * S::kCopyW : TW / 8 + wave * S::kCopyT) + c) * kBlock + lane * 16) = v;
     }
   }
   __device__ void next() {
@@ -244,16 +257,16 @@ __global__ __launch_bounds__(64 * S::kWaves, 2) void product_kernel(ProductArgs 
       for (int j = 0; j < S::kT; ++j) acc[i][j] = f32x16{};
   };
   clear();
-  // chunk 2 c + lane / 32 of a wave's rows: the positions differ in the address bits of a row's chunks only
-  const uint32_t read = (lane % 32) * kRowBytes + (((lane / 32) ^ swz(lane % 32)) << 4);
-  const uint32_t read_w = wave_w * S::kW * 32 * kRowBytes + read, read_t = TW * kRowBytes + wave_t * S::kT * 32 * kRowBytes + read;
+  // chunk 2 c + lane / 32 of a wave's rows, 32 of them a read
+  const uint32_t read = line_at(lane % 32) + lane / 32 * 16;
+  const uint32_t read_w = wave_w * (S::kW * 4 * kBlock) + read, read_t = S::kSideW + wave_t * (S::kT * 4 * kBlock) + read;
   s16x8 frag[2][S::kW + S::kT];
   const auto fetch = [&](uint32_t at, int c, int i) {
-    return i < S::kW ? read_b128(((at + read_w) ^ (c << 5)) + i * 32 * kRowBytes)
-                     : read_b128(((at + read_t) ^ (c << 5)) + (i - S::kW) * 32 * kRowBytes);
+    const int n = i < S::kW ? i : i - S::kW;
+    return read_b128(at + (i < S::kW ? read_w : read_t) + n / 2 * 8 * kBlock + n % 2 * 4 * kRowBytes + c * 32);
   };
   constexpr int kProducts = S::kW * S::kT, kReads = S::kW + S::kT;
-  static_assert(S::kCopyW == 4 && S::kCopyT == 4);
+  static_assert(S::kCopyW == 4 && S::kCopyT == 4 && S::kW % 2 == 0 && S::kT % 2 == 0);
   static_assert(kReads <= 2 * kProducts);
   // The products of 16 elements of K, with the reads of the next 16's operands and a step's copies of one side (1: weights, 2:
   // tokens) among them.

@@ -85,20 +85,36 @@ __device__ inline void row_sum(float (&v)[N]) {
     for (int i = 0; i < N; ++i) v[i] += __shfl_xor(v[i], o, 64);
 }
 
+// A thread's share of a row as it lies in memory: it stays so while it is on its way.
+template <typename T, int V, bool HALF, int K>
+struct Fetched {
+  struct Some {
+    T v[V];
+  };
+  static constexpr int C = Unit<V, HALF>::kTwo ? 2 : 1;
+  Some c[K][C];
+  __device__ void load(const T* row, const Unit<V, HALF>* u) {
+#pragma unroll
+    for (int k = 0; k < K; ++k) {
+      c[k][0] = Some{};
+      if constexpr (C > 1) c[k][1] = Some{};
+      if (u[k].live) __builtin_memcpy(&c[k][0], row + u[k].i, sizeof(Some));
+      if constexpr (C > 1)
+        if (u[k].two()) __builtin_memcpy(&c[k][1], row + u[k].j, sizeof(Some));
+    }
+  }
+};
+
 // A thread's share of a row: W values of each of K units, the first V of chunk i and the others of chunk j.
 template <typename T, int V, bool HALF, int K>
 struct Share {
   static constexpr int W = Unit<V, HALF>::kTwo ? 2 * V : V;
   float v[K][W];
-  __device__ void load(const T* row, const Unit<V, HALF>* u) {
+  __device__ explicit Share(const Fetched<T, V, HALF, K>& f) {
 #pragma unroll
-    for (int k = 0; k < K; ++k) {
+    for (int k = 0; k < K; ++k)
 #pragma unroll
-      for (int e = 0; e < W; ++e) v[k][e] = 0.0f;
-      if (u[k].live) get<T, V>(row + u[k].i, v[k]);
-      if constexpr (W > V)
-        if (u[k].two()) get<T, V>(row + u[k].j, v[k] + V);
-    }
+      for (int e = 0; e < W; ++e) v[k][e] = static_cast<float>(f.c[k][e / V].v[e % V]);
   }
   __device__ void store(T* row, const Unit<V, HALF>* u) const {
 #pragma unroll
@@ -192,12 +208,12 @@ __global__ __launch_bounds__(kThreads) void qk_kernel(QkArgs a, int units, int h
   const int h0 = blockIdx.y * heads, h1 = min(h0 + heads, a.r.Hq + a.r.Hk);
   const auto walk = [&](const View& in, const OutView& out, const void* w, int from, int to) {
     if (from >= to) return;
-    S next;
+    Fetched<T, V, HALF, K> next;
     next.load(at.row(in, from), at.u);
     float f[K][S::W];
     load_factors<V, HALF, K>(a, w, at.u, f);
     for (int h = from; h < to; ++h) {
-      S x = next;
+      S x(next);
       if (h + 1 < to) next.load(at.row(in, h + 1), at.u);
       const float r = x.template normalize<TPR>(a, at.u);
 #pragma unroll
@@ -213,27 +229,29 @@ __global__ __launch_bounds__(kThreads) void qk_kernel(QkArgs a, int units, int h
   walk(a.r.k, a.r.ko, a.wk, max(h0 - a.r.Hq, 0), h1 - a.r.Hq);
 }
 
+// A workgroup has heads of Q alone (blockIdx.y below q_parts) or of K, and so one set of weights and sums.
 template <typename T, int V, bool HALF, int TPR, int K>
-__global__ __launch_bounds__(kThreads) void qk_bwd_kernel(QkArgs a, int units, int heads) {
+__global__ __launch_bounds__(kThreads) void qk_bwd_kernel(QkArgs a, int units, int heads, int q_parts) {
   using S = Share<T, V, HALF, K>;
   Token<T, V, HALF, TPR, K> at(a.r, units);
-  const int h0 = blockIdx.y * heads, h1 = min(h0 + heads, a.r.Hq + a.r.Hk);
+  const bool is_q = static_cast<int>(blockIdx.y) < q_parts;
+  const int h0 = (static_cast<int>(blockIdx.y) - (is_q ? 0 : q_parts)) * heads, h1 = min(h0 + heads, is_q ? a.r.Hq : a.r.Hk);
+  const View in = is_q ? a.xq : a.xk, grad = is_q ? a.r.q : a.r.k;
+  const OutView out = is_q ? a.r.qo : a.r.ko;
   const float inv = 1.0f / static_cast<float>(a.r.d);
-  float fq[K][S::W], fk[K][S::W], sq[K][S::W], sk[K][S::W];
-  load_factors<V, HALF, K>(a, a.wq, at.u, fq);
-  load_factors<V, HALF, K>(a, a.wk, at.u, fk);
+  float f[K][S::W], sum[K][S::W];
+  load_factors<V, HALF, K>(a, is_q ? a.wq : a.wk, at.u, f);
 #pragma unroll
   for (int k = 0; k < K; ++k)
 #pragma unroll
-    for (int e = 0; e < S::W; ++e) sq[k][e] = sk[k][e] = 0.0f;
-  const auto walk = [&](const View& in, const View& grad, const OutView& out, const float (*f)[S::W], float (*sum)[S::W], int from, int to) {
-    if (from >= to) return;
-    S nx, ng;
-    nx.load(at.row(in, from), at.u);
-    ng.load(at.row(grad, from), at.u);
-    for (int h = from; h < to; ++h) {
-      S x = nx, g = ng;
-      if (h + 1 < to) {
+    for (int e = 0; e < S::W; ++e) sum[k][e] = 0.0f;
+  const auto walk = [&] {
+    Fetched<T, V, HALF, K> nx, ng;
+    nx.load(at.row(in, h0), at.u);
+    ng.load(at.row(grad, h0), at.u);
+    for (int h = h0; h < h1; ++h) {
+      S x(nx), g(ng);
+      if (h + 1 < h1) {
         nx.load(at.row(in, h + 1), at.u);
         ng.load(at.row(grad, h + 1), at.u);
       }
@@ -265,40 +283,32 @@ __global__ __launch_bounds__(kThreads) void qk_bwd_kernel(QkArgs a, int units, i
   const uint64_t tokens = static_cast<uint64_t>(a.r.B) * a.r.N;
   for (uint64_t token = blockIdx.x * (kThreads / TPR) + threadIdx.x / TPR; token < tokens; token += gridDim.x * (kThreads / TPR)) {
     at.move_to(a.r, static_cast<uint32_t>(token));
-    walk(a.xq, a.r.q, a.r.qo, fq, sq, h0, min(h1, a.r.Hq));
-    walk(a.xk, a.r.k, a.r.ko, fk, sk, max(h0 - a.r.Hq, 0), h1 - a.r.Hq);
+    walk();
   }
   if (!a.dwq && !a.dwk) return;
   // the rows that a wave holds, then the waves
-  __shared__ float cols[kThreads / 64][2][kQkMaxD];
+  __shared__ float cols[kThreads / 64][kQkMaxD];
   const int wave = threadIdx.x / 64;
 #pragma unroll
   for (int k = 0; k < K; ++k)
 #pragma unroll
     for (int e = 0; e < S::W; ++e) {
 #pragma unroll
-      for (int o = TPR; o < 64; o <<= 1) {
-        sq[k][e] += __shfl_xor(sq[k][e], o, 64);
-        sk[k][e] += __shfl_xor(sk[k][e], o, 64);
-      }
-      if (threadIdx.x % 64 < TPR && S::holds(at.u[k], e)) {
-        const int ch = e < V ? at.u[k].i + e : at.u[k].j + (e - V);
-        cols[wave][0][ch] = sq[k][e];
-        cols[wave][1][ch] = sk[k][e];
-      }
+      for (int o = TPR; o < 64; o <<= 1) sum[k][e] += __shfl_xor(sum[k][e], o, 64);
+      if (threadIdx.x % 64 < TPR && S::holds(at.u[k], e)) cols[wave][e < V ? at.u[k].i + e : at.u[k].j + (e - V)] = sum[k][e];
     }
   __syncthreads();
   float* part = a.ws + (static_cast<int64_t>(blockIdx.y) * gridDim.x + blockIdx.x) * 2 * a.r.d;
-  for (int i = threadIdx.x; i < 2 * a.r.d; i += kThreads) {
-    const int which = i >= a.r.d, ch = i - which * a.r.d;
-    float t = cols[0][which][ch];
+  for (int i = threadIdx.x; i < a.r.d; i += kThreads) {
+    float t = cols[0][i];
 #pragma unroll
-    for (int w = 1; w < kThreads / 64; ++w) t += cols[w][which][ch];
-    part[i] = t;
+    for (int w = 1; w < kThreads / 64; ++w) t += cols[w][i];
+    part[i] = is_q ? t : 0.0f;
+    part[a.r.d + i] = is_q ? 0.0f : t;
   }
 }
 
-constexpr int kMaxParts = 1024;  // workgroups of the backward pass: four a CU
+constexpr int kWide = 512, kMaxParts = 3 * kWide;  // workgroups of the backward pass: along the tokens, and in all at most
 
 // Units of a block for chunks of V.
 int units_of(const RopeArgs& r, int V) {
@@ -344,8 +354,9 @@ hipError_t launch_qk(const QkArgs& a, hipStream_t stream) {
   return with_shape(a.r, [&]<typename T, int V, bool HALF, int TPR, int K>(int units) {
     const int all = a.r.Hq + a.r.Hk;
     const int64_t tokens = static_cast<int64_t>(a.r.B) * a.r.N, blocks = (tokens + kThreads / TPR - 1) / (kThreads / TPR);
-    // as many heads a thread as leave the card 2^20 threads
-    int64_t heads = tokens * TPR * all >> 20;
+    // A thread keeps its cosines and sines for as many heads as leave the card 2^18 threads, 16 waves a CU (24 heads of 6,333
+    // tokens: 22 us, with 2^19 and 2^20 25 and 34).
+    int64_t heads = tokens * TPR * all >> 18;
     heads = heads < 1 ? 1 : heads > all ? all : heads;
     qk_kernel<T, V, HALF, TPR, K><<<dim3(static_cast<unsigned>(blocks), static_cast<unsigned>((all + heads - 1) / heads)), kThreads, 0, stream>>>(
         a, units, static_cast<int>(heads));
@@ -358,13 +369,12 @@ hipError_t launch_qk_bwd(const QkArgs& a, hipStream_t stream) {
   const hipError_t e = with_shape(a.r, [&]<typename T, int V, bool HALF, int TPR, int K>(int units) {
     const int64_t all = a.r.Hq + a.r.Hk, tokens = static_cast<int64_t>(a.r.B) * a.r.N;
     int64_t x = (tokens + kThreads / TPR - 1) / (kThreads / TPR);
-    x = x < kMaxParts ? x : kMaxParts;
-    int64_t y = kMaxParts / x;
-    y = y < all ? y : all;
-    const int64_t heads = (all + y - 1) / y;
-    y = (all + heads - 1) / heads;
-    parts = x * y;
-    qk_bwd_kernel<T, V, HALF, TPR, K><<<dim3(static_cast<unsigned>(x), static_cast<unsigned>(y)), kThreads, 0, stream>>>(a, units, static_cast<int>(heads));
+    x = x < kWide ? x : kWide;
+    const int64_t most = kWide / x > 2 ? kWide / x : 2, heads = (all + most - 1) / most;
+    const int64_t q_parts = (a.r.Hq + heads - 1) / heads, y = q_parts + (a.r.Hk + heads - 1) / heads;
+    parts = x * y;  // at most 3 kWide
+    qk_bwd_kernel<T, V, HALF, TPR, K><<<dim3(static_cast<unsigned>(x), static_cast<unsigned>(y)), kThreads, 0, stream>>>(
+        a, units, static_cast<int>(heads), static_cast<int>(q_parts));
     return hipGetLastError();
   });
   if (e != hipSuccess || (!a.dwq && !a.dwk)) return e;
