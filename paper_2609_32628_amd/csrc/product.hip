@@ -398,6 +398,102 @@ __global__ __launch_bounds__(256) void product_join_kernel(ProductArgs a, int sp
   finish8<T, GLU>(a.f, RowPlace<T, GLU>(a.f, m), v, u, f8, f8);
 }
 
+// ---- few tokens ------------------------------------------------------------------------
+// Up to 16 tokens: the weights are read once, which bounds it. A workgroup has 16 features (of a gated block both halves) and
+// all tokens; its eight waves take every eighth 64 elements of K each, straight from memory into the operands of the 16x16x32
+// products, two of them on their way at a time, and their sums are added up in order in LDS.
+constexpr int kFew = 16, kFewWaves = 8, kAhead = 2;
+
+template <typename T>
+__device__ inline f32x4 mma16(const s16x8& a, const s16x8& b, const f32x4& c) {
+  if constexpr (__is_same(T, bf16_t)) {
+    return __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, a), __builtin_bit_cast(bf16x8, b), c, 0, 0, 0);
+  } else {
+    return __builtin_amdgcn_mfma_f32_16x16x32_f16(__builtin_bit_cast(f16x8, a), __builtin_bit_cast(f16x8, b), c, 0, 0, 0);
+  }
+}
+
+// Eight elements of a row from p on, of which `left` are the row's; zeros behind them.
+__device__ inline s16x8 load_row8(const uint16_t* p, int left) {
+  s16x8 v = {};
+  if (left >= 8) {
+    v = *reinterpret_cast<const s16x8*>(p);
+  } else {
+#pragma unroll
+    for (int i = 0; i < 8; ++i)
+      if (i < left) v[i] = static_cast<short>(p[i]);
+  }
+  return v;
+}
+
+template <typename T, bool GLU>
+__global__ __launch_bounds__(64 * kFewWaves, 4) void product_few_kernel(ProductArgs a) {
+  constexpr int P = GLU ? 2 : 1;
+  __shared__ __attribute__((aligned(16))) float sums[kFewWaves][kFew][16 * P + 4];
+  const int lane = threadIdx.x % 64, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64), r = lane % 16, g = lane / 16;
+  const int f0 = blockIdx.x * 16;
+  const uint16_t* w[P];
+#pragma unroll
+  for (int p = 0; p < P; ++p)
+    w[p] = static_cast<const uint16_t*>(a.w.p) + row_at(a.w, min(f0 + r, a.f.F - 1) + static_cast<int64_t>(p) * a.f.F) + 8 * g;
+  const bool live = r < a.M;
+  const uint16_t* t = static_cast<const uint16_t*>(a.t.p) + row_at(a.t, live ? r : 0) + 8 * g;
+  f32x4 acc[P] = {};
+  const int blocks = (a.K + 63) / 64, whole = a.K / 64;
+  const auto at = [&](int k) {  // of element k, the first of 64 in a row of t
+    const int h = k / a.t.C;
+    return h * a.t.sh + (k - h * a.t.C);
+  };
+  const auto add = [&](const s16x8 (&fw)[P][2], const s16x8 (&ft)[2]) {
+#pragma unroll
+    for (int c = 0; c < 2; ++c)
+#pragma unroll
+      for (int p = 0; p < P; ++p) acc[p] = mma16<T>(fw[p][c], ft[c], acc[p]);
+  };
+  int b = wave;
+  for (; b + (kAhead - 1) * kFewWaves < whole; b += kAhead * kFewWaves) {
+    s16x8 fw[kAhead][P][2], ft[kAhead][2] = {};
+#pragma unroll
+    for (int u = 0; u < kAhead; ++u) {
+      const int k = (b + u * kFewWaves) * 64;
+      const int64_t x = at(k);
+#pragma unroll
+      for (int c = 0; c < 2; ++c) {
+#pragma unroll
+        for (int p = 0; p < P; ++p) fw[u][p][c] = *reinterpret_cast<const s16x8*>(w[p] + k + 32 * c);
+        if (live) ft[u][c] = *reinterpret_cast<const s16x8*>(t + x + 32 * c);
+      }
+    }
+#pragma unroll
+    for (int u = 0; u < kAhead; ++u) add(fw[u], ft[u]);
+  }
+  for (; b < blocks; b += kFewWaves) {
+    s16x8 fw[P][2], ft[2];
+    const int k = b * 64, left = a.K - k - 8 * g;
+    const int64_t x = at(k);
+#pragma unroll
+    for (int c = 0; c < 2; ++c) {
+#pragma unroll
+      for (int p = 0; p < P; ++p) fw[p][c] = load_row8(w[p] + k + 32 * c, left - 32 * c);
+      ft[c] = load_row8(t + x + 32 * c, live ? left - 32 * c : 0);
+    }
+    add(fw, ft);
+  }
+  // lane: token r, features 4 g + {0..3}
+#pragma unroll
+  for (int p = 0; p < P; ++p) *reinterpret_cast<f32x4*>(&sums[wave][r][16 * p + 4 * g]) = acc[p];
+  __syncthreads();
+  const int m = threadIdx.x / 2, c = threadIdx.x % 2, f8 = f0 + 8 * c;
+  if (m >= a.M || f8 >= a.f.F) return;
+  float v[2][8] = {};
+#pragma unroll
+  for (int p = 0; p < P; ++p)
+    for (int s = 0; s < kFewWaves; ++s)
+#pragma unroll
+      for (int e = 0; e < 8; ++e) v[p][e] += sums[s][m][p * 16 + c * 8 + e];
+  finish8<T, GLU>(a.f, RowPlace<T, GLU>(a.f, m), v[0], v[1], f8, f8);
+}
+
 // How a product is cut: big tiles or small ones, and parts of K.
 struct Plan {
   bool big;
@@ -439,12 +535,27 @@ hipError_t launch_plan(const ProductArgs& a, const Plan& p, hipStream_t stream) 
 int64_t product_ws_bytes(int64_t M, int64_t N, int64_t F, int64_t K, int parts) {
   const auto of = [&](int64_t rows) {
     const Plan p = plan_of(rows, F * parts, K);
-    return p.splits > 1 ? 4 * p.splits * rows * ((F * parts + 7) / 8 * 8) : 0;
+    return rows > kFew && p.splits > 1 ? 4 * p.splits * rows * ((F * parts + 7) / 8 * 8) : 0;
   };
   return M == N ? of(M) : std::max(of(M), of(N));
 }
 
 hipError_t launch_product(const ProductArgs& a, hipStream_t stream) {
+  if (a.M <= kFew)
+    return by_dtype(a.dtype, [&](auto t) {
+      using T = decltype(t);
+      if constexpr (sizeof(T) == 4) {
+        return hipErrorInvalidValue;
+      } else {
+        const unsigned blocks = (a.f.F + 15) / 16;
+        if (a.parts == 2) {
+          product_few_kernel<T, true><<<blocks, 64 * kFewWaves, 0, stream>>>(a);
+        } else {
+          product_few_kernel<T, false><<<blocks, 64 * kFewWaves, 0, stream>>>(a);
+        }
+        return hipGetLastError();
+      }
+    });
   // A tile addresses its token rows by 32 bits from the lowest. Samples further apart than that go one by one.
   const int64_t samples = a.M / a.t.N;
   if (samples > 1 && (std::min<int64_t>(samples, 256 / a.t.N + 2) * a.t.sb + a.t.N * a.t.sn + (1 << 16)) >> 31) {
