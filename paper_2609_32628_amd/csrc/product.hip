@@ -88,6 +88,15 @@ __device__ inline void copy_4k_if(const i32x4& base, const uint32_t* v, uint32_t
       : "memory", "m0");
 }
 
+template <typename T>
+__device__ inline f32x4 mma16(const s16x8& a, const s16x8& b, const f32x4& c) {
+  if constexpr (__is_same(T, bf16_t)) {
+    return __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, a), __builtin_bit_cast(bf16x8, b), c, 0, 0, 0);
+  } else {
+    return __builtin_amdgcn_mfma_f32_16x16x32_f16(__builtin_bit_cast(f16x8, a), __builtin_bit_cast(f16x8, b), c, 0, 0, 0);
+  }
+}
+
 __device__ inline void in_order() { asm volatile("" ::: "memory"); }
 
 
@@ -96,8 +105,8 @@ template <int MODE_, bool END, int TW_, int TT_, int WW_, int WT_>
 struct Shape {
   static constexpr int MODE = MODE_, TW = TW_, TT = TT_, WW = WW_, WT = WT_;
   static constexpr bool kEnd = END;
-  static constexpr int kWaves = WW * WT, kW = TW / WW / 32, kT = TT / WT / 32;   // 32x32 blocks of a wave
-  static constexpr int kBlocks = MODE == kGated ? kW / 2 : kW;                   // blocks of features
+  static constexpr int kWaves = WW * WT, kW = TW / WW / 16, kT = TT / WT / 16;   // 16x16 blocks of a wave
+  static constexpr int kBlocks = kW / (MODE == kGated ? 4 : 2);                  // 32s of features
   static constexpr int kCopyW = TW / 8 / kWaves, kCopyT = TT / 8 / kWaves;       // 1 KB copies a wave makes of a step
   static constexpr int kSideW = TW / 8 * kBlock;                                  // LDS bytes of a step's feature rows
   static constexpr int kTile = kSideW + TT / 8 * kBlock;                         // of a step
@@ -249,41 +258,23 @@ __global__ __launch_bounds__(64 * S::kWaves, 2) void product_kernel(ProductArgs 
   Copies<S> copies(a, tiles_w, tiles_t, splits, lds0, lane, wave);
   copies.step(lds);
 
-  f32x16 acc[S::kW][S::kT];
+  f32x4 acc[S::kW][S::kT];
   const auto clear = [&] {
 #pragma unroll
     for (int i = 0; i < S::kW; ++i)
 #pragma unroll
-      for (int j = 0; j < S::kT; ++j) acc[i][j] = f32x16{};
+      for (int j = 0; j < S::kT; ++j) acc[i][j] = f32x4{};
   };
   clear();
-  // chunk 2 c + lane / 32 of a wave's rows, 32 of them a read
-  const uint32_t read = line_at(lane % 32) + lane / 32 * 16;
-  const uint32_t read_w = wave_w * (S::kW * 4 * kBlock) + read, read_t = S::kSideW + wave_t * (S::kT * 4 * kBlock) + read;
-  s16x8 frag[2][S::kW + S::kT];
-  const auto fetch = [&](uint32_t at, int c, int i) {
-    const int n = i < S::kW ? i : i - S::kW;
-    return read_b128(at + (i < S::kW ? read_w : read_t) + n / 2 * 8 * kBlock + n % 2 * 4 * kRowBytes + c * 32);
-  };
-  constexpr int kProducts = S::kW * S::kT, kReads = S::kW + S::kT;
-  static_assert(S::kCopyW == 4 && S::kCopyT == 4 && S::kW % 2 == 0 && S::kT % 2 == 0);
-  static_assert(kReads <= 2 * kProducts);
-  // The products of 16 elements of K, with the reads of the next 16's operands and a step's copies of one side (1: weights, 2:
-  // tokens) among them.
-  const auto products = [&]<int SIDE>(uint32_t from, int c, const s16x8* f, s16x8* into, int lanes) {
-    const auto product = [&]<int P>() {
-      // two reads a product: those that the next 16's first products take come first
-#pragma unroll
-      for (int q = 2 * P; q < 2 * P + 2 && q < kReads; ++q) {
-        const int i = q == 0 ? 0 : q <= S::kT ? S::kW + q - 1 : q - S::kT;
-        into[i] = fetch(from, c, i);
-      }
-      if constexpr (SIDE && P == kProducts / 2 - 1) copies.template side<SIDE == 1>(lanes);
-      acc[P / S::kT][P % S::kT] = mma<T>(f[P / S::kT], f[S::kW + P % S::kT], acc[P / S::kT][P % S::kT]);
-      __builtin_amdgcn_sched_barrier(0);
-    };
-    [&]<int... P>(std::integer_sequence<int, P...>) { (product.template operator()<P>(), ...); }(std::make_integer_sequence<int, kProducts>{});
-  };
+  // Operand n of half h of a step: chunk 4 h + lane / 16 of 16 rows.
+  const uint32_t read = line_at(lane % 16) + lane / 16 * 16;
+  const uint32_t read_w = wave_w * (S::kW * 2 * kBlock) + read, read_t = S::kSideW + wave_t * (S::kT * 2 * kBlock) + read;
+  const auto fetch = [&](uint32_t at, int n, int h) { return read_b128(at + n / 4 * 8 * kBlock + n % 4 * 2 * kRowBytes + h * 64); };
+  static_assert(S::kCopyW == 4 && S::kCopyT == 4 && S::kT == 4);
+  // A step is 2 kW operands of weights, kW of each half, one after the other with the four token operands of the half. The weights'
+  // are read kLead ahead, the tokens' while the half before is multiplied.
+  constexpr int kLead = 3, kAll = 2 * S::kW;
+  s16x8 fw[kLead + 1], ft[2][S::kT];
   const auto mask = [&](bool whole) { return __builtin_amdgcn_readfirstlane(whole ? -1 : 0); };
   bool whole = copies.whole();
   if (whole) copies.template side<true>(-1);
@@ -291,33 +282,49 @@ __global__ __launch_bounds__(64 * S::kWaves, 2) void product_kernel(ProductArgs 
   wait_copies();
   barrier();
 #pragma unroll
-  for (int i = 0; i < kReads; ++i) frag[0][i] = fetch(at, 0, i);
+  for (int j = 0; j < S::kT; ++j) ft[0][j] = fetch(at + read_t, j, 0);
+#pragma unroll
+  for (int n = 0; n < kLead; ++n) fw[n] = fetch(at + read_w, n, 0);
+  // Operand N of the step at `at`; from N = kAll - kLead on reads are of the next step, at `other`.
+  const auto operand = [&]<int N>(uint32_t from) {
+    constexpr int h = N / S::kW, next = (N + kLead) % kAll, tokens = N - (h + 1) * S::kW + kLead;
+    fw[(N + kLead) % (kLead + 1)] = fetch(from + read_w, next % S::kW, next / S::kW);
+    // the next half's token operands: two, one and one
+    if constexpr (tokens == 0) {
+      ft[1 - h][0] = fetch(from + read_t, 0, 1 - h);
+      ft[1 - h][1] = fetch(from + read_t, 1, 1 - h);
+    } else if constexpr (tokens > 0) {
+      ft[1 - h][tokens + 1] = fetch(from + read_t, tokens + 1, 1 - h);
+    }
+    if constexpr (N == kAll - kLead + 1) copies.template side<true>(mask(whole));
+    if constexpr (N == 2) copies.template side<false>(mask(whole));
+#pragma unroll
+    for (int j = 0; j < S::kT; ++j) acc[N % S::kW][j] = mma16<T>(fw[N % (kLead + 1)], ft[h][j], acc[N % S::kW][j]);
+    __builtin_amdgcn_sched_barrier(0);
+  };
 
   for (; mine.unit < mine.end; mine.unit += mine.stride) {
     const Unit u(mine.unit, tiles_w, tiles_t, splits, a.K);
     for (int s = 0; s < u.steps; ++s) {
-      products.template operator()<2>(at, 1, frag[0], frag[1], mask(whole));
-      products.template operator()<0>(at, 2, frag[1], frag[0], 0);
+      [&]<int... N>(std::integer_sequence<int, N...>) { (operand.template operator()<N>(at), ...); }(std::make_integer_sequence<int, S::kW>{});
       if (S::kEnd && copies.more() && !whole) copies.copy_end(lds);
       copies.next();
       whole = copies.whole();
-      products.template operator()<0>(at, 3, frag[0], frag[1], 0);
+      [&]<int... N>(std::integer_sequence<int, N...>) { (operand.template operator()<S::kW + N>(at), ...); }(std::make_integer_sequence<int, S::kW - kLead>{});
       // the next step has arrived, and every wave's reads of this one have been answered: its buffer takes the one after
       wait_copies();
       barrier();
       at = lds0 + (at == lds0 ? S::kTile : 0);
-      products.template operator()<1>(at, 0, frag[1], frag[0], mask(whole));
+      [&]<int... N>(std::integer_sequence<int, N...>) { (operand.template operator()<kAll - kLead + N>(at), ...); }(std::make_integer_sequence<int, kLead>{});
     }
 
     // The epilogue, 16 tokens and 32 features at a time: the sums go through the wave's 2 KB of LDS, so that one piece of
     // code with 8 features of a token a lane serves all blocks (unrolled over the blocks' registers it was 170 KB of
     // instructions, whose fetches took 18 us a tile).
-    const int64_t m0 = static_cast<int64_t>(u.tile_t) * TT + wave_t * S::kT * 32;
+    const int64_t m0 = static_cast<int64_t>(u.tile_t) * TT + wave_t * S::kT * 16;
     const int f0 = (u.tile_w * WW + wave_w) * (32 * S::kBlocks), chunk = lane % 4;
-    const auto put = [&](const f32x16& x) {
-#pragma unroll
-      for (int q = 0; q < 4; ++q)
-        *reinterpret_cast<f32x4*>(stage + lane % 16 * 128 + (((2 * q + lane / 32) ^ (lane % 8)) << 4)) = f32x4{x[4 * q], x[4 * q + 1], x[4 * q + 2], x[4 * q + 3]};
+    const auto put = [&](const f32x4& x, int half) {  // 16 features
+      *reinterpret_cast<f32x4*>(stage + lane % 16 * 128 + (((4 * half + lane / 16) ^ (lane % 8)) << 4)) = x;
     };
     const auto take = [&](float* v) {
       const int row = lane / 4;
@@ -329,17 +336,19 @@ __global__ __launch_bounds__(64 * S::kWaves, 2) void product_kernel(ProductArgs 
       }
     };
 #pragma unroll 1
-    for (int t16 = 0; t16 < 2 * S::kT; ++t16) {
+    for (int t16 = 0; t16 < S::kT; ++t16) {
       const int64_t m = m0 + t16 * 16 + lane / 4;
       const bool live = m < a.M;
       const RowPlace<T, MODE == kGated> row(a.f, live ? m : a.M - 1);
-      const bool writes = lane % 32 / 16 == t16 % 2;
 #pragma unroll 1
       for (int i = 0; i < S::kBlocks; ++i) {
         const auto put_block = [&]<int SECOND>() {
-          if (!writes) return;
           const auto one = [&]<int B>() {
-            if (i + t16 / 2 * S::kBlocks == B) put(acc[B % S::kBlocks + SECOND * S::kBlocks][B / S::kBlocks]);
+            constexpr int w = 2 * (B % S::kBlocks) + SECOND * (S::kW / 2);
+            if (i + t16 * S::kBlocks == B) {
+              put(acc[w][B / S::kBlocks], 0);
+              put(acc[w + 1][B / S::kBlocks], 1);
+            }
           };
           [&]<int... B>(std::integer_sequence<int, B...>) { (one.template operator()<B>(), ...); }(std::make_integer_sequence<int, S::kBlocks * S::kT>{});
         };
@@ -403,15 +412,6 @@ __global__ __launch_bounds__(256) void product_join_kernel(ProductArgs a, int sp
 // all tokens; its eight waves take every eighth 64 elements of K each, straight from memory into the operands of the 16x16x32
 // products, two of them on their way at a time, and their sums are added up in order in LDS.
 constexpr int kFew = 16, kFewWaves = 8, kAhead = 2;
-
-template <typename T>
-__device__ inline f32x4 mma16(const s16x8& a, const s16x8& b, const f32x4& c) {
-  if constexpr (__is_same(T, bf16_t)) {
-    return __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, a), __builtin_bit_cast(bf16x8, b), c, 0, 0, 0);
-  } else {
-    return __builtin_amdgcn_mfma_f32_16x16x32_f16(__builtin_bit_cast(f16x8, a), __builtin_bit_cast(f16x8, b), c, 0, 0, 0);
-  }
-}
 
 // Eight elements of a row from p on, of which `left` are the row's; zeros behind them.
 __device__ inline s16x8 load_row8(const uint16_t* p, int left) {
