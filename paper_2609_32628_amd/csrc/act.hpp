@@ -122,20 +122,57 @@ struct RowPlace {
   }
 };
 
-// Features [f8, f8 + 8) of a row from their sums v (gated block: v and u); they lie in 32 features from fb on, a number that
-// is the same for the whole wave, or fb = f8.
+// Eight elements at p, of which n are the row's, as they lie in memory.
+template <typename T>
+__device__ inline uint4 raw8(const T* p, int n) {
+  uint4 v = make_uint4(0, 0, 0, 0);
+  if (n >= 8) {
+    __builtin_memcpy(&v, p, 16);
+  } else {
+    const uint16_t* e = reinterpret_cast<const uint16_t*>(p);
+    uint32_t w[4] = {};
+#pragma unroll
+    for (int i = 0; i < 8; ++i)
+      if (i < n) w[i / 2] |= static_cast<uint32_t>(e[i]) << (16 * (i % 2));
+    v = make_uint4(w[0], w[1], w[2], w[3]);
+  }
+  return v;
+}
+template <typename T>
+__device__ inline float element(const uint4& v, int i) {
+  return static_cast<float>(__builtin_bit_cast(Chunk<T>, v).v[i]);
+}
+
+// What the epilogue reads for features [f8, f8 + 8) of a row, asked for ahead. They lie in 32 features from fb on, a number
+// that is the same for the whole wave, or fb = f8.
 template <typename T, bool GLU>
-__device__ inline void finish8(const Finish& e, const RowPlace<T, GLU>& row, float* v, float* u, int f8, int fb) {
+struct Beside {
+  uint4 bias, bias_u, gate, r;
+  int64_t y;  // element offset of the outputs in the row
+  Beside() = default;
+  __device__ Beside(const Finish& e, const RowPlace<T, GLU>& row, int f8, int fb) {
+    const int left = e.F - f8;
+    // features are blocks of Cy; 32 of them lie in one where blocks are whole 32s
+    const int h = e.Hy == 1 ? 0 : e.Cy % 32 == 0 ? fb / e.Cy : f8 / e.Cy, c = f8 - h * e.Cy;
+    y = h * e.y.sh + c;
+    if (e.bias) {
+      bias = raw8(static_cast<const T*>(e.bias) + f8, left);
+      if constexpr (GLU) bias_u = raw8(static_cast<const T*>(e.bias) + e.F + f8, left);
+    }
+    if (!GLU && e.gate) gate = raw8(row.gate + f8, left);
+    if (!GLU && e.r.p) r = raw8(row.r + h * e.r.sh + c, left);
+  }
+};
+
+// Features [f8, f8 + 8) of a row from their sums v (gated block: v and u).
+template <typename T, bool GLU>
+__device__ inline void finish8(const Finish& e, const RowPlace<T, GLU>& row, const Beside<T, GLU>& x, float* v, float* u, int f8) {
   const int left = e.F - f8;
-  float x[8];
   if (e.bias) {
-    load8<T>(e.bias, f8, left, x);
 #pragma unroll
-    for (int i = 0; i < 8; ++i) v[i] += x[i];
-    if constexpr (GLU) {
-      load8<T>(e.bias, static_cast<int64_t>(e.F) + f8, left, x);
-#pragma unroll
-      for (int i = 0; i < 8; ++i) u[i] += x[i];
+    for (int i = 0; i < 8; ++i) {
+      v[i] += element<T>(x.bias, i);
+      if constexpr (GLU) u[i] += element<T>(x.bias_u, i);
     }
   }
   if (e.z) {
@@ -146,19 +183,17 @@ __device__ inline void finish8(const Finish& e, const RowPlace<T, GLU>& row, flo
   if constexpr (GLU) {
 #pragma unroll
     for (int i = 0; i < 8; ++i) v[i] *= u[i];
-  } else if (e.gate) {
-    load8<T>(row.gate, f8, left, x);
+  } else {
+    if (e.gate) {
 #pragma unroll
-    for (int i = 0; i < 8; ++i) v[i] *= x[i];
-  }
-  // features are blocks of Cy; 32 of them lie in one where blocks are whole 32s
-  const int h = e.Hy == 1 ? 0 : e.Cy % 32 == 0 ? fb / e.Cy : f8 / e.Cy, c = f8 - h * e.Cy;
-  if (!GLU && e.r.p) {
-    load8<T>(row.r, h * e.r.sh + c, left, x);
+      for (int i = 0; i < 8; ++i) v[i] *= element<T>(x.gate, i);
+    }
+    if (e.r.p) {
 #pragma unroll
-    for (int i = 0; i < 8; ++i) v[i] += x[i];
+      for (int i = 0; i < 8; ++i) v[i] += element<T>(x.r, i);
+    }
   }
-  store8<T>(row.y, h * e.y.sh + c, left, v);
+  store8<T>(row.y, x.y, left, v);
 }
 
 }  // namespace da2

@@ -340,12 +340,19 @@ __global__ __launch_bounds__(64 * S::kWaves, 2) void product_kernel(ProductArgs 
       const int64_t m = m0 + t16 * 16 + lane / 4;
       const bool live = m < a.M;
       const RowPlace<T, MODE == kGated> row(a.f, live ? m : a.M - 1);
-#pragma unroll 1
+      constexpr bool GLU = MODE == kGated;
+      constexpr int kPair = S::kBlocks < 2 ? 1 : 2;  // blocks whose epilogue reads are asked for at once
+      Beside<T, GLU> beside[kPair];
+#pragma unroll
       for (int i = 0; i < S::kBlocks; ++i) {
+        if (MODE != kPartial && i % kPair == 0)
+#pragma unroll
+          for (int k = 0; k < kPair; ++k)
+            beside[k] = Beside<T, GLU>(a.f, row, min(f0 + (i + k) * 32 + 8 * chunk, a.f.F - 1), min(f0 + (i + k) * 32, a.f.F - 1));
         const auto put_block = [&]<int SECOND>() {
           const auto one = [&]<int B>() {
             constexpr int w = 2 * (B % S::kBlocks) + SECOND * (S::kW / 2);
-            if (i + t16 * S::kBlocks == B) {
+            if (B % S::kBlocks == i && B / S::kBlocks == t16) {
               put(acc[w][B / S::kBlocks], 0);
               put(acc[w + 1][B / S::kBlocks], 1);
             }
@@ -364,7 +371,7 @@ __global__ __launch_bounds__(64 * S::kWaves, 2) void product_kernel(ProductArgs 
           take(w);
           in_order();
         }
-        const int fb = f0 + i * 32, f8 = fb + 8 * chunk;
+        const int f8 = f0 + i * 32 + 8 * chunk;
         if constexpr (MODE == kPartial) {
           if (live && f8 < R) {
             float* to = a.ws + (static_cast<int64_t>(u.split) * a.M + m) * ((R + 7) / 8 * 8) + f8;
@@ -372,7 +379,7 @@ __global__ __launch_bounds__(64 * S::kWaves, 2) void product_kernel(ProductArgs 
             store_vec(to + 4, v + 4);
           }
         } else if (live && f8 < a.f.F) {
-          finish8<T, MODE == kGated>(a.f, row, v, w, f8, fb);
+          finish8<T, GLU>(a.f, row, beside[i % kPair], v, w, f8);
         }
       }
     }
@@ -404,7 +411,8 @@ __global__ __launch_bounds__(256) void product_join_kernel(ProductArgs a, int sp
       for (int i = 0; i < 8; ++i) u[i] += x[i];
     }
   }
-  finish8<T, GLU>(a.f, RowPlace<T, GLU>(a.f, m), v, u, f8, f8);
+  const RowPlace<T, GLU> row(a.f, m);
+  finish8<T, GLU>(a.f, row, Beside<T, GLU>(a.f, row, f8, f8), v, u, f8);
 }
 
 // ---- few tokens ------------------------------------------------------------------------
@@ -491,22 +499,40 @@ __global__ __launch_bounds__(64 * kFewWaves, 4) void product_few_kernel(ProductA
     for (int s = 0; s < kFewWaves; ++s)
 #pragma unroll
       for (int e = 0; e < 8; ++e) v[p][e] += sums[s][m][p * 16 + c * 8 + e];
-  finish8<T, GLU>(a.f, RowPlace<T, GLU>(a.f, m), v[0], v[1], f8, f8);
+  const RowPlace<T, GLU> row(a.f, m);
+  finish8<T, GLU>(a.f, row, Beside<T, GLU>(a.f, row, f8, f8), v[0], v[1], f8);
 }
 
-// How a product is cut: big tiles or small ones, and parts of K.
+// How a product is cut: tiles of 256x256 or 128x128, and parts of K that are joined. The least by these times in us, fitted to
+// 16 products of 100 to 8,192 rows: a round of workgroups takes 9 and 1.4 a step (big tiles, one workgroup a CU) or 8 and 0.95 (small,
+// two a CU; 0.7 with one); a join takes 3 and the partial sums' bytes, written and read, at 4 TB/s. (5,120 x 1,280 x 8,192: 110
+// with big tiles and two parts, 165 whole, 119 and 130 with small ones; 2,331 x 1,280 x 1,024: 20 with small tiles, 26 in two
+// parts, 34 with big ones.)
 struct Plan {
   bool big;
   int splits;
 };
 Plan plan_of(int64_t M, int64_t R, int64_t K) {
   const int64_t big = ((M + 255) / 256) * ((R + 255) / 256), small = ((M + 127) / 128) * ((R + 127) / 128);
-  const int64_t steps = (K + 63) / 64;
-  if (big >= 256) return {true, 1};
-  int64_t splits = 1;
-  while (small * splits * 2 <= 512 && steps / (splits * 2) >= 8) splits *= 2;
-  const int64_t per = (steps + splits - 1) / splits;
-  return {false, static_cast<int>((steps + per - 1) / per)};
+  const int64_t steps = (K + kStep - 1) / kStep;
+  Plan best{false, 1};
+  double least = 1e300;
+  for (int64_t splits = 1; splits <= 8 && (splits == 1 || steps >= 4 * splits); splits *= 2) {
+    const int64_t per = (steps + splits - 1) / splits, parts = (steps + per - 1) / per;
+    const double join = parts > 1 ? 3.0 + 8e-6 / 4 * static_cast<double>(parts) * static_cast<double>(M) * static_cast<double>(R) : 0.0;
+    const double b = static_cast<double>((big * parts + 255) / 256) * (1.4 * per + 9) + join;
+    const int64_t rest = small * parts % 512;
+    const double s = static_cast<double>(small * parts / 512) * (0.95 * per + 8) + (rest > 256 ? 0.95 * per + 8 : rest ? 0.7 * per + 8 : 0.0) + join;
+    if (b < least) {
+      least = b;
+      best = {true, static_cast<int>(parts)};
+    }
+    if (s < least) {
+      least = s;
+      best = {false, static_cast<int>(parts)};
+    }
+  }
+  return best;
 }
 
 template <typename T, typename S>
