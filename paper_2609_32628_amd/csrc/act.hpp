@@ -112,6 +112,7 @@ struct RowPlace {
   T* y;
   const T *r, *gate;
   float* z;
+  RowPlace() = default;
   __device__ RowPlace(const Finish& e, int64_t m) {
     const int b = static_cast<int>(static_cast<uint32_t>(m) / static_cast<uint32_t>(e.N));
     const int n = static_cast<int>(m - static_cast<int64_t>(b) * e.N);

@@ -130,7 +130,7 @@ bool gate_ok(const void* gate, int64_t stride, const Proj& e) {
 }
 
 Side rows_side(const void* p, const da2_tensor* t, const Ext& e) {
-  return Side{p, e.B > 1 ? t->stride_b : 0, e.H > 1 ? t->stride_h : 0, e.N > 1 ? t->stride_n : 0, (int)e.N, (int)e.C};
+  return Side{p, e.B > 1 ? t->stride_b : 0, e.H > 1 ? t->stride_h : 0, e.N > 1 ? t->stride_n : 0, (int)e.N, (int)e.C, (int)e.B};
 }
 
 Finish plain_finish(OutView y, int64_t H, int64_t C, int64_t N) {
@@ -199,7 +199,7 @@ int32_t forward(const da2_proj* p, int parts, const void* X, const da2_tensor* x
   if ((st = check_device())) return st;
   ProductArgs a{};
   a.t = rows_side(X, x, e.x);
-  a.w = Side{W, e.F * w_stride, 0, w_stride, (int)e.F, (int)e.K};
+  a.w = Side{W, e.F * w_stride, 0, w_stride, (int)e.F, (int)e.K, parts};
   a.f = plain_finish(out_view(Y, y), p->Hy, p->Cy, p->N);
   a.f.bias = bias;
   a.f.gate = gate;
@@ -276,18 +276,18 @@ int32_t backward(const da2_proj* p, int parts, const void* dY, const da2_tensor*
   a.parts = 1;
   a.dtype = p->dtype;
   if (err == hipSuccess && dX) {
-    err = launch_transpose(TransposeArgs{Side{W, e.F * w_stride, 0, w_stride, (int)e.F, (int)e.K}, parts, (int)e.K, p->dtype, at + s.wt, e.F64, wide}, stream);
-    a.t = direct ? rows_side(dY, dy, e.y) : Side{z.dz, 0, 0, wide, (int)e.M, (int)wide};
+    err = launch_transpose(TransposeArgs{Side{W, e.F * w_stride, 0, w_stride, (int)e.F, (int)e.K, parts}, parts, (int)e.K, p->dtype, at + s.wt, e.F64, wide}, stream);
+    a.t = direct ? rows_side(dY, dy, e.y) : Side{z.dz, 0, 0, wide, (int)e.M, (int)wide, 1};
     a.K = direct ? (int)e.F : (int)wide;
-    a.w = Side{at + s.wt, 0, 0, wide, (int)e.K, a.K};
+    a.w = Side{at + s.wt, 0, 0, wide, (int)e.K, a.K, 1};
     a.f = plain_finish(out_view(dX, dx), p->Hx, p->Cx, p->N);
     a.M = e.M;
     if (err == hipSuccess) err = launch_product(a, stream);
   }
   if (err == hipSuccess && dW) {
     err = launch_transpose(TransposeArgs{rows_side(X, x, e.x), p->B, (int)e.K, p->dtype, at + s.xt, e.Np, e.ldt}, stream);
-    a.t = Side{at + s.dzt, e.F64 * e.ldt, 0, e.ldt, (int)e.F, (int)e.ldt};
-    a.w = Side{at + s.xt, 0, 0, e.ldt, (int)e.K, (int)e.ldt};
+    a.t = Side{at + s.dzt, e.F64 * e.ldt, 0, e.ldt, (int)e.F, (int)e.ldt, parts};
+    a.w = Side{at + s.xt, 0, 0, e.ldt, (int)e.K, (int)e.ldt, 1};
     a.K = (int)e.ldt;
     a.f = plain_finish(OutView{dW, e.F * dw_stride, 0, dw_stride}, 1, e.K, e.F);
     a.M = e.R;

@@ -12,7 +12,7 @@ namespace da2 {
 struct Side {
   const void* p;
   int64_t sb, sh, sn;
-  int N, C;
+  int N, C, B;  // B: samples (or parts)
 };
 
 // What is done with the sums z of a row of features before they are stored.

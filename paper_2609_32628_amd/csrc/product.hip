@@ -34,11 +34,13 @@ __device__ inline int line_at(int r) { return r % 16 / 2 * kBlock + (r / 16 * 2 
 
 // Element offset of row r.
 __device__ inline int64_t row_at(const Side& s, int64_t r) {
+  if (s.B == 1) return r * s.sn;
   const uint32_t b = static_cast<uint32_t>(r) / static_cast<uint32_t>(s.N);
   return b * s.sb + (static_cast<uint32_t>(r) - b * static_cast<uint32_t>(s.N)) * s.sn;
 }
 // The least element offset of rows [r, last].
 __device__ inline int64_t first_at(const Side& s, int64_t r, int64_t last) {
+  if (s.B == 1) return r * s.sn;
   const uint32_t b = static_cast<uint32_t>(r) / static_cast<uint32_t>(s.N);
   const int64_t here = row_at(s, r);
   return static_cast<uint32_t>(last) / static_cast<uint32_t>(s.N) > b ? min(here, (b + 1) * s.sb) : here;
@@ -335,52 +337,60 @@ __global__ __launch_bounds__(64 * S::kWaves, 2) void product_kernel(ProductArgs 
         for (int e = 0; e < 4; ++e) v[4 * h + e] = x[e];
       }
     };
+    // Part t16, i: tokens t16 * 16 + {0..15}, features i * 32 + {0..31}. What the next part's epilogue reads is asked for before
+    // this part is worked on.
+    constexpr bool GLU = MODE == kGated;
+    const auto row_of_part = [&](int t16) { return min(m0 + t16 * 16 + lane / 4, a.M - 1); };
+    RowPlace<T, GLU> row{}, next_row{};
+    Beside<T, GLU> beside{}, next{};
+    const auto ask = [&](int t16, int i) {
+      if constexpr (MODE != kPartial) {
+        if (i == 0) next_row = RowPlace<T, GLU>(a.f, row_of_part(t16));
+        next = Beside<T, GLU>(a.f, next_row, min(f0 + i * 32 + 8 * chunk, a.f.F - 1), min(f0 + i * 32, a.f.F - 1));
+      }
+    };
+    ask(0, 0);
 #pragma unroll 1
-    for (int t16 = 0; t16 < S::kT; ++t16) {
-      const int64_t m = m0 + t16 * 16 + lane / 4;
-      const bool live = m < a.M;
-      const RowPlace<T, MODE == kGated> row(a.f, live ? m : a.M - 1);
-      constexpr bool GLU = MODE == kGated;
-      constexpr int kPair = S::kBlocks < 2 ? 1 : 2;  // blocks whose epilogue reads are asked for at once
-      Beside<T, GLU> beside[kPair];
-#pragma unroll
-      for (int i = 0; i < S::kBlocks; ++i) {
-        if (MODE != kPartial && i % kPair == 0)
-#pragma unroll
-          for (int k = 0; k < kPair; ++k)
-            beside[k] = Beside<T, GLU>(a.f, row, min(f0 + (i + k) * 32 + 8 * chunk, a.f.F - 1), min(f0 + (i + k) * 32, a.f.F - 1));
-        const auto put_block = [&]<int SECOND>() {
-          const auto one = [&]<int B>() {
-            constexpr int w = 2 * (B % S::kBlocks) + SECOND * (S::kW / 2);
-            if (B % S::kBlocks == i && B / S::kBlocks == t16) {
-              put(acc[w][B / S::kBlocks], 0);
-              put(acc[w + 1][B / S::kBlocks], 1);
-            }
-          };
-          [&]<int... B>(std::integer_sequence<int, B...>) { (one.template operator()<B>(), ...); }(std::make_integer_sequence<int, S::kBlocks * S::kT>{});
-        };
-        // the wave's lanes read what others wrote: LDS takes its accesses in order, and the compiler has to leave them so
-        float v[8], w[8];
-        put_block.template operator()<0>();
-        in_order();
-        take(v);
-        in_order();
-        if constexpr (MODE == kGated) {
-          put_block.template operator()<1>();
-          in_order();
-          take(w);
-          in_order();
-        }
-        const int f8 = f0 + i * 32 + 8 * chunk;
-        if constexpr (MODE == kPartial) {
-          if (live && f8 < R) {
-            float* to = a.ws + (static_cast<int64_t>(u.split) * a.M + m) * ((R + 7) / 8 * 8) + f8;
-            store_vec(to, v);
-            store_vec(to + 4, v + 4);
+    for (int t16 = 0, i = 0; t16 < S::kT;) {
+      row = next_row;
+      beside = next;
+      const int part = i + t16 * S::kBlocks, at16 = t16, f8 = f0 + i * 32 + 8 * chunk;
+      if (++i == S::kBlocks) {
+        i = 0;
+        ++t16;
+      }
+      if (t16 < S::kT) ask(t16, i);
+      const auto put_block = [&]<int SECOND>() {
+        const auto one = [&]<int B>() {
+          constexpr int w = 2 * (B % S::kBlocks) + SECOND * (S::kW / 2);
+          if (part == B) {
+            put(acc[w][B / S::kBlocks], 0);
+            put(acc[w + 1][B / S::kBlocks], 1);
           }
-        } else if (live && f8 < a.f.F) {
-          finish8<T, GLU>(a.f, row, beside[i % kPair], v, w, f8);
+        };
+        [&]<int... B>(std::integer_sequence<int, B...>) { (one.template operator()<B>(), ...); }(std::make_integer_sequence<int, S::kBlocks * S::kT>{});
+      };
+      // the wave's lanes read what others wrote: LDS takes its accesses in order, and the compiler has to leave them so
+      float v[8], w[8];
+      put_block.template operator()<0>();
+      in_order();
+      take(v);
+      in_order();
+      if constexpr (GLU) {
+        put_block.template operator()<1>();
+        in_order();
+        take(w);
+        in_order();
+      }
+      const int64_t m = m0 + at16 * 16 + lane / 4;
+      if constexpr (MODE == kPartial) {
+        if (m < a.M && f8 < R) {
+          float* to = a.ws + (static_cast<int64_t>(u.split) * a.M + m) * ((R + 7) / 8 * 8) + f8;
+          store_vec(to, v);
+          store_vec(to + 4, v + 4);
         }
+      } else if (m < a.M && f8 < a.f.F) {
+        finish8<T, GLU>(a.f, row, beside, v, w, f8);
       }
     }
     clear();
@@ -583,12 +593,13 @@ hipError_t launch_product(const ProductArgs& a, hipStream_t stream) {
       }
     });
   // A tile addresses its token rows by 32 bits from the lowest. Samples further apart than that go one by one.
-  const int64_t samples = a.M / a.t.N;
+  const int64_t samples = a.t.B;
   if (samples > 1 && (std::min<int64_t>(samples, 256 / a.t.N + 2) * a.t.sb + a.t.N * a.t.sn + (1 << 16)) >> 31) {
     for (int64_t b = 0; b < samples; ++b) {
       ProductArgs one = a;
       const auto skip = [&](const void* p, int64_t n) { return p ? static_cast<const char*>(p) + 2 * b * n : nullptr; };
       one.M = a.t.N;
+      one.t.B = 1;
       one.t.p = skip(a.t.p, a.t.sb);
       one.f.gate = skip(a.f.gate, a.f.gate_sb);
       one.f.r.p = skip(a.f.r.p, a.f.r.sb);
