@@ -158,7 +158,7 @@ def alloc(p, scope="head", device="cuda", fmt4="nvfp4", with16=False):
                    ws_draft=raw(s["ws_draft_bytes"]), ws_rank=raw(s["ws_rank_bytes"]))
 
 
-def attention(Q, K, V, buf, lam, budgets, O, stream=None, num16=0, fmt4=None, qk_norm=None, rope=None):
+def attention(Q, K, V, buf, lam, budgets, O, stream=None, num16=0, fmt4=None, qk_norm=None, rope=None, one_pass=False):
     """The four calls in order: draft map, ranking, operand preparation,
     attention. budgets = (num8, num4, den); num16/den go to the 16-bit path;
     fmt4 ("nvfp4" or "mxfp4", default: the buffers' encoding) is the encoding
@@ -167,8 +167,9 @@ def attention(Q, K, V, buf, lam, budgets, O, stream=None, num16=0, fmt4=None, qk
     numbers) or three (the problem's grid): they are rotated next. Both work in
     place, on Q and K themselves: a second call with them would do so again, and
     who needs them as they were calls da2_norm and da2_rope into tensors of
-    their own and then this without. All arguments of all calls are checked
-    before Q and K are touched."""
+    their own and then this without. one_pass: both in one call, da2_qk_norm_rope,
+    which reads and writes Q and K once and rounds once. All arguments of all
+    calls are checked before Q and K are touched."""
     p = buf.p
     fmt4 = buf.fmt4 if fmt4 is None else fmt4
     if fmt4 != buf.fmt4 or (num16 > 0 and not buf.with16):
@@ -176,14 +177,18 @@ def attention(Q, K, V, buf, lam, budgets, O, stream=None, num16=0, fmt4=None, qk
                          f"num16={num16}")
     if rope is not None and len(rope.rot_axis) not in (1, 3):
         raise ValueError(f"rope: expected 1 or 3 axes, got {len(rope.rot_axis)}")
+    if one_pass and (qk_norm is None or rope is None):
+        raise ValueError("one_pass: expected qk_norm and rope")
     if (qk_norm is not None or rope is not None) and Q.data_ptr() == K.data_ptr():
         raise ValueError("Q and K are one tensor: the norm and rotation in place would meet it twice")
     if qk_norm is not None or rope is not None:
         turn = _check_in_place(Q, K, V, buf, lam, budgets, O, num16, qk_norm, rope)
-    if qk_norm is not None:
+    if one_pass:
+        da2_qk_norm_rope(rope, Q, Q, K, K, *qk_norm, grid=None if len(rope.rot_axis) == 1 else (p.Hg, p.Wg), stream=stream)
+    elif qk_norm is not None:
         da2_norm(Q, Q, qk_norm[0], kind="rms", stream=stream)
         da2_norm(K, K, qk_norm[1], kind="rms", stream=stream)
-    if rope is not None:
+    if rope is not None and not one_pass:
         _run("da2_rope", stream, *turn)
     da2_draft_map(Q, K, buf.layout, p, lam, buf.A, buf.stats, buf.ws_draft, stream)
     da2_rank_assign(buf.A, p, num16, *budgets, buf.scope, buf.cls, buf.lists, buf.ws_rank, stream)

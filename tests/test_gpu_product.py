@@ -323,3 +323,24 @@ def test_two_calls_at_once():
     torch.cuda.synchronize()
     for c in cases:
         c.check()
+
+
+@pytest.mark.parametrize("glu", [False, True])
+def test_offsets_that_pass_32_bits(glu):
+    """Samples 4 GB apart, which no tile's 32-bit offsets span, of many tokens and of few."""
+    for N in (130, 3):
+        c = Case(2, N, 72, 40, act="silu", gate="none" if glu else "adaptive", residual=not glu, glu=glu)
+        apart = 1 << 31
+        for name in ("X", "dY"):
+            t = getattr(c, name)
+            big = torch.empty(apart + t.shape[2] * 80, dtype=t.dtype, device="cuda")
+            far = torch.as_strided(big, t.shape, (apart, 0, 80, 1))
+            far.copy_(t)
+            setattr(c, name, far)
+        c.outputs()
+        y = torch.empty(apart + N * 48, dtype=torch.bfloat16, device="cuda")
+        plain, c.Y = c.Y, torch.as_strided(y, c.Y.shape, (apart, 0, 48, 1))
+        c.run()
+        plain.copy_(c.Y)
+        c.Y = plain
+        c.check()
