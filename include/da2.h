@@ -593,7 +593,7 @@ typedef enum {
  * Tensors are bf16 or fp16 (fp32: UNSUPPORTED), all of the one dtype, and read and written in 16-byte
  * vectors: bases 16-byte aligned (bias and gate: of an element), every stride of X, Y, R, W and their gradients a multiple
  * of 8 elements, the stride_n of inputs and the row stride of W at most 2^22. Any K and F: what lies between a row's end and
- * its stride is neither used nor written.
+ * its stride is neither used nor written (a row's last 16 bytes are read whole: of the last row, too, they are the tensor's memory).
  * K and F at most 2^20; B*N at most 2^31 - 1 (backward with dW: 2^22 - 8*B), and
  * ceil(B*N / 128) ceil(K or F / 128) at most 2^24 - 8 (da2_glu: 2 F; and (F + 256) times W's row stride below 2^31). */
 typedef struct {

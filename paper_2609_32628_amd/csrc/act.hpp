@@ -79,21 +79,13 @@ __device__ inline void act8(int act, float* z) {
   });
 }
 
-// Eight elements at p (n of them are the row's) as floats, and back.
-template <typename T>
-__device__ inline void load8(const void* p, int64_t at, int n, float* x) {
-  load_part(static_cast<const T*>(p) + at, n, x);
-}
+// Stores the first n of eight values.
 template <typename T>
 __device__ inline void store8(void* p, int64_t at, int n, const float* x) {
   store_part(static_cast<T*>(p) + at, n, x);
 }
 
-// Eight floats at p, of which n are the row's.
-__device__ inline void load_eight(const float* p, int n, float* x) {
-  load_part(p, n, x);
-  load_part(p + 4, n - 4, x + 4);
-}
+// Stores the first n of eight floats.
 __device__ inline void store_eight(float* p, int n, const float* x) {
   store_part(p, n, x);
   store_part(p + 4, n - 4, x + 4);
@@ -123,21 +115,25 @@ struct RowPlace {
   }
 };
 
-// Eight elements at p, of which n are the row's, as they lie in memory.
+// Eight elements at p, of which n (at least one) are there, as they lie in memory; behind those the last one again.
 template <typename T>
 __device__ inline uint4 raw8(const T* p, int n) {
-  uint4 v = make_uint4(0, 0, 0, 0);
+  uint4 v;
   if (n >= 8) {
     __builtin_memcpy(&v, p, 16);
   } else {
     const uint16_t* e = reinterpret_cast<const uint16_t*>(p);
-    uint32_t w[4] = {};
+    uint32_t w[8];
 #pragma unroll
-    for (int i = 0; i < 8; ++i)
-      if (i < n) w[i / 2] |= static_cast<uint32_t>(e[i]) << (16 * (i % 2));
-    v = make_uint4(w[0], w[1], w[2], w[3]);
+    for (int i = 0; i < 8; ++i) w[i] = e[min(i, n - 1)];
+    v = make_uint4(w[0] | w[1] << 16, w[2] | w[3] << 16, w[4] | w[5] << 16, w[6] | w[7] << 16);
   }
   return v;
+}
+// The first n of the eight elements of a 16-byte chunk, zeros behind them.
+__device__ inline uint4 first8(const uint4& v, int n) {
+  const auto keep = [&](uint32_t w, int i) { return n >= 2 * i + 2 ? w : n == 2 * i + 1 ? w & 0xFFFFu : 0u; };
+  return make_uint4(keep(v.x, 0), keep(v.y, 1), keep(v.z, 2), keep(v.w, 3));
 }
 template <typename T>
 __device__ inline float element(const uint4& v, int i) {

@@ -203,24 +203,24 @@ struct Copies {
     if constexpr (S::kEnd) copy_4k_if(buffer_at((W ? walk_w.at : walk_t.at) - 3 * kBlock), W ? off_w : off_t, at, lanes);
     else copy_4k(buffer_at((W ? walk_w.at : walk_t.at) - 3 * kBlock), W ? off_w : off_t, at);
   }
-  // The end of K inside a step: through registers, zeros behind it.
+  // The end of K inside a step: through registers, zeros behind it. A row's last chunk lies in its stride, and is whole in memory.
   __device__ void copy_end(char* lds) {
+    constexpr int n = S::kCopyW + S::kCopyT;
+    const int rest = a.K - k - lane % 8 * 8;
+    uint4 v[n];
 #pragma unroll
-    for (int i = 0; i < S::kCopyW + S::kCopyT; ++i) {
+    for (int i = 0; i < n; ++i) {
       const bool w = i < S::kCopyW;
-      const int c = w ? i : i - S::kCopyW, rest = a.K - k - lane % 8 * 8;
+      const int c = w ? i : i - S::kCopyW;
       const char* p = (w ? walk_w.at + off_w[w ? c : 0] : walk_t.at + off_t[w ? 0 : c]) - kBlock * (3 - c);
-      uint4 v = make_uint4(0, 0, 0, 0);
-      if (rest >= 8) {
-        v = *reinterpret_cast<const uint4*>(p);
-      } else if (rest > 0) {
-        uint32_t e[4] = {};
+      v[i] = make_uint4(0, 0, 0, 0);
+      if (rest > 0) v[i] = *reinterpret_cast<const uint4*>(p);
+    }
 #pragma unroll
-        for (int j = 0; j < 8; ++j)
-          if (j < rest) e[j / 2] |= static_cast<uint32_t>(reinterpret_cast<const uint16_t*>(p)[j]) << (16 * (j % 2));
-        v = make_uint4(e[0], e[1], e[2], e[3]);
-      }
-      *reinterpret_cast<uint4*>(lds + (to - lds0) + ((w ? wave * S::kCopyW : TW / 8 + wave * S::kCopyT) + c) * kBlock + lane * 16) = v;
+    for (int i = 0; i < n; ++i) {
+      const bool w = i < S::kCopyW;
+      const int c = w ? i : i - S::kCopyW;
+      *reinterpret_cast<uint4*>(lds + (to - lds0) + ((w ? wave * S::kCopyW : TW / 8 + wave * S::kCopyT) + c) * kBlock + lane * 16) = first8(v[i], rest);
     }
   }
   __device__ void next() {
@@ -431,17 +431,11 @@ __global__ __launch_bounds__(256) void product_join_kernel(ProductArgs a, int sp
 // products, two of them on their way at a time, and their sums are added up in order in LDS.
 constexpr int kFew = 16, kFewWaves = 8, kAhead = 2;
 
-// Eight elements of a row from p on, of which `left` are the row's; zeros behind them.
+// A chunk of a row, of which `left` elements are the row's; zeros behind them.
 __device__ inline s16x8 load_row8(const uint16_t* p, int left) {
-  s16x8 v = {};
-  if (left >= 8) {
-    v = *reinterpret_cast<const s16x8*>(p);
-  } else {
-#pragma unroll
-    for (int i = 0; i < 8; ++i)
-      if (i < left) v[i] = static_cast<short>(p[i]);
-  }
-  return v;
+  uint4 v = make_uint4(0, 0, 0, 0);
+  if (left > 0) v = *reinterpret_cast<const uint4*>(p);
+  return __builtin_bit_cast(s16x8, first8(v, left));
 }
 
 template <typename T, bool GLU>

@@ -9,6 +9,11 @@ namespace da2 {
 
 namespace {
 
+__device__ inline void load_eight(const float* p, float* x) {
+  load_vec(p, x);
+  load_vec(p + 4, x + 4);
+}
+
 constexpr int kTileN = 64;  // rows and columns of a tile
 constexpr int kThreads = 256;
 constexpr int kPitch = kTileN + 8;  // elements of a tile's row in LDS: 16-byte rows, columns over all banks
@@ -44,7 +49,11 @@ __global__ __launch_bounds__(kThreads) void dz_kernel(DzArgs a, int per, int blo
   float sb[P][8] = {}, sg[8] = {}, gate[8];
 #pragma unroll
   for (int i = 0; i < 8; ++i) gate[i] = 1.0f;
-  if (!GLU && a.gate && left > 0) load8<T>(a.gate, b * a.gate_sb + f8, left, gate);
+  const auto floats = [](const uint4& v, float* x) {
+#pragma unroll
+    for (int i = 0; i < 8; ++i) x[i] = element<T>(v, i);
+  };
+  if (!GLU && a.gate && left > 0) floats(raw8(static_cast<const T*>(a.gate) + b * a.gate_sb + f8, left), gate);
   for (int t = blockIdx.y * per; t < min(static_cast<int>((blockIdx.y + 1) * per), tiles); ++t) {
     for (int h = 0; h < 2; ++h) {
       const int row = h * 32 + threadIdx.x / 8, n = t * kTileN + row;
@@ -53,10 +62,13 @@ __global__ __launch_bounds__(kThreads) void dz_kernel(DzArgs a, int per, int blo
       if (live) {
         const int64_t m = static_cast<int64_t>(b) * a.N + n;
         float dy[8], z[8], u[8];
-        load8<T>(a.dy.p, b * a.dy.sb + n * a.dy.sn + feature_at(f8, a.Hy, a.Cy, a.dy.sh), left, dy);
+        // chunks of rows are whole in memory, and what lies behind F is taken out below
+        uint4 raw;
+        __builtin_memcpy(&raw, static_cast<const T*>(a.dy.p) + b * a.dy.sb + n * a.dy.sn + feature_at(f8, a.Hy, a.Cy, a.dy.sh), 16);
+        floats(first8(raw, left), dy);
         if (a.z) {
-          load_eight(a.z + m * P * a.z_ld + f8, left, z);
-          if constexpr (GLU) load_eight(a.z + (m * P + 1) * a.z_ld + f8, left, u);
+          load_eight(a.z + m * P * a.z_ld + f8, z);
+          if constexpr (GLU) load_eight(a.z + (m * P + 1) * a.z_ld + f8, u);
           with_act(a.act, [&]<int ACT>() {
 #pragma unroll
             for (int i = 0; i < 8; ++i) {
@@ -155,18 +167,10 @@ __global__ __launch_bounds__(kThreads) void transpose_kernel(TransposeArgs a) {
   if (n0 >= end) return;
   for (int i = threadIdx.x; i < kTileN * 8; i += kThreads) {
     const int row = i / 8, k = k0 + i % 8 * 8, left = a.K - k;
-    uint16_t e[8] = {};
-    if (n0 + row < a.s.N && left > 0) {
-      const uint16_t* p = static_cast<const uint16_t*>(a.s.p) + b * a.s.sb + (n0 + row) * a.s.sn + feature_at(k, a.K > a.s.C ? 2 : 1, a.s.C, a.s.sh);
-      if (left >= 8) {
-        __builtin_memcpy(e, p, 16);
-      } else {
-#pragma unroll
-        for (int j = 0; j < 8; ++j)
-          if (j < left) e[j] = p[j];
-      }
-    }
-    __builtin_memcpy(tile + row * kPitch + i % 8 * 8, e, 16);
+    uint4 v = make_uint4(0, 0, 0, 0);
+    if (n0 + row < a.s.N && left > 0)
+      __builtin_memcpy(&v, static_cast<const uint16_t*>(a.s.p) + b * a.s.sb + (n0 + row) * a.s.sn + feature_at(k, a.K > a.s.C ? 2 : 1, a.s.C, a.s.sh), 16);
+    __builtin_memcpy(tile + row * kPitch + i % 8 * 8, &v, 16);
   }
   __syncthreads();
   store_transposed(tile, static_cast<uint16_t*>(a.out), a.ld, k0, min(kTileN, a.K - k0), b * a.Np + n0, end - n0);
