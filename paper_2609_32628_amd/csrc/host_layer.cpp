@@ -276,7 +276,7 @@ int32_t backward(const da2_proj* p, int parts, const void* dY, const da2_tensor*
   a.parts = 1;
   a.dtype = p->dtype;
   if (err == hipSuccess && dX) {
-    err = launch_transpose(TransposeArgs{Side{W, e.F * w_stride, 0, w_stride, (int)e.F, (int)e.K, parts}, parts, (int)e.K, p->dtype, at + s.wt, e.F64, wide}, stream);
+    err = launch_transpose(TransposeArgs{Side{W, e.F * w_stride, 0, w_stride, (int)e.F, (int)e.K, parts}, parts, (int)e.K, at + s.wt, e.F64, wide}, stream);
     a.t = direct ? rows_side(dY, dy, e.y) : Side{z.dz, 0, 0, wide, (int)e.M, (int)wide, 1};
     a.K = direct ? (int)e.F : (int)wide;
     a.w = Side{at + s.wt, 0, 0, wide, (int)e.K, a.K, 1};
@@ -285,7 +285,7 @@ int32_t backward(const da2_proj* p, int parts, const void* dY, const da2_tensor*
     if (err == hipSuccess) err = launch_product(a, stream);
   }
   if (err == hipSuccess && dW) {
-    err = launch_transpose(TransposeArgs{rows_side(X, x, e.x), p->B, (int)e.K, p->dtype, at + s.xt, e.Np, e.ldt}, stream);
+    err = launch_transpose(TransposeArgs{rows_side(X, x, e.x), p->B, (int)e.K, at + s.xt, e.Np, e.ldt}, stream);
     a.t = Side{at + s.dzt, e.F64 * e.ldt, 0, e.ldt, (int)e.F, (int)e.ldt, parts};
     a.w = Side{at + s.xt, 0, 0, e.ldt, (int)e.K, (int)e.ldt, 1};
     a.K = (int)e.ldt;

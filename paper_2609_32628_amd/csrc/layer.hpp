@@ -68,9 +68,9 @@ hipError_t launch_column_sum(const float* p, int64_t parts, int64_t cols, int64_
                              int64_t split, int64_t out_sb, hipStream_t stream);
 
 // out[k][b Np + n] = element k of row (b, n), zeros for n from N on and up to column ld of the last sample.
-struct TransposeArgs {
+struct TransposeArgs {  // of 16-bit elements
   Side s;
-  int B, K, dtype;
+  int B, K;
   void* out;
   int64_t Np, ld;
 };
