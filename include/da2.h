@@ -624,7 +624,8 @@ int32_t da2_linear(const da2_proj* p, const void* X, const da2_tensor* x, const 
 /* Gradients of da2_linear (that of R is dY): with dZ = dY gate act'(Z),
  *   dX = dZ W, dW = dZ' X, dbias = column sums of dZ, dgate = those of dY act(Z) (per sample when gate_stride_b > 0).
  * dZ is rounded to the tensors' type for the products with W and X (with neither activation nor gate it
- * is dY itself); the column sums are taken in float32 before.
+ * is dY itself; up to B*N = 16 it is taken in two such numbers, the second what the first left over); the column
+ * sums are taken in float32 before.
  *   Z      what da2_linear wrote; needed with an activation or for dgate
  *   dX     device out per *dx, like X, or NULL; dW device out [F][K], dw_stride elements between the rows, or NULL
  *   dbias  device out [F], or NULL; dgate device out like gate (same gate_stride_b), or NULL
@@ -645,7 +646,7 @@ int32_t da2_glu_ws_bytes(const da2_proj* p, int32_t train, int64_t* bytes);
 int32_t da2_glu(const da2_proj* p, const void* X, const da2_tensor* x, const void* W, int64_t w_stride,
                 const void* bias, void* Y, const da2_tensor* y, float* Z, void* ws, int64_t ws_bytes, void* stream);
 
-/* Gradients of da2_glu: with dG = dY U act'(G) and dU = dY act(G), rounded to the tensors' type for the products,
+/* Gradients of da2_glu: with dG = dY U act'(G) and dU = dY act(G), rounded for the products as dZ is,
  *   dX = dG Wg + dU Wu, dW = [dG' X; dU' X], dbias = their column sums.
  * Z is what da2_glu wrote. The rest as in da2_linear_bwd. */
 int32_t da2_glu_bwd(const da2_proj* p, const void* dY, const da2_tensor* dy, const void* X, const da2_tensor* x,

@@ -156,13 +156,14 @@ BwdSpace bwd_space(const Proj& e, int64_t B, int64_t N) {
     return here;
   };
   const int64_t blocks = B * dz_blocks(B, N, e.F);
-  s.dz = take(2 * e.M * e.parts * e.F64);
-  s.dzt = take(2 * e.parts * e.F64 * e.ldt);
+  const int64_t both = e.M <= kFewTokens ? 2 : 1;  // dZ, and what its rounding left over
+  s.dz = take(2 * both * e.M * e.parts * e.F64);
+  s.dzt = take(2 * both * e.parts * e.F64 * e.ldt);
   s.wt = take(2 * e.K * e.parts * e.F64);
   s.xt = take(2 * e.K * e.ldt);
   s.pbias = take(4 * blocks * e.R);
   s.pgate = take(e.parts == 1 ? 4 * blocks * e.F : 0);
-  s.product = take(std::max(product_ws_bytes(e.M, N, e.K, e.parts * e.F64, 1), product_ws_bytes(e.R, e.F, e.K, e.ldt, 1)));
+  s.product = take(std::max({product_ws_bytes(e.M, N, e.K, e.parts * e.F64, 1), product_ws_bytes(e.R, e.F, e.K, e.ldt, 1), product_ws_bytes(e.R, e.F, e.K, both * e.ldt, 1)}));
   s.bytes = at;
   return s;
 }
@@ -264,6 +265,8 @@ int32_t backward(const da2_proj* p, int parts, const void* dY, const da2_tensor*
   z.F64 = e.F64;
   z.Np = e.Np;
   z.ldt = e.ldt;
+  // Over many tokens and features the rounding of dZ averages out to as much as the gradients' own; over a few it need not.
+  z.lo = !direct && e.M <= kFewTokens;
   if (dbias) z.pbias = reinterpret_cast<float*>(at + s.pbias);
   if (dgate) z.pgate = reinterpret_cast<float*>(at + s.pgate);
   z.dbias = dbias;
@@ -277,7 +280,8 @@ int32_t backward(const da2_proj* p, int parts, const void* dY, const da2_tensor*
   a.dtype = p->dtype;
   if (err == hipSuccess && dX) {
     err = launch_transpose(TransposeArgs{Side{W, e.F * w_stride, 0, w_stride, (int)e.F, (int)e.K, parts}, parts, (int)e.K, at + s.wt, e.F64, wide}, stream);
-    a.t = direct ? rows_side(dY, dy, e.y) : Side{z.dz, 0, 0, wide, (int)e.M, (int)wide, 1};
+    a.t = direct ? rows_side(dY, dy, e.y) : Side{z.dz, 0, wide, wide << z.lo, (int)e.M, (int)wide, 1};
+    a.lo = z.lo;
     a.K = direct ? (int)e.F : (int)wide;
     a.w = Side{at + s.wt, 0, 0, wide, (int)e.K, a.K, 1};
     a.f = plain_finish(out_view(dX, dx), p->Hx, p->Cx, p->N);
@@ -286,7 +290,9 @@ int32_t backward(const da2_proj* p, int parts, const void* dY, const da2_tensor*
   }
   if (err == hipSuccess && dW) {
     err = launch_transpose(TransposeArgs{rows_side(X, x, e.x), p->B, (int)e.K, at + s.xt, e.Np, e.ldt}, stream);
-    a.t = Side{at + s.dzt, e.F64 * e.ldt, 0, e.ldt, (int)e.F, (int)e.ldt, parts};
+    const int64_t ld = e.ldt << z.lo;
+    a.t = Side{at + s.dzt, e.F64 * ld, e.ldt, ld, (int)e.F, (int)e.ldt, parts};
+    a.lo = z.lo;
     a.w = Side{at + s.xt, 0, 0, e.ldt, (int)e.K, (int)e.ldt, 1};
     a.K = (int)e.ldt;
     a.f = plain_finish(OutView{dW, e.F * dw_stride, 0, dw_stride}, 1, e.K, e.F);

@@ -30,7 +30,10 @@ struct Finish {
   int F;             // features (of each part)
 };
 
-// Products of the rows of t (tokens) with the rows of w (weights) over K elements.
+constexpr int kFewTokens = 16;  // of a product by one launch that reads the weights once
+
+// Products of the rows of t (tokens) with the rows of w (weights) over K elements. lo: t's elements are the sums of two
+// blocks of K, t.sh apart (values, and what their rounding left over); K is whole steps.
 struct ProductArgs {
   Side t, w;
   Finish f;
@@ -38,6 +41,7 @@ struct ProductArgs {
   int64_t M;    // rows of t
   int K, parts; // parts: 2 for a gated block (w's rows are part 0, then part 1), else 1
   int dtype;
+  bool lo;
 };
 // Workspace of a product of M rows, which may be taken N at a time.
 int64_t product_ws_bytes(int64_t M, int64_t N, int64_t F, int64_t K, int parts);
@@ -52,9 +56,10 @@ struct DzArgs {
   const void* gate;
   int64_t gate_sb;
   int act, dtype;
-  void* dz;           // [B N][parts][F64], or null
-  void* dzt;          // [parts][F64][ldt], column b Np + n; or null
+  void* dz;           // [B N][1 + lo][parts][F64], or null
+  void* dzt;          // [parts][F64][1 + lo][ldt], column b Np + n; or null
   int64_t F64, Np, ldt;
+  int lo;             // 1: behind the rounded values what rounding left over
   float *pbias, *pgate;  // partial sums [B][blocks][parts][F] and [B][blocks][F], or null
   void *dbias, *dgate;
   int64_t dgate_sb;   // 0: one gate for all samples

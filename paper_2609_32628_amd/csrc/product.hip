@@ -429,7 +429,7 @@ __global__ __launch_bounds__(256) void product_join_kernel(ProductArgs a, int sp
 // Up to 16 tokens: the weights are read once, which bounds it. A workgroup has 16 features (of a gated block both halves) and
 // all tokens; its eight waves take every eighth 64 elements of K each, straight from memory into the operands of the 16x16x32
 // products, two of them on their way at a time, and their sums are added up in order in LDS.
-constexpr int kFew = 16, kFewWaves = 8, kAhead = 2;
+constexpr int kFew = kFewTokens, kFewWaves = 8, kAhead = 2;
 
 // A chunk of a row, of which `left` elements are the row's; zeros behind them.
 __device__ inline s16x8 load_row8(const uint16_t* p, int left) {
@@ -438,7 +438,7 @@ __device__ inline s16x8 load_row8(const uint16_t* p, int left) {
   return __builtin_bit_cast(s16x8, first8(v, left));
 }
 
-template <typename T, bool GLU>
+template <typename T, bool GLU, bool LO>
 __global__ __launch_bounds__(64 * kFewWaves, 4) void product_few_kernel(ProductArgs a) {
   constexpr int P = GLU ? 2 : 1;
   __shared__ __attribute__((aligned(16))) float sums[kFewWaves][kFew][16 * P + 4];
@@ -456,15 +456,18 @@ __global__ __launch_bounds__(64 * kFewWaves, 4) void product_few_kernel(ProductA
     const int h = k / a.t.C;
     return h * a.t.sh + (k - h * a.t.C);
   };
-  const auto add = [&](const s16x8 (&fw)[P][2], const s16x8 (&ft)[2]) {
+  constexpr int L = LO ? 2 : 1;
+  const auto add = [&](const s16x8 (&fw)[P][2], const s16x8 (&ft)[L][2]) {
 #pragma unroll
     for (int c = 0; c < 2; ++c)
 #pragma unroll
-      for (int p = 0; p < P; ++p) acc[p] = mma16<T>(fw[p][c], ft[c], acc[p]);
+      for (int p = 0; p < P; ++p)
+#pragma unroll
+        for (int l = L; l--;) acc[p] = mma16<T>(fw[p][c], ft[l][c], acc[p]);
   };
   int b = wave;
   for (; b + (kAhead - 1) * kFewWaves < whole; b += kAhead * kFewWaves) {
-    s16x8 fw[kAhead][P][2], ft[kAhead][2] = {};
+    s16x8 fw[kAhead][P][2], ft[kAhead][L][2] = {};
 #pragma unroll
     for (int u = 0; u < kAhead; ++u) {
       const int k = (b + u * kFewWaves) * 64;
@@ -473,21 +476,24 @@ __global__ __launch_bounds__(64 * kFewWaves, 4) void product_few_kernel(ProductA
       for (int c = 0; c < 2; ++c) {
 #pragma unroll
         for (int p = 0; p < P; ++p) fw[u][p][c] = *reinterpret_cast<const s16x8*>(w[p] + k + 32 * c);
-        if (live) ft[u][c] = *reinterpret_cast<const s16x8*>(t + x + 32 * c);
+#pragma unroll
+        for (int l = 0; l < L; ++l)
+          if (live) ft[u][l][c] = *reinterpret_cast<const s16x8*>(t + l * a.t.sh + x + 32 * c);
       }
     }
 #pragma unroll
     for (int u = 0; u < kAhead; ++u) add(fw[u], ft[u]);
   }
   for (; b < blocks; b += kFewWaves) {
-    s16x8 fw[P][2], ft[2];
+    s16x8 fw[P][2], ft[L][2];
     const int k = b * 64, left = a.K - k - 8 * g;
     const int64_t x = at(k);
 #pragma unroll
     for (int c = 0; c < 2; ++c) {
 #pragma unroll
       for (int p = 0; p < P; ++p) fw[p][c] = load_row8(w[p] + k + 32 * c, left - 32 * c);
-      ft[c] = load_row8(t + x + 32 * c, live ? left - 32 * c : 0);
+#pragma unroll
+      for (int l = 0; l < L; ++l) ft[l][c] = load_row8(t + l * a.t.sh + x + 32 * c, live ? left - 32 * c : 0);
     }
     add(fw, ft);
   }
@@ -579,13 +585,23 @@ hipError_t launch_product(const ProductArgs& a, hipStream_t stream) {
       } else {
         const unsigned blocks = (a.f.F + 15) / 16;
         if (a.parts == 2) {
-          product_few_kernel<T, true><<<blocks, 64 * kFewWaves, 0, stream>>>(a);
+          product_few_kernel<T, true, false><<<blocks, 64 * kFewWaves, 0, stream>>>(a);
+        } else if (a.lo) {
+          product_few_kernel<T, false, true><<<blocks, 64 * kFewWaves, 0, stream>>>(a);
         } else {
-          product_few_kernel<T, false><<<blocks, 64 * kFewWaves, 0, stream>>>(a);
+          product_few_kernel<T, false, false><<<blocks, 64 * kFewWaves, 0, stream>>>(a);
         }
         return hipGetLastError();
       }
     });
+  if (a.lo) {  // K twice over: the tokens' two blocks, and the weights again
+    ProductArgs two = a;
+    two.lo = false;
+    two.w.C = a.K;
+    two.w.sh = 0;
+    two.K = 2 * a.K;
+    return launch_product(two, stream);
+  }
   // A tile addresses its token rows by 32 bits from the lowest. Samples further apart than that go one by one.
   const int64_t samples = a.t.B;
   if (samples > 1 && (std::min<int64_t>(samples, 256 / a.t.N + 2) * a.t.sb + a.t.N * a.t.sn + (1 << 16)) >> 31) {

@@ -54,7 +54,10 @@ __global__ __launch_bounds__(kThreads) void dz_kernel(DzArgs a, int per, int blo
     for (int i = 0; i < 8; ++i) x[i] = element<T>(v, i);
   };
   if (!GLU && a.gate && left > 0) floats(raw8(static_cast<const T*>(a.gate) + b * a.gate_sb + f8, left), gate);
-  for (int t = blockIdx.y * per; t < min(static_cast<int>((blockIdx.y + 1) * per), tiles); ++t) {
+  // a tile, and once more for what rounding left over
+  const int first = blockIdx.y * per, some = max(min(first + per, tiles) - first, 0);
+  for (int i = 0; i < some << a.lo; ++i) {
+    const int t = first + (i >> a.lo), lo = i & a.lo;
     for (int h = 0; h < 2; ++h) {
       const int row = h * 32 + threadIdx.x / 8, n = t * kTileN + row;
       const bool live = n < a.N && left > 0;
@@ -79,7 +82,7 @@ __global__ __launch_bounds__(kThreads) void dz_kernel(DzArgs a, int per, int blo
                 dz[P - 1][i] = dy[i] * f;
               } else {
                 dz[0][i] = dy[i] * gate[i] * d;
-                sg[i] = __builtin_fmaf(dy[i], i < left ? f : 0.0f, sg[i]);
+                if (!lo) sg[i] = __builtin_fmaf(dy[i], i < left ? f : 0.0f, sg[i]);
               }
             }
           });
@@ -93,13 +96,15 @@ __global__ __launch_bounds__(kThreads) void dz_kernel(DzArgs a, int per, int blo
 #pragma unroll
           for (int i = 0; i < 8; ++i) {
             dz[p][i] = i < left ? dz[p][i] : 0.0f;
-            sb[p][i] += dz[p][i];
+            if (!lo) sb[p][i] += dz[p][i];
+            const float rounded = static_cast<float>(static_cast<T>(dz[p][i]));
+            if (lo) dz[p][i] = __builtin_isfinite(rounded) ? dz[p][i] - rounded : 0.0f;
           }
       }
       if (a.dz && n < a.N && f8 < a.F64) {
 #pragma unroll
         for (int p = 0; p < P; ++p)
-          store_vec(static_cast<T*>(a.dz) + ((static_cast<int64_t>(b) * a.N + n) * P + p) * a.F64 + f8, dz[p]);
+          store_vec(static_cast<T*>(a.dz) + (((static_cast<int64_t>(b) * a.N + n) * (1 + a.lo) + lo) * P + p) * a.F64 + f8, dz[p]);
       }
       if (a.dzt) {
 #pragma unroll
@@ -111,7 +116,7 @@ __global__ __launch_bounds__(kThreads) void dz_kernel(DzArgs a, int per, int blo
       const int64_t n0 = static_cast<int64_t>(t) * kTileN;
 #pragma unroll
       for (int p = 0; p < P; ++p)
-        store_transposed(tile[p], static_cast<uint16_t*>(a.dzt), a.ldt, p * a.F64 + f0, min(kTileN, a.F - f0), b * a.Np + n0, end - n0);
+        store_transposed(tile[p], static_cast<uint16_t*>(a.dzt), a.ldt << a.lo, p * a.F64 + f0, min(kTileN, a.F - f0), lo * a.ldt + b * a.Np + n0, end - n0);
       __syncthreads();
     }
   }
