@@ -360,15 +360,21 @@ __global__ __launch_bounds__(64 * S::kWaves, 2) void product_kernel(ProductArgs 
         ++t16;
       }
       if (t16 < S::kT) ask(t16, i);
+      // by halves: one after the other the comparisons take longer than the part
       const auto put_block = [&]<int SECOND>() {
-        const auto one = [&]<int B>() {
-          constexpr int w = 2 * (B % S::kBlocks) + SECOND * (S::kW / 2);
-          if (part == B) {
-            put(acc[w][B / S::kBlocks], 0);
-            put(acc[w + 1][B / S::kBlocks], 1);
+        const auto among = [&]<int FROM, int TO>(auto&& self) {
+          if constexpr (TO - FROM == 1) {
+            constexpr int w = 2 * (FROM % S::kBlocks) + SECOND * (S::kW / 2);
+            put(acc[w][FROM / S::kBlocks], 0);
+            put(acc[w + 1][FROM / S::kBlocks], 1);
+            asm volatile("; part %0" ::"n"(FROM));  // leaves that are alike would become one, with the sums in memory
+          } else if (part < (FROM + TO) / 2) {
+            self.template operator()<FROM, (FROM + TO) / 2>(self);
+          } else {
+            self.template operator()<(FROM + TO) / 2, TO>(self);
           }
         };
-        [&]<int... B>(std::integer_sequence<int, B...>) { (one.template operator()<B>(), ...); }(std::make_integer_sequence<int, S::kBlocks * S::kT>{});
+        among.template operator()<0, S::kBlocks * S::kT>(among);
       };
       // the wave's lanes read what others wrote: LDS takes its accesses in order, and the compiler has to leave them so
       float v[8], w[8];
