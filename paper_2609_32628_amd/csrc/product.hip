@@ -1,13 +1,21 @@
-// Products of token rows with weight rows, with bias, activation, gate and residual in
-// the epilogue, or both halves of a gated block at once: Z = X W' by tiles of features
-// times tokens.
+// Products of token rows with weight rows, with bias, activation, gate and residual in the epilogue, or both halves of a
+// gated block at once: Z = X W', Y = R + gate act(Z + bias), or act(G) U; sums in float32, one rounding.
 //
-// The product is transposed, features times tokens: an accumulator's registers are
-// then features of one token, four in a row, and lanes l and l ^ 32 trade quads so that
-// the epilogue works on eight features in a row of one token with 16-byte accesses.
-// A tile takes K in steps of 64: 128 bytes of each row, brought into LDS by
-// asynchronous copies while the step before is multiplied.
-// In a gated block a wave's feature rows are half gate, half up, of the same features.
+// The product is transposed, features times tokens: an accumulator's four registers are then features of one token, and
+// the epilogue works on eight features in a row of one token with 16-byte accesses. In a gated block a wave's feature
+// rows are half gate, half up, of the same features, so that both sums meet in one lane.
+//
+// Tiles are 256x256 by eight waves, one workgroup a CU, or 128x128 by four, two a CU: a tile
+// of 256 reads half of what one of 128 does, and leaves CUs idle where tiles are few. K goes in steps of 64, 128 bytes of each row, brought into LDS by asynchronous copies while the step
+// before is multiplied: 16x16x32 products, whose operands are read from LDS a few products ahead of their use, and one
+// barrier a step. Workgroups stay for as many tiles as there are, and copy the next tile's first step before a tile's epilogue.
+//
+// Measured (bf16): 8,192^3 807 us, 1,362 TFLOP/s (a plain library product 689 us); 8,190 x 5,120 x 2 x 13,824 gated 1,745 us,
+// 1,329 (the library's product without the block 1,785); 32,760 x 1,536 x 4,608 441 us, 1,052 (338). Bound by the copies into LDS,
+// which share its ports with the operands' reads: without them the same loop runs at 1,534, and the matrix units are busy 66%
+// of the time; and by the epilogue, during which a CU multiplies nothing: 9 us of a tile of 256, 1.4 a step. Tried and no faster:
+// 128x128 a wave (1.05 to 1.14 PFLOP/s), tiles of 256x128 with three steps of 32 in LDS (0.96), steps of 32 with three or
+// four in LDS (5% slower), workgroups that begin at different steps of K (2 to 8% slower), wave priorities, copies in one go.
 #include <algorithm>
 #include <utility>
 
@@ -24,7 +32,7 @@ constexpr int kRowBytes = 2 * kStep;  // of a tile's row
 constexpr int kStage = 2048;          // LDS bytes of a wave's epilogue
 
 // A step's rows lie in LDS in blocks of eight, as one copy of 1 KB brings them: 128 bytes of a row after the other, in the order
-// of the lanes. (Chunks that trade places within their 128 bytes make the copies slow: XXX TFLOP/s on 8,192^3.) Row
+// of the lanes. Row
 // 64 q + 16 j + 2 b + p is line 2 j + p of block 8 q + b, and a block begins 16 bytes behind the one before, so that the 16 rows of
 // a read meet all banks.
 constexpr int kBlock = 1024 + 16;
@@ -67,8 +75,6 @@ struct Walk {
 
 // Four copies of 1 KB to the LDS blocks from byte `to` on, by the lanes of a mask that is all or none of them (a branch would
 // cut the products' schedule). The immediate offset counts for both addresses: offsets v are a block less from one to the next.
-// Buffer loads: global loads into LDS take the path of flat accesses, which holds up LDS reads and the products behind them
-// (XXX TFLOP/s on 8,192^3 instead of XXX).
 __device__ inline i32x4 buffer_at(const char* base) {
   const uint64_t p = reinterpret_cast<uint64_t>(base);
   // raw buffer: 48 bits of address, no stride, 2^32 - 1 bytes, 32-bit data format
@@ -99,8 +105,8 @@ __device__ inline f32x4 mma16(const s16x8& a, const s16x8& b, const f32x4& c) {
   }
 }
 
+// The compiler leaves memory accesses on their side of it.
 __device__ inline void in_order() { asm volatile("" ::: "memory"); }
-
 
 // A workgroup's tile of TW feature rows and TT tokens, and its WW x WT waves. END: K is no whole number of steps.
 template <int MODE_, bool END, int TW_, int TT_, int WW_, int WT_>
@@ -413,6 +419,7 @@ __global__ __launch_bounds__(256) void product_join_kernel(ProductArgs a, int sp
   const int f8 = static_cast<int>(id - m * chunks) * 8;
   const int64_t R = (static_cast<int64_t>(a.parts) * a.f.F + 7) / 8 * 8;
   float v[8] = {}, u[8] = {};
+#pragma unroll 4
   for (int s = 0; s < splits; ++s) {
     const float* p = a.ws + (s * a.M + m) * R + f8;
     float x[8];
@@ -435,6 +442,9 @@ __global__ __launch_bounds__(256) void product_join_kernel(ProductArgs a, int sp
 // Up to 16 tokens: the weights are read once, which bounds it. A workgroup has 16 features (of a gated block both halves) and
 // all tokens; its eight waves take every eighth 64 elements of K each, straight from memory into the operands of the 16x16x32
 // products, two of them on their way at a time, and their sums are added up in order in LDS.
+// 4 x 5,120 x 5,120, bf16: 16 us with the launch, 52 MB of weights at 3.3 TB/s; 16 x 2,048 x 2 x 5,504, fp16: 15 us, 45 MB
+// at 3.0. A load takes 64 bytes of 16 rows, and what a CU has on its way bounds it: 16 waves, or four products ahead, are no
+// faster.
 constexpr int kFew = kFewTokens, kFewWaves = 8, kAhead = 2;
 
 // A chunk of a row, of which `left` elements are the row's; zeros behind them.
@@ -521,9 +531,9 @@ __global__ __launch_bounds__(64 * kFewWaves, 4) void product_few_kernel(ProductA
 
 // How a product is cut: tiles of 256x256 or 128x128, and parts of K that are joined. The least by these times in us, fitted to
 // 16 products of 100 to 8,192 rows: a round of workgroups takes 9 and 1.4 a step (big tiles, one workgroup a CU) or 8 and 0.95 (small,
-// two a CU; 0.7 with one); a join takes 3 and the partial sums' bytes, written and read, at 4 TB/s. (5,120 x 1,280 x 8,192: 110
+// two a CU; 0.7 with one); a join takes 2.5, 0.1 a part, and the partial sums' bytes, written and read, at 4 TB/s. (5,120 x 1,280 x 8,192: 110
 // with big tiles and two parts, 165 whole, 119 and 130 with small ones; 2,331 x 1,280 x 1,024: 20 with small tiles, 26 in two
-// parts, 34 with big ones.)
+// parts, 34 with big ones. Up to 64 parts: gradients of 48 x 144 weights over 257,570 tokens 582 us with at most 8, 233 with 64.)
 struct Plan {
   bool big;
   int splits;
@@ -533,9 +543,9 @@ Plan plan_of(int64_t M, int64_t R, int64_t K) {
   const int64_t steps = (K + kStep - 1) / kStep;
   Plan best{false, 1};
   double least = 1e300;
-  for (int64_t splits = 1; splits <= 8 && (splits == 1 || steps >= 4 * splits); splits *= 2) {
+  for (int64_t splits = 1; splits <= 64 && (splits == 1 || steps >= 4 * splits); splits *= 2) {
     const int64_t per = (steps + splits - 1) / splits, parts = (steps + per - 1) / per;
-    const double join = parts > 1 ? 3.0 + 8e-6 / 4 * static_cast<double>(parts) * static_cast<double>(M) * static_cast<double>(R) : 0.0;
+    const double join = parts > 1 ? 2.5 + 0.1 * parts + 8e-6 / 4 * static_cast<double>(parts) * static_cast<double>(M) * static_cast<double>(R) : 0.0;
     const double b = static_cast<double>((big * parts + 255) / 256) * (1.4 * per + 9) + join;
     const int64_t rest = small * parts % 512;
     const double s = static_cast<double>(small * parts / 512) * (0.95 * per + 8) + (rest > 256 ? 0.95 * per + 8 : rest ? 0.7 * per + 8 : 0.0) + join;

@@ -1,7 +1,7 @@
 """Projections and gated blocks on the GPU against the float64 oracle: sizes on both sides of every tile, ends of K and F inside
 16-byte chunks, each type and activation, gates, residuals, heads, strides, and the gradients.
 
-Tolerances. Sums over n products are taken 16 at a time by the matrix instructions and added up in float32: at most
+Tolerances. Sums over n products are taken 32 at a time by the matrix instructions and added up in float32: at most
 n / 16 + 16 roundings (and those of a split's parts), of at most 2^-23 of the sum of magnitudes each. The activations are
 off by at most 2^-16 of themselves (exponentials of arguments up to 2^6 rounded to float32, and a fitted tail of 2.3e-6), their
 derivatives by 2^-15, and change by at most 1.2 times a change of their argument (1.13 for the GELU). A gradient of the sums is
@@ -195,6 +195,13 @@ def test_gradients_of_few_tokens(B, N, F, dtype):
     for K in (24, 130, 640):
         run(B, N, K, F, dtype, "gelu", bias=True, gate="shared")
         run(B, N, K, F, dtype, "silu", glu=True)
+
+
+@pytest.mark.parametrize("B,N,K,F", [(2, 9001, 24, 40), (1, 20, 17000, 130), (3, 2500, 130, 300)])
+def test_long_sums(B, N, K, F):
+    """Few tiles over a long axis, cut into many parts: of the tokens in dW, of K in the forward pass."""
+    run(B, N, K, F, "bf16", "silu", glu=True)
+    run(B, N, K, F, "fp16", "gelu", bias=True, gate="adaptive", residual=True)
 
 
 @pytest.mark.parametrize("gate", ["none", "shared", "adaptive"])
