@@ -1,4 +1,5 @@
-// Shared by the kernels that work on tiles in LDS: operand fragments, 32x32x16 MFMAs, LDS reads and asynchronous copies, and the order of work over the XCDs.
+// Shared by the kernels that work on tiles in LDS: operand fragments, 32x32x16 MFMAs,
+// LDS reads and asynchronous copies, and the order of work over the XCDs.
 #pragma once
 
 #include "common.hpp"

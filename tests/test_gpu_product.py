@@ -5,7 +5,7 @@ Tolerances. Sums over n products are taken 32 at a time by the matrix instructio
 n / 16 + 16 roundings (and those of a split's parts), of at most 2^-23 of the sum of magnitudes each. The activations are
 off by at most 2^-16 of themselves (exponentials of arguments up to 2^6 rounded to float32, and a fitted tail of 2.3e-6), their
 derivatives by 2^-15, and change by at most 1.2 times a change of their argument (1.13 for the GELU). A gradient of the sums is
-rounded to the type for the products: half a step of itself, or of its smallest subnormal. A result rounded to the type t
+rounded to the type for the products: half a step of itself, or of its smallest subnormal (up to 16 tokens in two numbers). A result rounded to the type t
 adds finfo(t).eps / 2 of itself, and half the smallest subnormal."""
 import numpy as np
 import pytest
