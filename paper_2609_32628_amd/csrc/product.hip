@@ -11,7 +11,7 @@
 // barrier a step. Workgroups stay for as many tiles as there are, and copy the next tile's first step before a tile's epilogue.
 //
 // Measured (bf16): 8,192^3 807 us, 1,362 TFLOP/s (a plain library product 689 us); 8,190 x 5,120 x 2 x 13,824 gated 1,745 us,
-// 1,329 (the library's product without the block 1,785); 32,760 x 1,536 x 4,608 441 us, 1,052 (338). Bound by the copies into LDS,
+// 1,329 (the library's product without the block 1,785); 32,760 x 1,536 x 4,608 with bias 431 to 443 us, 1,047 to 1,076 (338). Bound by the copies into LDS,
 // which share its ports with the operands' reads: without them the same loop runs at 1,534, and the matrix units are busy 66%
 // of the time; and by the epilogue, during which a CU multiplies nothing: 9 us of a tile of 256, 1.4 a step. Tried and no faster:
 // 128x128 a wave (1.05 to 1.14 PFLOP/s), tiles of 256x128 with three steps of 32 in LDS (0.96), steps of 32 with three or
@@ -343,29 +343,28 @@ __global__ __launch_bounds__(64 * S::kWaves, 2) void product_kernel(ProductArgs 
         for (int e = 0; e < 4; ++e) v[4 * h + e] = x[e];
       }
     };
-    // Part t16, i: tokens t16 * 16 + {0..15}, features i * 32 + {0..31}. What the next part's epilogue reads is asked for before
-    // this part is worked on.
+    // Part p = t16 kBlocks + i: tokens t16 * 16 + {0..15}, features i * 32 + {0..31}. What the next part's epilogue reads is
+    // asked for before this part is worked on.
     constexpr bool GLU = MODE == kGated;
-    const auto row_of_part = [&](int t16) { return min(m0 + t16 * 16 + lane / 4, a.M - 1); };
-    RowPlace<T, GLU> row{}, next_row{};
-    Beside<T, GLU> beside{}, next{};
-    const auto ask = [&](int t16, int i) {
+    constexpr int kParts = S::kBlocks * S::kT;
+    RowPlace<T, GLU> next_row{};
+    Beside<T, GLU> next{};
+    const auto ask = [&](int p) {
       if constexpr (MODE != kPartial) {
-        if (i == 0) next_row = RowPlace<T, GLU>(a.f, row_of_part(t16));
+        const int t16 = p / S::kBlocks, i = p % S::kBlocks;
+        if (i == 0) next_row = RowPlace<T, GLU>(a.f, min(m0 + t16 * 16 + lane / 4, a.M - 1));
         next = Beside<T, GLU>(a.f, next_row, min(f0 + i * 32 + 8 * chunk, a.f.F - 1), min(f0 + i * 32, a.f.F - 1));
       }
     };
-    ask(0, 0);
-#pragma unroll 1
-    for (int t16 = 0, i = 0; t16 < S::kT;) {
-      row = next_row;
-      beside = next;
-      const int part = i + t16 * S::kBlocks, at16 = t16, f8 = f0 + i * 32 + 8 * chunk;
-      if (++i == S::kBlocks) {
-        i = 0;
-        ++t16;
-      }
-      if (t16 < S::kT) ask(t16, i);
+    ask(0);
+    // two at a time where registers allow it (32,760 x 1,536 x 4,608: 431 us instead of 453; gated and small tiles 3 and 1% slower)
+    constexpr int kTogether = MODE == kLinear && TW == 256 ? 2 : 1;
+#pragma unroll kTogether
+    for (int part = 0; part < kParts; ++part) {
+      const int at16 = part / S::kBlocks, f8 = f0 + part % S::kBlocks * 32 + 8 * chunk;
+      const RowPlace<T, GLU> row = next_row;
+      const Beside<T, GLU> beside = next;
+      if (part + 1 < kParts) ask(part + 1);
       // by halves: one after the other the comparisons take longer than the part
       const auto put_block = [&]<int SECOND>() {
         const auto among = [&]<int FROM, int TO>(auto&& self) {
