@@ -5,15 +5,17 @@
 // the epilogue works on eight features in a row of one token with 16-byte accesses. In a gated block a wave's feature
 // rows are half gate, half up, of the same features, so that both sums meet in one lane.
 //
-// Tiles are 256x256 by eight waves, one workgroup a CU, or 128x128 by four, two a CU: a tile
-// of 256 reads half of what one of 128 does, and leaves CUs idle where tiles are few. K goes in steps of 64, 128 bytes of each row, brought into LDS by asynchronous copies while the step
-// before is multiplied: 16x16x32 products, whose operands are read from LDS a few products ahead of their use, and one
-// barrier a step. Workgroups stay for as many tiles as there are, and copy the next tile's first step before a tile's epilogue.
+// Tiles are 256x256 by eight waves, one workgroup a CU, or 128x128 by four, two a CU: a tile of 256 reads half of what
+// one of 128 does, and leaves CUs idle where tiles are few. K goes in steps of 64, 128 bytes of each row, brought into LDS by
+// asynchronous copies while the step before is multiplied: 16x16x32 products, whose operands are read from LDS a few products
+// ahead of their use, and one barrier a step. Workgroups stay for as many tiles as there are, and copy the next tile's first
+// step before a tile's epilogue.
 //
 // Measured (bf16): 8,192^3 807 us, 1,362 TFLOP/s (a plain library product 689 us); 8,190 x 5,120 x 2 x 13,824 gated 1,745 us,
-// 1,329 (the library's product without the block 1,785); 32,760 x 1,536 x 4,608 with bias 431 to 443 us, 1,047 to 1,076 (338). Bound by the copies into LDS,
-// which share its ports with the operands' reads: without them the same loop runs at 1,534, and the matrix units are busy 66%
-// of the time; and by the epilogue, during which a CU multiplies nothing: 9 us of a tile of 256, 1.4 a step. Tried and no faster:
+// 1,329 (the library's product without the block 1,785); 32,760 x 1,536 x 4,608 with bias 431 to 443 us, 1,047 to 1,076 (338).
+// Bound by the copies into LDS, which share its ports with the operands' reads: without them the same loop runs at 1,534, and
+// the matrix units are busy 66% of the time; and by the epilogue, during which a CU multiplies nothing: 9 us of a tile of 256,
+// 1.4 a step. Tried and no faster:
 // 128x128 a wave (1.05 to 1.14 PFLOP/s), tiles of 256x128 with three steps of 32 in LDS (0.96), steps of 32 with three or
 // four in LDS (5% slower), workgroups that begin at different steps of K (2 to 8% slower), wave priorities, copies in one go.
 #include <algorithm>
