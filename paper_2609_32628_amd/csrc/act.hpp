@@ -34,8 +34,9 @@ __device__ inline float normal_cdf(float z, float& e) {
 template <int ACT, bool D>
 __device__ inline float act_one(float z, float& d) {
   if constexpr (ACT == DA2_ACT_RELU) {
-    if (D) d = z > 0.0f ? 1.0f : 0.0f;
-    return z > 0.0f ? z : z * 0.0f;  // a NaN stays one
+    // a NaN stays one, in both; -inf gives 0
+    if (D) d = z > 0.0f ? 1.0f : z <= 0.0f ? 0.0f : z;
+    return z < 0.0f ? 0.0f : z;
   } else if constexpr (ACT == DA2_ACT_GELU) {
     float e;
     const float p = normal_cdf(z, e);

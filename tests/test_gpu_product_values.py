@@ -1,0 +1,96 @@
+"""Projections and gated blocks on the GPU at single sums: activations and their derivatives at infinities and at NaN.
+
+The rows of X are zeros, so that a sum is its bias, exactly; one row of dY is ones and the others zeros, so that dbias is the
+derivative there, and dgate the activation.
+
+Tolerances. Exponentials of arguments rounded to float32 are off by at most |argument| 2^-23 of themselves, quotients and the few products
+around them by 2^-21, the GELU's tail by 2.3e-6: 2^-15 of the value covers them for arguments up to 100. A result rounded to the type
+t adds finfo(t).eps / 2 of itself, and half the smallest subnormal."""
+import numpy as np
+import pytest
+import torch
+
+from oracle import layer
+from paper_2609_32628_amd import api
+
+pytestmark = pytest.mark.gpu
+T = {"bf16": torch.bfloat16, "fp16": torch.float16}
+INF, NAN = float("inf"), float("nan")
+
+
+def f64(x):
+    return x.double().cpu().numpy()
+
+
+def close(got, want, what):
+    t = torch.finfo(got.dtype)
+    got = f64(got)
+    tol = (2.0 ** -15 + t.eps / 2 * (1 + 2.0 ** -15)) * np.abs(want) + t.smallest_normal * t.eps / 2
+    with np.errstate(invalid="ignore"):
+        near = (np.abs(got - want) <= tol) | (got == want) | (np.isnan(got) & np.isnan(want))
+    assert near.all(), (what, got[~near], np.broadcast_to(want, got.shape)[~near])
+
+
+def rows(M, F, t):
+    """[1, 1, M, F] rows, each padded to 16 bytes."""
+    return torch.zeros(1, 1, M, -(-F // 8) * 8, dtype=t, device="cuda")[..., :F]
+
+
+def sums(values, act, dtype, M):
+    """(Y, dbias, dgate) of a projection of M tokens whose sums are the values."""
+    t = T[dtype]
+    bias = torch.tensor(values, dtype=torch.float64).to(t).cuda()
+    F = bias.numel()
+    X, W = torch.zeros(1, 1, M, 72, dtype=t, device="cuda"), torch.ones(F, 72, dtype=t, device="cuda")
+    Y, dY = rows(M, F, t), rows(M, F, t)
+    dY[0, 0, M // 2] = 1
+    gate, dbias, dgate = torch.ones_like(bias), torch.empty_like(bias), torch.empty_like(bias)
+    ws = torch.empty(max(1, api.da2_linear_ws_bytes(X, W, Y, True)), dtype=torch.uint8, device="cuda")
+    Z = api.da2_linear_z(X, Y)
+    api.da2_linear(X, W, Y, bias, act=act, gate=gate, Z=Z, ws=ws)
+    api.da2_linear_bwd(dY, X, W, Z, dbias=dbias, act=act, gate=gate, dgate=dgate, ws=ws)
+    return f64(bias), Y[0, 0], dbias, dgate
+
+
+def halves(values, act, dtype, M):
+    """Y and dbias's first half of a gated block whose gate sums are the values and whose other half is 1."""
+    t = T[dtype]
+    g = torch.tensor(values, dtype=torch.float64).to(t).cuda()
+    F = g.numel()
+    X, W = torch.zeros(1, 1, M, 72, dtype=t, device="cuda"), torch.ones(2 * F, 72, dtype=t, device="cuda")
+    Y, dY = rows(M, F, t), rows(M, F, t)
+    dY[0, 0, M // 2] = 1
+    bias, Z = torch.cat([g, torch.ones_like(g)]), api.da2_glu_z(X, Y)
+    dbias = torch.empty_like(bias)
+    ws = torch.empty(max(1, api.da2_glu_ws_bytes(X, W, Y, True)), dtype=torch.uint8, device="cuda")
+    api.da2_glu(X, W, Y, bias, act=act, Z=Z, ws=ws)
+    api.da2_glu_bwd(dY, X, W, Z, dbias=dbias, act=act, ws=ws)
+    return f64(g), Y[0, 0], dbias[:F], dbias[F:]
+
+
+# z Phi(z) and z / (1 + exp(-z)) are -inf 0 and -inf / inf at -inf
+AT = {"none": (-INF, INF), "relu": (0.0, INF), "gelu": (NAN, INF), "gelu_tanh": (NAN, INF), "silu": (NAN, INF), "sigmoid": (0.0, 1.0)}
+
+
+@pytest.mark.parametrize("act", AT)
+@pytest.mark.parametrize("M", [3, 40])
+@pytest.mark.parametrize("dtype", ["bf16", "fp16"])
+def test_infinities_and_nan(act, M, dtype):
+    """max(z, 0) and 1 / (1 + exp(-z)) have values at -inf; a NaN stays one."""
+    values = [-INF, INF, NAN, -3.0, 0.0, 2.0] + [1.0] * 12
+    with np.errstate(invalid="ignore"):
+        want = layer.act(np.array(values), act)[0]
+    np.testing.assert_array_equal(want[:3], [*AT[act], NAN])
+    for make in (sums, halves):
+        _, Y, _, sum_of = make(values, act, dtype, M)
+        close(Y, want[None], (make, "Y"))
+        # dgate, or dbias's second half; the other rows add 0 f(z)
+        close(sum_of, np.where(np.isinf(want), NAN, want), (make, "dY f"))
+
+
+@pytest.mark.parametrize("M", [3, 40])
+@pytest.mark.parametrize("dtype", ["bf16", "fp16"])
+def test_relu_at_infinities_and_nan_backward(M, dtype):
+    for make in (sums, halves):
+        _, _, slope, _ = make([-INF, INF, NAN, -3.0, 0.0, 2.0, 1.0, 1.0], "relu", dtype, M)
+        np.testing.assert_array_equal(f64(slope), [0, 1, NAN, 0, 0, 1, 1, 1])
