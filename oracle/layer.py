@@ -37,7 +37,7 @@ def act(z, kind):
     if kind == "silu":
         return z * sig(z), sig(z) * (1 + z * (1 - sig(z)))
     if kind == "sigmoid":
-        return sig(z), sig(z) * (1 - sig(z))
+        return sig(z), sig(z) * sig(-z)
     return z, np.ones_like(z)
 
 

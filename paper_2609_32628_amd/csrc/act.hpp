@@ -52,9 +52,10 @@ __device__ inline float act_one(float z, float& d) {
     if (D) d = __builtin_fmaf(z, p - p * p, p);
     return z * p;
   } else if constexpr (ACT == DA2_ACT_SIGMOID) {
-    const float p = rcp_fast(1.0f + exp_fast(-z));
-    if (D) d = p - p * p;
-    return p;
+    // from the smaller side, where 1 - p would have no digits left (p - p p is off by 6% at 16 and 0 from 17 on)
+    const float e = exp_fast(-__builtin_fabsf(z)), p = rcp_fast(1.0f + e);
+    if (D) d = e * p * p;
+    return z < 0.0f ? e * p : p;
   } else {
     if (D) d = 1.0f;
     return z;

@@ -1,4 +1,5 @@
-"""Projections and gated blocks on the GPU at single sums: activations and their derivatives at infinities and at NaN.
+"""Projections and gated blocks on the GPU at single sums: activations and their derivatives at infinities, at NaN and in
+their tails.
 
 The rows of X are zeros, so that a sum is its bias, exactly; one row of dY is ones and the others zeros, so that dbias is the
 derivative there, and dgate the activation.
@@ -94,3 +95,18 @@ def test_relu_at_infinities_and_nan_backward(M, dtype):
     for make in (sums, halves):
         _, _, slope, _ = make([-INF, INF, NAN, -3.0, 0.0, 2.0, 1.0, 1.0], "relu", dtype, M)
         np.testing.assert_array_equal(f64(slope), [0, 1, NAN, 0, 0, 1, 1, 1])
+
+
+# sums that both types hold, around zero and far out on both sides
+NEAR = np.concatenate([np.linspace(-30, 30, 241), [-60, -40, 40, 60]])
+
+
+@pytest.mark.parametrize("M", [3, 40])
+@pytest.mark.parametrize("dtype", ["bf16", "fp16"])
+def test_sigmoid_keeps_its_digits(M, dtype):
+    """p (1 - p) to the relative error of the type on both sides, as long as the type holds it."""
+    for make in (sums, halves):
+        z, Y, slope, _ = make(NEAR, "sigmoid", dtype, M)
+        small = np.exp(-np.abs(z)) / (1 + np.exp(-np.abs(z)))
+        close(Y, np.where(z < 0, small, 1 - small)[None], (make, "Y"))
+        close(slope, small * (1 - small), (make, "slope"))
