@@ -45,7 +45,11 @@ __device__ inline float act_one(float z, float& d) {
   } else if constexpr (ACT == DA2_ACT_GELU_TANH) {  // z (1 + tanh u) / 2 = z / (1 + exp(-2 u))
     constexpr float a = 2 * 0.79788456080286536f, b = a * 0.044715f;
     const float zz = z * z, p = rcp_fast(1.0f + exp_fast(-z * __builtin_fmaf(zz, b, a)));
-    if (D) d = __builtin_fmaf(z * (p - p * p), __builtin_fmaf(zz, 3 * b, a), p);
+    if (D) {
+      // beyond 32 p is 0 or 1 and p - p p is 0, but its factor of z^3 would be infinite from 2^64 on, and 0 times that a NaN
+      const float c = __builtin_amdgcn_fmed3f(z, -32.0f, 32.0f);
+      d = __builtin_fmaf(c * (p - p * p), __builtin_fmaf(c * c, 3 * b, a), p);
+    }
     return z * p;
   } else if constexpr (ACT == DA2_ACT_SILU) {
     const float p = rcp_fast(1.0f + exp_fast(-z));

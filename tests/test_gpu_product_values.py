@@ -1,5 +1,5 @@
-"""Projections and gated blocks on the GPU at single sums: activations and their derivatives at infinities, at NaN and in
-their tails.
+"""Projections and gated blocks on the GPU at single sums: activations and their derivatives at infinities, at NaN, in their
+tails and far beyond them.
 
 The rows of X are zeros, so that a sum is its bias, exactly; one row of dY is ones and the others zeros, so that dbias is the
 derivative there, and dgate the activation.
@@ -110,3 +110,21 @@ def test_sigmoid_keeps_its_digits(M, dtype):
         small = np.exp(-np.abs(z)) / (1 + np.exp(-np.abs(z)))
         close(Y, np.where(z < 0, small, 1 - small)[None], (make, "Y"))
         close(slope, small * (1 - small), (make, "slope"))
+
+
+# far out; bf16 holds further ones
+FAR = [-1e4, 1e4, -6e4, 6e4]
+FARTHER = [s * v for v in (1e6, 1e10, 1e19, 1e20, 1e30, 3e38) for s in (-1, 1)]
+
+
+@pytest.mark.parametrize("act", ["none", "relu", "gelu", "gelu_tanh", "silu", "sigmoid"])
+@pytest.mark.parametrize("M", [3, 40])
+@pytest.mark.parametrize("dtype", ["bf16", "fp16"])
+def test_far_sums(act, M, dtype):
+    """Far out an activation is 0, 1 or its sum, and its derivative 0 or 1."""
+    values = FAR + (FARTHER if dtype == "bf16" else [])
+    for make in (sums, halves):
+        z, Y, slope, _ = make(values, act, dtype, M)
+        up, below = (np.ones_like(z), np.zeros_like(z)) if act == "sigmoid" else (z, z if act == "none" else np.zeros_like(z))
+        close(Y, np.where(z > 0, up, below)[None], (make, "Y"))
+        close(slope, np.where(z > 0, act != "sigmoid", act == "none").astype(np.float64), (make, "slope"))
