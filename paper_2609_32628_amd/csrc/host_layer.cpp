@@ -163,7 +163,10 @@ BwdSpace bwd_space(const Proj& e, int64_t B, int64_t N) {
   s.xt = take(2 * e.K * e.ldt);
   s.pbias = take(4 * blocks * e.R);
   s.pgate = take(e.parts == 1 ? 4 * blocks * e.F : 0);
-  s.product = take(std::max({product_ws_bytes(e.M, N, e.K, e.parts * e.F64, 1), product_ws_bytes(e.R, e.F, e.K, e.ldt, 1), product_ws_bytes(e.R, e.F, e.K, both * e.ldt, 1)}));
+  int64_t product = 0;
+  for (int64_t n = 1; n <= both; ++n)
+    product = std::max({product, product_ws_bytes(e.M, N, e.K, n * e.parts * e.F64, 1), product_ws_bytes(e.R, e.F, e.K, n * e.ldt, 1)});
+  s.product = take(product);
   s.bytes = at;
   return s;
 }

@@ -2,6 +2,7 @@
 // the norm and rotation of Q and K in one pass. Internal to libda2.
 #pragma once
 
+#include "plan.hpp"
 #include "token.hpp"
 
 namespace da2 {
@@ -29,8 +30,6 @@ struct Finish {
   int N;             // tokens of a sample
   int F;             // features (of each part)
 };
-
-constexpr int kFewTokens = 16;  // of a product by one launch that reads the weights once
 
 // Products of the rows of t (tokens) with the rows of w (weights) over K elements. lo: t's elements are the sums of two
 // blocks of K, t.sh apart (values, and what their rounding left over); K is whole steps.

@@ -29,7 +29,6 @@ namespace {
 
 enum Mode { kLinear, kGated, kPartial };
 
-constexpr int kStep = 64;            // elements of K a step
 constexpr int kRowBytes = 2 * kStep;  // of a tile's row
 constexpr int kStage = 2048;          // LDS bytes of a wave's epilogue
 
@@ -530,38 +529,6 @@ __global__ __launch_bounds__(64 * kFewWaves, 4) void product_few_kernel(ProductA
   finish8<T, GLU>(a.f, row, Beside<T, GLU>(a.f, row, f8, f8), v[0], v[1], f8);
 }
 
-// How a product is cut: tiles of 256x256 or 128x128, and parts of K that are joined. The least by these times in us, fitted to
-// 16 products of 100 to 8,192 rows: a round of workgroups takes 9 and 1.4 a step (big tiles, one workgroup a CU) or 8 and 0.95 (small,
-// two a CU; 0.7 with one); a join takes 2.5, 0.1 a part, and the partial sums' bytes, written and read, at 4 TB/s. (5,120 x 1,280 x 8,192: 110
-// with big tiles and two parts, 165 whole, 119 and 130 with small ones; 2,331 x 1,280 x 1,024: 20 with small tiles, 26 in two
-// parts, 34 with big ones. Up to 64 parts: gradients of 48 x 144 weights over 257,570 tokens 582 us with at most 8, 233 with 64.)
-struct Plan {
-  bool big;
-  int splits;
-};
-Plan plan_of(int64_t M, int64_t R, int64_t K) {
-  const int64_t big = ((M + 255) / 256) * ((R + 255) / 256), small = ((M + 127) / 128) * ((R + 127) / 128);
-  const int64_t steps = (K + kStep - 1) / kStep;
-  Plan best{false, 1};
-  double least = 1e300;
-  for (int64_t splits = 1; splits <= 64 && (splits == 1 || steps >= 4 * splits); splits *= 2) {
-    const int64_t per = (steps + splits - 1) / splits, parts = (steps + per - 1) / per;
-    const double join = parts > 1 ? 2.5 + 0.1 * parts + 8e-6 / 4 * static_cast<double>(parts) * static_cast<double>(M) * static_cast<double>(R) : 0.0;
-    const double b = static_cast<double>((big * parts + 255) / 256) * (1.4 * per + 9) + join;
-    const int64_t rest = small * parts % 512;
-    const double s = static_cast<double>(small * parts / 512) * (0.95 * per + 8) + (rest > 256 ? 0.95 * per + 8 : rest ? 0.7 * per + 8 : 0.0) + join;
-    if (b < least) {
-      least = b;
-      best = {true, static_cast<int>(parts)};
-    }
-    if (s < least) {
-      least = s;
-      best = {false, static_cast<int>(parts)};
-    }
-  }
-  return best;
-}
-
 template <typename T, typename S>
 hipError_t launch_tiles(const ProductArgs& a, int splits, hipStream_t stream) {
   // a gated tile's rows are two for each feature
@@ -586,15 +553,11 @@ hipError_t launch_plan(const ProductArgs& a, const Plan& p, hipStream_t stream) 
 }  // namespace
 
 int64_t product_ws_bytes(int64_t M, int64_t N, int64_t F, int64_t K, int parts) {
-  const auto of = [&](int64_t rows) {
-    const Plan p = plan_of(rows, F * parts, K);
-    return rows > kFew && p.splits > 1 ? 4 * p.splits * rows * ((F * parts + 7) / 8 * 8) : 0;
-  };
-  return M == N ? of(M) : std::max(of(M), of(N));
+  return std::max(partial_bytes(M, F, K, parts), M == N ? 0 : partial_bytes(N, F, K, parts));
 }
 
 hipError_t launch_product(const ProductArgs& a, hipStream_t stream) {
-  if (a.M <= kFew)
+  if (few_rows(a.M, a.f.F, a.K, a.parts))
     return by_dtype(a.dtype, [&](auto t) {
       using T = decltype(t);
       if constexpr (sizeof(T) == 4) {
@@ -611,7 +574,7 @@ hipError_t launch_product(const ProductArgs& a, hipStream_t stream) {
         return hipGetLastError();
       }
     });
-  if (a.lo) {  // K twice over: the tokens' two blocks, and the weights again
+  if (a.lo) {  // K twice over: the tokens' two blocks, and the weights again (still too long for few rows)
     ProductArgs two = a;
     two.lo = false;
     two.w.C = a.K;

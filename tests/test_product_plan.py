@@ -1,0 +1,70 @@
+"""How products are cut (few rows at once, tiles of two sizes, parts of a long sum), from the library's own rule compiled for the CPU:
+long sums are not left to a few workgroups, and workspaces follow."""
+import os
+import subprocess
+
+import pytest
+
+from paper_2609_32628_amd import _lib
+
+PROBE = os.path.join(os.path.dirname(os.path.abspath(__file__)), "probes", "plan_probe.cpp")
+
+
+@pytest.fixture(scope="module")
+def plans(tmp_path_factory):
+    """For (rows, features, K, parts) each: (kernel, parts of K, K ends inside a step, several units a workgroup, bytes)."""
+    exe = str(tmp_path_factory.mktemp("plan") / "plan_probe")
+    subprocess.run(["g++", "-O1", "-std=c++20", "-o", exe, PROBE], check=True, timeout=120)
+
+    def ask(shapes):
+        r = subprocess.run([exe], input="".join("%d %d %d %d\n" % s for s in shapes), capture_output=True, text=True, check=True, timeout=60)
+        out = [line.split() for line in r.stdout.splitlines()]
+        assert len(out) == len(shapes)
+        return [(o[0], int(o[1]), o[2] == "1", o[3] == "1", int(o[4])) for o in out]
+
+    return ask
+
+
+def ws_bytes(call, train, B, N, K, F):
+    out = _lib.ctypes.c_int64()
+    assert getattr(_lib.lib(), call)(_lib.Proj(B, N, 1, K, 1, F, 0, _lib.DA2_BF16), train, out) == 0
+    return out.value
+
+
+@pytest.mark.parametrize("rows", [1, 5, 16])
+def test_long_sums_of_few_rows_are_cut(plans, rows):
+    """The kernel for few rows has a workgroup for 16 features and does not cut K: 4 workgroups for 64 features, however long K is."""
+    for F in (1, 16, 64, 1000):
+        for K in (20000, 200000, 1 << 22):
+            kernel, cut, _, _, _ = plans([(rows, F, K, 1)])[0]
+            assert kernel != "few" and cut >= 8, (F, K)
+    short = plans([(rows, F, K, parts) for F in (16, 1000, 8192) for K in (64, 2048, 4096) for parts in (1, 2)])
+    assert all(p[0] == "few" for p in short)
+
+
+def test_workspaces_of_few_rows(plans):
+    """Calls of few tokens with a long sum need room for its parts, forward, and backward for the gradients of few weight rows and for
+    those of few tokens of many features, whose two numbers count twice."""
+    for call, parts in (("da2_linear_ws_bytes", 1), ("da2_glu_ws_bytes", 2)):
+        for N, K, F in ((1, 131072, 64), (16, 20000, 100), (3, 5000, 40), (1, 64, 64)):
+            (kernel, _, _, _, need), = plans([(N, F, K, parts)])
+            assert ws_bytes(call, 0, 1, N, K, F) == need and (need > 0) == (K > 64 and (kernel != "few"))
+        for N, K, F in ((200000, 64, 16 // parts), (5, 24, 9000), (16, 100, 5000)):
+            rows, wide, up = F * parts, -(-F // 64) * 64 * parts, -(-(-(-N // 8) * 8) // 64) * 64
+            both = 2 if N <= 16 else 1
+            products = [(N, K, n * wide, 1) for n in range(1, both + 1)] + [(rows, K, n * up, 1) for n in range(1, both + 1)]
+            need = max(p[4] for p in plans(products))
+            assert need > 0 and ws_bytes(call, 1, 1, N, K, F) >= need + 2 * both * (N + up) * wide
+
+
+# (tokens, K, F, gated) of gradients: of few weight rows over many tokens, of few tokens of many features
+GRADIENTS = [(18002, 24, 16, False), (20000, 130, 3, False), (18002, 72, 8, True),
+             (5, 24, 9000, False), (16, 100, 5000, True), (1, 40, 20000, False)]
+
+
+def test_gradients_reach_the_cut_products(plans):
+    up = lambda n: -(-n // 64) * 64  # noqa: E731
+    dw = plans([(F * (1 + glu), K, up(M) * (2 if M <= 16 else 1), 1) for M, K, F, glu in GRADIENTS])
+    dx = plans([(M, K, up(F) * (1 + glu) * (2 if M <= 16 else 1), 1) for M, K, F, glu in GRADIENTS])
+    assert all(p[0] == "small" and p[1] > 1 for p in dw[:3])
+    assert all(p[0] == "small" and p[1] > 1 for p in dx[3:])
