@@ -1,11 +1,16 @@
-"""Projections and gated blocks on the GPU against the float64 oracle where few rows meet long sums, which are cut into parts;
-test_product_plan checks on the CPU that they are. Tolerances: those of test_gpu_product."""
+"""Projections and gated blocks on the GPU against the float64 oracle at shapes that reach every way of cutting a product;
+test_product_plan checks on the CPU that they do. Tolerances: those of test_gpu_product."""
 import pytest
 
 from test_gpu_product import run
-from test_product_plan import GRADIENTS
+from test_product_plan import GRADIENTS, PATHS
 
 pytestmark = pytest.mark.gpu
+
+
+@pytest.mark.parametrize("M,K,F,glu", PATHS)
+def test_forward(M, K, F, glu):
+    run(1, M, K, F, "bf16", "silu", bias=True, glu=glu, train=False, **({} if glu else dict(gate="shared", residual=True)))
 
 
 @pytest.mark.parametrize("M,K,F,glu", GRADIENTS)
@@ -13,7 +18,7 @@ def test_gradients(M, K, F, glu):
     run(1, M, K, F, "bf16", "silu", bias=True, glu=glu)
 
 
-@pytest.mark.parametrize("M,K,F,glu", GRADIENTS)
+@pytest.mark.parametrize("M,K,F,glu", GRADIENTS[2:])
 def test_gradients_of_plain_projections(M, K, F, glu):
     """Nothing between dY and dZ (a gated block in fp16)."""
     run(1, M, K, F, "fp16", "silu" if glu else "none", glu=glu)

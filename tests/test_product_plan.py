@@ -1,5 +1,5 @@
 """How products are cut (few rows at once, tiles of two sizes, parts of a long sum), from the library's own rule compiled for the CPU:
-long sums are not left to a few workgroups, and workspaces follow."""
+long sums are not left to a few workgroups, workspaces follow, and the shapes that the GPU tests run reach every kernel."""
 import os
 import subprocess
 
@@ -57,14 +57,37 @@ def test_workspaces_of_few_rows(plans):
             assert need > 0 and ws_bytes(call, 1, 1, N, K, F) >= need + 2 * both * (N + up) * wide
 
 
-# (tokens, K, F, gated) of gradients: of few weight rows over many tokens, of few tokens of many features
-GRADIENTS = [(18002, 24, 16, False), (20000, 130, 3, False), (18002, 72, 8, True),
+# (tokens, K, F, gated) of forward products
+PATHS = [(700, 64, 12800, False), (700, 40, 12800, False), (2000, 64, 9000, False), (2000, 40, 9000, False), (300, 64, 12800, True), (300, 40, 12800, True),
+         (700, 64, 12800, True), (700, 40, 12800, True), (3000, 8192, 257, False), (6000, 4100, 257, False), (4154, 6016, 67, True), (4154, 5932, 67, True),
+         (640, 64, 12800, True), (640, 40, 12800, True), (1025, 64, 13120, False), (2101, 40, 7426, False), (17, 6720, 8538, False), (17, 7625, 8386, False),
+         (19, 7616, 4108, True), (21, 8333, 4314, True), (40, 64, 72, False), (40, 40, 72, False), (40, 64, 72, True), (40, 40, 72, True),
+         (20, 1024, 40, False), (20, 1000, 40, False), (20, 1024, 40, True), (20, 1000, 40, True), (5, 64, 40, False), (5, 40, 40, True)]
+# (tokens, K, F, gated) of gradients: of weights on large tiles in parts, of few weight rows over many tokens, of few tokens of many features
+GRADIENTS = [(8192, 257, 3000, False), (8150, 257, 1500, True), (18002, 24, 16, False), (20000, 130, 3, False), (18002, 72, 8, True),
              (5, 24, 9000, False), (16, 100, 5000, True), (1, 40, 20000, False)]
+
+
+def test_shapes_reach_every_kernel(plans):
+    """Each tile, with whole steps and without, plain, gated and in parts, with one unit of work a workgroup and with several. (Large
+    tiles in parts are only taken where they are too few for the card, so no workgroup has several.)"""
+    seen = set()
+    for (M, K, F, glu), (kernel, cut, end, several, _) in zip(PATHS, plans([(M, F, K, 1 + glu) for M, K, F, glu in PATHS])):
+        seen.add((kernel, "gated" if glu else "plain", cut > 1, end, several) if kernel != "few" else (kernel, glu))
+    want = {("few", False), ("few", True)}
+    for tile in ("big", "small"):
+        for kind in ("plain", "gated"):
+            for end in (False, True):
+                want |= {(tile, kind, False, end, False), (tile, kind, False, end, True), (tile, kind, True, end, False)}
+                if tile == "small":
+                    want.add((tile, kind, True, end, True))
+    assert seen == want, (sorted(want - seen, key=str), sorted(seen - want, key=str))
 
 
 def test_gradients_reach_the_cut_products(plans):
     up = lambda n: -(-n // 64) * 64  # noqa: E731
     dw = plans([(F * (1 + glu), K, up(M) * (2 if M <= 16 else 1), 1) for M, K, F, glu in GRADIENTS])
     dx = plans([(M, K, up(F) * (1 + glu) * (2 if M <= 16 else 1), 1) for M, K, F, glu in GRADIENTS])
-    assert all(p[0] == "small" and p[1] > 1 for p in dw[:3])
-    assert all(p[0] == "small" and p[1] > 1 for p in dx[3:])
+    assert all(p[0] == "big" and p[1] > 1 for p in dw[:2])
+    assert all(p[0] == "small" and p[1] > 1 for p in dw[2:5])
+    assert all(p[0] == "small" and p[1] > 1 for p in dx[5:])
