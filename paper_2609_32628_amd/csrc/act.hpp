@@ -167,10 +167,21 @@ struct Beside {
   }
 };
 
+// The factor of the sums, the same for all: through the scalar cache, since a vector load would wait for the copies issued before it.
+template <typename T, bool GLU>
+__device__ inline float back_of(const Finish& e) {
+  if (GLU || !kScaledDz<T> || !e.back) return 1.0f;
+  return *(const __attribute__((address_space(4))) float*)e.back;
+}
+
 // Features [f8, f8 + 8) of a row from their sums v (gated block: v and u).
 template <typename T, bool GLU>
-__device__ inline void finish8(const Finish& e, const RowPlace<T, GLU>& row, const Beside<T, GLU>& x, float* v, float* u, int f8) {
+__device__ inline void finish8(const Finish& e, const RowPlace<T, GLU>& row, const Beside<T, GLU>& x, float back, float* v, float* u, int f8) {
   const int left = e.F - f8;
+  if (!GLU && kScaledDz<T> && back != 1.0f) {
+#pragma unroll
+    for (int i = 0; i < 8; ++i) v[i] *= back;
+  }
   if (e.bias) {
 #pragma unroll
     for (int i = 0; i < 8; ++i) {

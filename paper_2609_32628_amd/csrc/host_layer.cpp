@@ -84,6 +84,7 @@ struct Proj {
   int64_t M, K, F, R;  // tokens, input features, output features, rows of W
   int parts;
   int64_t F8, F64, Np, ldt;
+  int dtype;
 };
 
 bool same(const void* a, const void* b) { return a == b; }
@@ -110,6 +111,7 @@ int32_t check_proj(const da2_proj* p, int parts, Proj* e) {
   e->F64 = up(e->F, 64);
   e->Np = up(p->N, 8);
   e->ldt = up(p->B * e->Np, 64);
+  e->dtype = p->dtype;
   return DA2_OK;
 }
 
@@ -145,7 +147,7 @@ Finish plain_finish(OutView y, int64_t H, int64_t C, int64_t N) {
 
 // The workspace of the backward pass, in the order of the fields.
 struct BwdSpace {
-  int64_t dz, dzt, wt, xt, pbias, pgate, product, bytes;
+  int64_t dz, dzt, wt, xt, pbias, pgate, scale, product, bytes;
 };
 BwdSpace bwd_space(const Proj& e, int64_t B, int64_t N) {
   BwdSpace s{};
@@ -163,6 +165,7 @@ BwdSpace bwd_space(const Proj& e, int64_t B, int64_t N) {
   s.xt = take(2 * e.K * e.ldt);
   s.pbias = take(4 * blocks * e.R);
   s.pgate = take(e.parts == 1 ? 4 * blocks * e.F : 0);
+  s.scale = take(e.dtype == DA2_FP16 ? 4 * (1 + dz_tops(e.M, e.F)) : 0);
   int64_t product = 0;
   for (int64_t n = 1; n <= both; ++n)
     product = std::max({product, product_ws_bytes(e.M, N, e.K, n * e.parts * e.F64, 1), product_ws_bytes(e.R, e.F, e.K, n * e.ldt, 1)});
@@ -270,35 +273,50 @@ int32_t backward(const da2_proj* p, int parts, const void* dY, const da2_tensor*
   z.ldt = e.ldt;
   // Over many tokens and features the rounding of dZ averages out to as much as the gradients' own; over a few it need not.
   z.lo = !direct && e.M <= kFewTokens;
+  if (p->dtype == DA2_FP16 && !(plain && !gate) && (dX || dW)) {
+    z.back = reinterpret_cast<float*>(at + s.scale);
+    z.n_tops = dz_tops(e.M, e.F);
+  }
   if (dbias) z.pbias = reinterpret_cast<float*>(at + s.pbias);
   if (dgate) z.pgate = reinterpret_cast<float*>(at + s.pgate);
   z.dbias = dbias;
   z.dgate = dgate;
   z.dgate_sb = gate_stride_b;
   hipError_t err = hipSuccess;
-  if (z.dz || z.dzt || dbias || dgate) err = launch_dz(z, stream);
+  // A copy is made just before the product that reads it (both in front: 3 to 5% slower); with the largest gradients to be found, the
+  // first has to be in front.
+  const auto copy_w = [&](const DzArgs* top) {
+    return launch_transpose(TransposeArgs{Side{W, e.F * w_stride, 0, w_stride, (int)e.F, (int)e.K, parts}, parts, (int)e.K, at + s.wt, e.F64, wide}, top, stream);
+  };
+  const auto copy_x = [&](const DzArgs* top) {
+    return launch_transpose(TransposeArgs{rows_side(X, x, e.x), p->B, (int)e.K, at + s.xt, e.Np, e.ldt}, top, stream);
+  };
+  if (z.back) err = dX ? copy_w(&z) : copy_x(&z);
+  if (err == hipSuccess && (z.dz || z.dzt || dbias || dgate)) err = launch_dz(z, stream);
   ProductArgs a{};
   a.ws = reinterpret_cast<float*>(at + s.product);
   a.parts = 1;
   a.dtype = p->dtype;
   if (err == hipSuccess && dX) {
-    err = launch_transpose(TransposeArgs{Side{W, e.F * w_stride, 0, w_stride, (int)e.F, (int)e.K, parts}, parts, (int)e.K, at + s.wt, e.F64, wide}, stream);
+    if (!z.back) err = copy_w(nullptr);
     a.t = direct ? rows_side(dY, dy, e.y) : Side{z.dz, 0, wide, wide << z.lo, (int)e.M, (int)wide, 1};
     a.lo = z.lo;
     a.K = direct ? (int)e.F : (int)wide;
     a.w = Side{at + s.wt, 0, 0, wide, (int)e.K, a.K, 1};
     a.f = plain_finish(out_view(dX, dx), p->Hx, p->Cx, p->N);
+    a.f.back = z.back;
     a.M = e.M;
     if (err == hipSuccess) err = launch_product(a, stream);
   }
   if (err == hipSuccess && dW) {
-    err = launch_transpose(TransposeArgs{rows_side(X, x, e.x), p->B, (int)e.K, at + s.xt, e.Np, e.ldt}, stream);
+    if (!z.back || dX) err = copy_x(nullptr);
     const int64_t ld = e.ldt << z.lo;
     a.t = Side{at + s.dzt, e.F64 * ld, e.ldt, ld, (int)e.F, (int)e.ldt, parts};
     a.lo = z.lo;
     a.w = Side{at + s.xt, 0, 0, e.ldt, (int)e.K, (int)e.ldt, 1};
     a.K = (int)e.ldt;
     a.f = plain_finish(OutView{dW, e.F * dw_stride, 0, dw_stride}, 1, e.K, e.F);
+    a.f.back = z.back;
     a.M = e.R;
     if (err == hipSuccess) err = launch_product(a, stream);
   }

@@ -26,6 +26,7 @@ struct Finish {
   int Hy, Cy;        // features are Hy blocks of Cy
   float* z;          // the sums, [rows][parts][z_ld], or null
   int64_t z_ld;
+  const float* back; // factor of the sums before anything else (fp16), or null: 1
   int act;           // da2_act
   int N;             // tokens of a sample
   int F;             // features (of each part)
@@ -62,7 +63,13 @@ struct DzArgs {
   float *pbias, *pgate;  // partial sums [B][blocks][parts][F] and [B][blocks][F], or null
   void *dbias, *dgate;
   int64_t dgate_sb;   // 0: one gate for all samples
+  float* back;        // fp16: what undoes the scale of dz, then the n_tops values it comes from; null: dz is not scaled
+  int n_tops;
 };
+// Whether dz of T is stored times a power of two.
+template <typename T>
+constexpr bool kScaledDz = __is_same(T, fp16_t);
+int dz_tops(int64_t M, int64_t F);
 int dz_blocks(int64_t B, int64_t N, int64_t F);
 hipError_t launch_dz(const DzArgs& a, hipStream_t stream);
 
@@ -78,7 +85,8 @@ struct TransposeArgs {  // of 16-bit elements
   void* out;
   int64_t Np, ld;
 };
-hipError_t launch_transpose(const TransposeArgs& a, hipStream_t stream);
+// With top, the same launch finds the largest gradients of the sums, which launch_dz needs (fp16).
+hipError_t launch_transpose(const TransposeArgs& a, const DzArgs* top, hipStream_t stream);
 
 // Norm of the heads of Q and K, then rotary positions.
 struct QkArgs {

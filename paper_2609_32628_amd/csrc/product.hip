@@ -266,6 +266,7 @@ __global__ __launch_bounds__(64 * S::kWaves, 2) void product_kernel(ProductArgs 
   if (mine.unit >= mine.end) return;
   Copies<S> copies(a, tiles_w, tiles_t, splits, lds0, lane, wave);
   copies.step(lds);
+  const float back = back_of<T, MODE == kGated>(a.f);
 
   f32x4 acc[S::kW][S::kT];
   const auto clear = [&] {
@@ -402,7 +403,7 @@ __global__ __launch_bounds__(64 * S::kWaves, 2) void product_kernel(ProductArgs 
           store_vec(to + 4, v + 4);
         }
       } else if (m < a.M && f8 < a.f.F) {
-        finish8<T, GLU>(a.f, row, beside, v, w, f8);
+        finish8<T, GLU>(a.f, row, beside, back, v, w, f8);
       }
     }
     clear();
@@ -435,7 +436,7 @@ __global__ __launch_bounds__(256) void product_join_kernel(ProductArgs a, int sp
     }
   }
   const RowPlace<T, GLU> row(a.f, m);
-  finish8<T, GLU>(a.f, row, Beside<T, GLU>(a.f, row, f8, f8), v, u, f8);
+  finish8<T, GLU>(a.f, row, Beside<T, GLU>(a.f, row, f8, f8), back_of<T, GLU>(a.f), v, u, f8);
 }
 
 // ---- few tokens ------------------------------------------------------------------------
@@ -526,7 +527,7 @@ __global__ __launch_bounds__(64 * kFewWaves, 4) void product_few_kernel(ProductA
 #pragma unroll
       for (int e = 0; e < 8; ++e) v[p][e] += sums[s][m][p * 16 + c * 8 + e];
   const RowPlace<T, GLU> row(a.f, m);
-  finish8<T, GLU>(a.f, row, Beside<T, GLU>(a.f, row, f8, f8), v[0], v[1], f8);
+  finish8<T, GLU>(a.f, row, Beside<T, GLU>(a.f, row, f8, f8), back_of<T, GLU>(a.f), v[0], v[1], f8);
 }
 
 template <typename T, typename S>
