@@ -625,8 +625,8 @@ int32_t da2_linear(const da2_proj* p, const void* X, const da2_tensor* x, const 
  *   dX = dZ W, dW = dZ' X, dbias = column sums of dZ, dgate = those of dY act(Z) (per sample when gate_stride_b > 0).
  * dZ is rounded to the tensors' type for the products with W and X (with neither activation nor gate it
  * is dY itself; up to B*N = 16 it is taken in two such numbers, the second what the first left over, so that an infinity in W or X
- * may give a NaN); fp16 holds it times a power of two that brings its largest finite value to [2^14, 2^15), which the sums are
- * divided by, so that its size does not matter; the column sums are taken in float32 before.
+ * may give a NaN); fp16 holds it times a power of two that brings its largest finite value (here 1.2 dY gate is taken for it, in da2_glu
+ * itself) to [2^14, 2^15), which the sums are divided by, so that its size does not matter; the column sums are taken in float32 before.
  *   Z      what da2_linear wrote; needed with an activation or for dgate
  *   dX     device out per *dx, like X, or NULL; dW device out [F][K], dw_stride elements between the rows, or NULL
  *   dbias  device out [F], or NULL; dgate device out like gate (same gate_stride_b), or NULL

@@ -2,7 +2,8 @@
 subnormal numbers and above its largest, while the results are inside.
 
 Tolerances as in test_gpu_product, but for the rounding of dZ: half a step of itself wherever it lies, or 2^-39 of the largest
-dZ (which is brought to [2^14, 2^15), where 2^-25 is half a step of the smallest numbers); up to 16 tokens in two numbers."""
+dZ (which is brought to [2^14, 2^15), where 2^-25 is half a step of the smallest numbers; of a projection that is the largest
+1.2 dY gate); up to 16 tokens in two numbers."""
 import numpy as np
 import pytest
 import torch
@@ -38,7 +39,8 @@ def check(c):
         g = layer.linear_bwd(f64(c.dY), x, w, Z, c.act, f64(c.gate))
         ed = 2.0 ** -15 * dy * np.abs(layer.rows_gate(f64(c.gate), c.B, c.N))
     dz = np.abs(g["dz"])
-    er = ed + half(t) ** (2 if M <= 16 else 1) * (dz + ed) + 2.0 ** -39 * dz.max()
+    largest = dz.max() if c.glu else 1.2 * 2.0 ** 15 * ed.max()
+    er = ed + half(t) ** (2 if M <= 16 else 1) * (dz + ed) + 2.0 ** -39 * largest
     mag = dz + er
     X = np.abs(layer.flat(x))
     close(c.dX, layer.unflat(g["dx"], *c.dX.shape), layer.unflat(er @ np.abs(w) + (w.shape[0] / 16 + 24) * 2.0 ** -23 * (mag @ np.abs(w)), *c.dX.shape), "dX")
@@ -98,3 +100,13 @@ def test_not_a_number_and_infinities_do_not_move_the_others():
     cols = [f for f in range(136) if f not in (3, 5)]
     assert torch.equal(c.dX[0, 0, rows], dX[0, 0, rows]) and torch.equal(c.dW[cols], dW[cols])
     assert not c.dX[0, 0, [7, 9]].isfinite().any() and not c.dW[[3, 5]].isfinite().any()
+
+
+def test_saturated_everywhere():
+    """Derivatives of 2^-20 and less in every place, of which the scale knows nothing: dZ of 2^-27 keeps its digits."""
+    c = Case(1, 200, 64, 136, "fp16", "sigmoid", bias=True, gate="shared", scale=0.25, dscale=2.0 ** -6)
+    c.bias.copy_(-14.5)
+    dz, g = check(c)
+    assert dz.max() < 2.0 ** -22
+    # dW lies below 2^-14, where fp16's half step is 2^-25 whatever the value
+    assert (np.abs(f64(c.dW) - g["dw"]) <= 2.0 ** -6 * np.abs(g["dw"]).max() / 16 + 2.0 ** -25).all()
