@@ -168,14 +168,14 @@ BwdSpace bwd_space(const Proj& e, int64_t B, int64_t N) {
   s.scale = take(e.dtype == DA2_FP16 ? 4 * (1 + dz_tops(e.M, e.F)) : 0);
   int64_t product = 0;
   for (int64_t n = 1; n <= both; ++n)
-    product = std::max({product, product_ws_bytes(e.M, N, e.K, n * e.parts * e.F64, 1), product_ws_bytes(e.R, e.F, e.K, n * e.ldt, 1)});
+    product = std::max({product, product_ws_bytes(e.M, N, e.K, e.parts * e.F64, 1, n == 2), product_ws_bytes(e.R, e.F, e.K, e.ldt, 1, n == 2)});
   s.product = take(product);
   s.bytes = at;
   return s;
 }
 
 int64_t proj_ws(const Proj& e, int64_t B, int64_t N, bool train) {
-  const int64_t f = product_ws_bytes(e.M, N, e.F, e.K, e.parts);
+  const int64_t f = product_ws_bytes(e.M, N, e.F, e.K, e.parts, false);
   return train ? std::max(f, bwd_space(e, B, N).bytes) : f;
 }
 

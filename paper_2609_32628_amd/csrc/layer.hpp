@@ -44,7 +44,7 @@ struct ProductArgs {
   bool lo;
 };
 // Workspace of a product of M rows, which may be taken N at a time.
-int64_t product_ws_bytes(int64_t M, int64_t N, int64_t F, int64_t K, int parts);
+int64_t product_ws_bytes(int64_t M, int64_t N, int64_t F, int64_t K, int parts, bool lo);
 hipError_t launch_product(const ProductArgs& a, hipStream_t stream);
 
 // Gradients of the sums: dz of a row from dY, the saved sums z, activation and gate.

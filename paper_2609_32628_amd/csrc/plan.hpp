@@ -6,19 +6,26 @@
 namespace da2 {
 
 constexpr int kStep = 64;             // elements of K a step of the tiles
-constexpr int kFewTokens = 16;        // rows of a product by one launch that reads the weights once
-constexpr int64_t kFewSum = 8192;     // elements of the weights' rows that such a workgroup sums over, of both halves of a gated block
-constexpr int64_t kFewFeatures = 4096;
+constexpr int kFewTokens = 16;  // rows of a product by one launch that reads the weights once
 
-// Whether a product of M rows with (parts) F weight rows of K elements takes the kernel for few rows. It does not cut K: a
-// workgroup of 16 features sums over all of it, so long sums go there only where the features give every CU a workgroup, and are cut
-// into parts on tiles otherwise. Measured with 1 and 16 rows, few rows' kernel against tiles, us: K = 2,048, 64 to 4,096 features
-// 11.4 and 11.8 against 14.1 and 14.2; 8,192 x 1,024 11.9 and 17.0 against 14.4 and 14.5; 32,768 x 1,024 38 and 58 against 25 and 26,
-// x 4,096 45 and 61 against 50 and 52; 131,072 x 64 140 and 223 against 27 and 28; gated 4,096: 32,768 98 and 118 against 131 and 133,
-// 2 x 64 features of 8,192 19 and 24 against 14 and 15. Gradients of 16 x 64 weights over 4,096, 16,384 and 200,000 tokens, the whole
-// call: 18, 39 and 363 against 21, 22 and 69.
-inline bool few_rows(int64_t M, int64_t F, int64_t K, int parts) {
-  return M <= kFewTokens && (parts * K <= kFewSum || F >= kFewFeatures);
+// Whether a product of M rows with (parts) F weight rows of K elements takes the kernel for few rows (lo: with rows in two numbers).
+// It does not cut K: a workgroup of 16 features sums over all of it, and reads all M rows for them, which takes as long as 26 of
+// theirs would (52 gated) and the M rows; on tiles a long sum is cut into parts, but rows in two numbers read the weights
+// twice. So long sums go there only with the fewest rows and where the features give every CU a workgroup. Measured, few rows' kernel
+// against tiles, us, with 1 and 16 rows: K = 2,048, 64 to 4,096 features 11.4 and 11.8 against 14.1 and 14.2; 5,120 x 5,120 15 and 21
+// against 19 and 20; gated 2,048 x 2 x 5,504 12 and 14 against 17 and 17; 8,192 x 1,024 12 and 17 against 14 and 15; 8,960 x 1,536 13 and
+// 19 against 17 and 17; 32,768 x 1,024 38 and 58 against 25 and 26; 131,072 x 64 140 and 223 against 27 and 28; gated 8,192 x 2 x 64 19
+// and 24 against 14 and 15; of many features 13,824 x 5,120 34 and 50 against 33 and 34, 32,768 x 4,096 45 and 61 against 50 and 52,
+// gated 5,120 x 2 x 5,120 27 and 32 against 28 and 29. Gradients of 16 x 64 weights over 4,096, 16,384 and 200,000 tokens, the
+// whole call: 18, 39 and 363 against 21, 22 and 69. Two numbers, both passes of 2,048 to 2 x 5,504 features: 94 and 123 against 103 and
+// 119, of 1,536 to 8,960: 66 and 88 against 71 and 83.
+constexpr int64_t kFewSum = 320'000, kFewSumLo = 480'000;
+constexpr int kFewestRows = 4;
+constexpr int64_t kManyFeatures = 4096;
+inline bool few_rows(int64_t M, int64_t F, int64_t K, int parts, bool lo = false) {
+  if (M > kFewTokens) return false;
+  if (M <= kFewestRows && F >= kManyFeatures) return true;
+  return lo ? (26 + 2 * M) * K <= kFewSumLo : (26 * parts + M) * K <= kFewSum;
 }
 
 // How a product is cut otherwise: tiles of 256x256 or 128x128, and parts of K that are joined. The least by these times in us, fitted to
@@ -56,10 +63,10 @@ inline Plan plan_of(int64_t M, int64_t R, int64_t K) {
   return best;
 }
 
-// Bytes of the partial sums of a product of M rows.
-inline int64_t partial_bytes(int64_t M, int64_t F, int64_t K, int parts) {
-  if (few_rows(M, F, K, parts)) return 0;
-  const Plan p = plan_of(M, F * parts, K);
+// Bytes of the partial sums of a product of M rows (lo: on tiles the two numbers are a sum twice as long).
+inline int64_t partial_bytes(int64_t M, int64_t F, int64_t K, int parts, bool lo = false) {
+  if (few_rows(M, F, K, parts, lo)) return 0;
+  const Plan p = plan_of(M, F * parts, lo ? 2 * K : K);
   return p.splits > 1 ? 4 * p.splits * M * ((F * parts + 7) / 8 * 8) : 0;
 }
 

@@ -553,12 +553,12 @@ hipError_t launch_plan(const ProductArgs& a, const Plan& p, hipStream_t stream) 
 
 }  // namespace
 
-int64_t product_ws_bytes(int64_t M, int64_t N, int64_t F, int64_t K, int parts) {
-  return std::max(partial_bytes(M, F, K, parts), M == N ? 0 : partial_bytes(N, F, K, parts));
+int64_t product_ws_bytes(int64_t M, int64_t N, int64_t F, int64_t K, int parts, bool lo) {
+  return std::max(partial_bytes(M, F, K, parts, lo), M == N ? 0 : partial_bytes(N, F, K, parts, lo));
 }
 
 hipError_t launch_product(const ProductArgs& a, hipStream_t stream) {
-  if (few_rows(a.M, a.f.F, a.K, a.parts))
+  if (few_rows(a.M, a.f.F, a.K, a.parts, a.lo))
     return by_dtype(a.dtype, [&](auto t) {
       using T = decltype(t);
       if constexpr (sizeof(T) == 4) {
@@ -575,7 +575,7 @@ hipError_t launch_product(const ProductArgs& a, hipStream_t stream) {
         return hipGetLastError();
       }
     });
-  if (a.lo) {  // K twice over: the tokens' two blocks, and the weights again (still too long for few rows)
+  if (a.lo) {  // K twice over: the tokens' two blocks, and the weights again (which is too long for few rows, too)
     ProductArgs two = a;
     two.lo = false;
     two.w.C = a.K;
