@@ -11,8 +11,10 @@
 // ahead of their use, and one barrier a step. Workgroups stay for as many tiles as there are, and copy the next tile's first
 // step before a tile's epilogue.
 //
-// Measured (bf16): 8,192^3 807 us, 1,362 TFLOP/s (a plain library product 689 us); 8,190 x 5,120 x 2 x 13,824 gated 1,745 us,
-// 1,329 (the library's product without the block 1,785); 32,760 x 1,536 x 4,608 with bias 431 to 443 us, 1,047 to 1,076 (338).
+// Measured (bf16, calls in a row, over several cards): 8,192^3 804 to 820 us, 1,341 to 1,368 TFLOP/s (a plain library product 689 to
+// 702 us); 8,190 x 5,120 x 2 x 13,824 gated 1,740 to 1,854 us, 1,251 to 1,333 (the library's product without the block 1,785 to 1,814);
+// 32,760 x 1,536 x 4,608 with bias 431 to 475 us, 976 to 1,076 (335 to 373). The gated large tile keeps 15 to 17 vector registers in
+// scratch memory, around the loop over K, not in it.
 // Bound by the copies into LDS, which share its ports with the operands' reads: without them the same loop runs at 1,534, and
 // the matrix units are busy 66% of the time; and by the epilogue, during which a CU multiplies nothing: 9 us of a tile of 256,
 // 1.4 a step. Tried and no faster:
@@ -359,7 +361,8 @@ __global__ __launch_bounds__(64 * S::kWaves, 2) void product_kernel(ProductArgs 
       }
     };
     ask(0);
-    // two at a time where registers allow it (32,760 x 1,536 x 4,608: 431 us instead of 453; gated and small tiles 3 and 1% slower)
+    // two at a time where registers allow it (32,760 x 1,536 x 4,608 with bias, both in turn on one card: 455 us instead of 477; with gate
+    // and residual no difference; gated and small tiles 3 and 1% slower)
     constexpr int kTogether = MODE == kLinear && TW == 256 ? 2 : 1;
 #pragma unroll kTogether
     for (int part = 0; part < kParts; ++part) {
@@ -445,7 +448,8 @@ __global__ __launch_bounds__(256) void product_join_kernel(ProductArgs a, int sp
 // products, two of them on their way at a time, and their sums are added up in order in LDS.
 // 4 x 5,120 x 5,120, bf16: 16 us with the launch, 52 MB of weights at 3.3 TB/s; 16 x 2,048 x 2 x 5,504, fp16: 15 us, 45 MB
 // at 3.0. A load takes 64 bytes of 16 rows, and what a CU has on its way bounds it: 16 waves, or four products ahead, are no
-// faster.
+// faster. The tokens' rows are read by every workgroup, 16 of them as many bytes as its weights: 5,120 x 5,120 takes 15 us
+// for one token and 21 for 16. The gated kernel keeps 19 vector registers in scratch memory in its epilogue.
 constexpr int kFew = kFewTokens, kFewWaves = 8, kAhead = 2;
 
 // A chunk of a row, of which `left` elements are the row's; zeros behind them.
