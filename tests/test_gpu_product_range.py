@@ -110,3 +110,35 @@ def test_saturated_everywhere():
     assert dz.max() < 2.0 ** -22
     # dW lies below 2^-14, where fp16's half step is 2^-25 whatever the value
     assert (np.abs(f64(c.dW) - g["dw"]) <= 2.0 ** -6 * np.abs(g["dw"]).max() / 16 + 2.0 ** -25).all()
+
+
+@pytest.mark.parametrize("N", [3, 200])
+@pytest.mark.parametrize("glu", [False, True])
+def test_captured_with_gradients_of_other_sizes(N, glu):
+    """The scale of a replay is that of its own gradients: a step captured once and replayed with gradients of any size gives the
+    eager results bit for bit."""
+    c = Case(2, N, 136, 264, "fp16", act="gelu", bias=True, gate="none" if glu else "adaptive", residual=not glu, glu=glu)
+    c.outputs()
+    ws = torch.empty((api.da2_glu_ws_bytes if glu else api.da2_linear_ws_bytes)(c.X, c.W, c.Y, True), dtype=torch.uint8, device="cuda")
+    names = [n for n in ("Y", "Z", "dX", "dW", "dbias", "dgate") if getattr(c, n) is not None]
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(side):
+        c.run(ws=ws)
+        graph = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(graph, stream=side):
+            c.run(ws=ws)
+        for seed, size in enumerate((1.0, 2.0 ** -16, 2.0 ** 12, 2.0 ** -8, 2.0 ** 4)):
+            g = torch.Generator(device="cuda")
+            g.manual_seed(seed)
+            c.dY.copy_(torch.randn(c.dY.shape, generator=g, device="cuda") * size)
+            for n in names:
+                getattr(c, n).fill_(float("nan"))
+            ws.fill_(0xFF)
+            graph.replay()
+            got = {n: getattr(c, n).clone() for n in names}
+            ws.fill_(0xFF)
+            c.run(ws=ws)
+            side.synchronize()
+            for n in names:
+                assert torch.equal(got[n].nan_to_num(7.0), getattr(c, n).nan_to_num(7.0)), (n, size)
